@@ -55,7 +55,12 @@ typedef enum {
   TR_ERR_HIP = 8          /* a HIP runtime call failed (launch error)                 */
 } tr_status;
 
-typedef enum { TR_BF16 = 0, TR_F32 = 1 } tr_dtype;
+typedef enum {
+  TR_BF16 = 0,
+  TR_F32 = 1,
+  TR_F8E4M3 = 2, /* pages of a cache: OCP e4m3, finite up to 448, no infinities              */
+  TR_F8E8M0 = 3  /* their scales: a byte x stands for 2^(x - 127), 255 for NaN               */
+} tr_dtype;
 
 typedef enum {
   TR_MASK_NONE = 0,        /* every key is visible                                    */
@@ -274,12 +279,82 @@ int64_t tr_schedule_steps(int schedule, int n_devices, int n_inner, int causal, 
 size_t tr_ring_attn_workspace_bytes(const tr_tensor* q, int n_chunks);
 
 /*
+ * A paged K/V cache: what a device keeps of the keys of many sequences (its K_j, V_j of Algorithm 1, sequence by sequence).
+ *   k_pages, v_pages    [n_pages, Hkv, page_size, D] bf16 or e4m3, of one shape and with the same strides; D in {64, 128};
+ *                       page_size a multiple of 16; pointer and strides multiples of 16 bytes, stride_s at most 2^24 elements.
+ *                       Any order of the first three dimensions goes through the strides (a page may hold its keys head by head or
+ *                       token by token, K and V may lie side by side in one array).
+ *   k_scales, v_scales  [n_pages, Hkv, page_size] e8m0, with e4m3 pages only (else NULL): one scale for a key's row of D values.  Same
+ *                       strides for both, stride_s 1, pointer and other strides multiples of 16.  A value is e4m3 * 2^(scale - 127).
+ * Key c of sequence b lies on page page_table[b][c / page_size], in slot c mod page_size.  Several sequences may share pages
+ * that are read.  An entry that is no page (< 0 or >= n_pages) stands for keys that are not there: they are read as masked and
+ * written nowhere, and nothing outside the arrays is touched.
+ *
+ * The sequences.  Device arrays of int32, read by the kernels: a captured graph takes new contents on every replay.
+ *   kv_len[b]   keys of sequence b, new ones among them (taken as 0 .. max_pages * page_size)
+ *   q_start[b]  the new tokens of sequence b are tokens q_start[b] .. q_start[b + 1] - 1 of the call's tensors, which hold the
+ *               tokens of all sequences one behind the other along S (q_start ascends; its values are taken as 0 .. S).  Tokens in front of
+ *               the first and behind the last sequence take part in nothing, their rows of the results are left as they were.
+ *   q_pos[b]    number of the key that stands at the position of sequence b's first new token, NULL: kv_len[b] - its new tokens.
+ *               May be negative or beyond the keys, as on a device that holds a part of a sequence's cache.
+ */
+typedef struct {
+  const int32_t* page_table; /* [n_seqs][max_pages], rows table_stride elements apart */
+  const int32_t* kv_len;     /* [n_seqs]     */
+  const int32_t* q_start;    /* [n_seqs + 1] */
+  const int32_t* q_pos;      /* [n_seqs] or NULL */
+  int64_t n_seqs, max_pages, table_stride;
+} tr_sequences;
+
+/*
+ * Writes K and V of the new tokens into the cache: token i of sequence b as key q_pos[b] + i, if 0 <= q_pos[b] + i < kv_len[b].
+ *   k, v [1,Hkv,S,D] bf16, strides multiples of 8 elements
+ * bf16 pages take the rows as they are.  e4m3 pages: the scale of a row is the smallest power of two, 2^-126 at least, that brings its largest
+ * finite magnitude down to 448 or less (1 for a row of zeros); the values are divided by it, which is exact, and rounded to
+ * nearest even.  An infinity or NaN is stored as NaN.  Each new token needs a slot of its own: two rows of one call in the same slot of a page
+ * leave it with a row, or a scale and a row, of either.
+ */
+tr_status tr_cache_write(const tr_tensor* k, const tr_tensor* v, const tr_tensor* k_pages, const tr_tensor* v_pages,
+                         const tr_tensor* k_scales, const tr_tensor* v_scales, const tr_sequences* seqs, void* hip_stream);
+
+/*
+ * Reads the cache back as dense tensors, what tr_block_attn takes or another device is sent: row s of sequence b is key first + s.
+ *   k, v [n_seqs,Hkv,S,D] bf16 (written), strides multiples of 8 elements; first >= 0
+ * Exact: bf16 holds every e4m3 value times a power of two (down to its own smallest values, 2^-133, below which it rounds).
+ * Rows of keys that are not there (first + s >= kv_len[b], no page) are left as they were.  q_start and q_pos are not used.
+ */
+tr_status tr_cache_read(const tr_tensor* k_pages, const tr_tensor* v_pages, const tr_tensor* k_scales, const tr_tensor* v_scales,
+                        const tr_sequences* seqs, int64_t first, const tr_tensor* k, const tr_tensor* v, void* hip_stream);
+
+/*
+ * Attention of the new tokens of every sequence (a decode step's one, a few drafted ones, a chunk of a prompt, all mixed)
+ * on the keys in its pages: for token i of sequence b, with g = h / (Hq / Hkv), over the keys c < kv_len[b] and, with causal != 0,
+ * c <= q_pos[b] + i:
+ *   out[0,h,q_start[b]+i,:] = sum_c softmax_c(scale * <q[0,h,q_start[b]+i,:], K_c>) V_c
+ *   lse[0,h,q_start[b]+i]   = ln sum_c exp(scale * <q[0,h,q_start[b]+i,:], K_c>)
+ *   q [1,Hq,S,D] bf16      out [1,Hq,S,D] bf16 or fp32 (written)      lse [1,Hq,S] fp32 (written)
+ * A block result like tr_block_attn's: results on the parts of a cache that several devices hold are folded by tr_merge or
+ * tr_merge_n.  A token that sees no key gets out = 0, lse = -inf.  What lies at masked keys (infinities, NaN, slots never written) reaches no result.
+ * Arithmetic as tr_block_attn's; e4m3 values enter it exactly.
+ *   workspace: device memory through which long key ranges are shared out among workgroups, 256-byte aligned, at least
+ *   tr_paged_attn_workspace_bytes() bytes; its contents on return are unspecified, and it need not be initialised.  It serves one call at a
+ *   time: calls (replayed graphs too) that may run at once need one each.  NULL: a row's keys are one workgroup's work, the same
+ *   result up to rounding, slower where few tokens see many keys.
+ * The result is bitwise reproducible, given or not given the workspace.  Nothing is allocated; may be captured.
+ */
+tr_status tr_paged_attn(const tr_tensor* q, const tr_tensor* k_pages, const tr_tensor* v_pages, const tr_tensor* k_scales,
+                        const tr_tensor* v_scales, const tr_sequences* seqs, int causal, float scale, const tr_tensor* out,
+                        const tr_tensor* lse, void* workspace, size_t workspace_bytes, void* hip_stream);
+/* (0 on invalid arguments, and where no keys would be shared out.) */
+size_t tr_paged_attn_workspace_bytes(const tr_tensor* q, const tr_tensor* k_pages, int64_t n_seqs, int64_t max_pages);
+
+/*
  * Measurement aid (no operation of the paper): arms two hipEvent_t handles (either may be
  * NULL; both NULL disarms) for the calling thread.  The next kernel any entry point launches
  * from this thread carries them in its dispatch: start_event then holds the time the kernel
  * began executing and stop_event the time it finished, so hipEventElapsedTime(start, stop)
  * is the kernel's own duration without queueing gaps.  Only that one launch is timed
- * (tr_ring_attn: its first kernel; a block step whose keys are cut: its attention, not the fold); the events stay owned by the caller.  Always TR_OK.
+ * (tr_ring_attn: its first kernel; a block step whose keys are cut, tr_paged_attn: its attention, not the fold); the events stay owned by the caller.  Always TR_OK.
  */
 tr_status tr_time_next_kernel(void* start_event, void* stop_event);
 

@@ -15,7 +15,7 @@ import torch
 _PKG_DIR = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_PKG_DIR, "libtokenring.so")
 
-TR_BF16, TR_F32 = 0, 1
+TR_BF16, TR_F32, TR_F8E4M3, TR_F8E8M0 = 0, 1, 2, 3
 TR_MASK_NONE, TR_MASK_CAUSAL_DIAG = 0, 1
 TR_SCHED_TOKENRING, TR_SCHED_RING_ATTENTION, TR_SCHED_ZIGZAG, TR_SCHED_HYBRID = 0, 1, 2, 3
 
@@ -31,6 +31,14 @@ class TrTensor(ctypes.Structure):
         ("ptr", ctypes.c_void_p), ("dtype", ctypes.c_int32),
         ("B", ctypes.c_int64), ("H", ctypes.c_int64), ("S", ctypes.c_int64), ("D", ctypes.c_int64),
         ("stride_b", ctypes.c_int64), ("stride_h", ctypes.c_int64), ("stride_s", ctypes.c_int64),
+    ]
+
+
+class TrSequences(ctypes.Structure):
+    """Mirror of `tr_sequences` in include/tokenring.h."""
+    _fields_ = [
+        ("page_table", ctypes.c_void_p), ("kv_len", ctypes.c_void_p), ("q_start", ctypes.c_void_p), ("q_pos", ctypes.c_void_p),
+        ("n_seqs", ctypes.c_int64), ("max_pages", ctypes.c_int64), ("table_stride", ctypes.c_int64),
     ]
 
 
@@ -83,6 +91,15 @@ def _load():
     lib.tr_schedule_steps.restype = ctypes.c_int64
     lib.tr_ring_attn_workspace_bytes.argtypes = [P, ctypes.c_int]
     lib.tr_ring_attn_workspace_bytes.restype = ctypes.c_size_t
+    G = ctypes.POINTER(TrSequences)
+    lib.tr_cache_write.argtypes = [P, P, P, P, P, P, G, ctypes.c_void_p]
+    lib.tr_cache_write.restype = ctypes.c_int
+    lib.tr_cache_read.argtypes = [P, P, P, P, G, ctypes.c_int64, P, P, ctypes.c_void_p]
+    lib.tr_cache_read.restype = ctypes.c_int
+    lib.tr_paged_attn.argtypes = [P, P, P, P, P, G, ctypes.c_int, ctypes.c_float, P, P, ctypes.c_void_p, ctypes.c_size_t, ctypes.c_void_p]
+    lib.tr_paged_attn.restype = ctypes.c_int
+    lib.tr_paged_attn_workspace_bytes.argtypes = [P, P, ctypes.c_int64, ctypes.c_int64]
+    lib.tr_paged_attn_workspace_bytes.restype = ctypes.c_size_t
     lib.tr_last_error.argtypes = []
     lib.tr_last_error.restype = ctypes.c_char_p
     lib.tr_version.argtypes = []
@@ -255,3 +272,36 @@ def tr_ring_attn(q, k, v, n_chunks, causal, out, lse, scale=0.0, workspace=None,
 def tr_ring_attn_noalloc(q, k, v, n_chunks, causal, out, lse, scale=0.0, stream=None):
     """tr_ring_attn with the promise that nothing is allocated, for problems up to a limit (see tokenring.h)."""
     _check(_native.ring_attn_noalloc(q, k, v, n_chunks, causal, out, lse, scale, stream))
+
+
+def _shape(t: torch.Tensor) -> TrTensor:
+    """Descriptor of sizes alone, for questions about them."""
+    return TrTensor(None, 0, *t.shape, 0, 0, 0)
+
+
+def tr_cache_write(k, v, k_pages, v_pages, page_table, kv_len, q_start, k_scales=None, v_scales=None, q_pos=None, stream=None):
+    """Writes K and V of the new tokens of every sequence into the pages of a cache, e4m3 pages with their scales (see tokenring.h).
+
+    k, v: [1,Hkv,S,D]; pages: [n_pages,Hkv,page_size,D], scales: [n_pages,Hkv,page_size]; page_table [n_seqs,max_pages],
+    kv_len [n_seqs], q_start [n_seqs + 1] and q_pos [n_seqs]: int32.  Here and below every tensor is on the current GPU.
+    """
+    _check(_native.cache_write(k, v, k_pages, v_pages, page_table, kv_len, q_start, k_scales, v_scales, q_pos, stream))
+
+
+def tr_cache_read(k_pages, v_pages, page_table, kv_len, k, v, first=0, k_scales=None, v_scales=None, stream=None):
+    """k, v [n_seqs,Hkv,S,D] <- keys first, first + 1, ... of every sequence; rows of keys that are not there are left (see tokenring.h)."""
+    _check(_native.cache_read(k_pages, v_pages, page_table, kv_len, k, v, first, k_scales, v_scales, stream))
+
+
+def tr_paged_attn(q, k_pages, v_pages, page_table, kv_len, q_start, causal, scale, out, lse, k_scales=None, v_scales=None, q_pos=None,
+                  workspace=None, stream=None):
+    """out, lse <- attention of the new tokens of every sequence, q [1,Hq,S,D], on the keys in its pages (see tokenring.h).
+
+    `workspace`: None, or a caller-owned device tensor of at least tr_paged_attn_workspace_bytes(q, k_pages, page_table) bytes.
+    """
+    _check(_native.paged_attn(q, k_pages, v_pages, page_table, kv_len, q_start, causal, scale, out, lse, k_scales, v_scales, q_pos, workspace, stream))
+
+
+def tr_paged_attn_workspace_bytes(q, k_pages, page_table) -> int:
+    """Bytes of a workspace for tr_paged_attn on tensors of these shapes."""
+    return int(_lib.tr_paged_attn_workspace_bytes(ctypes.byref(_shape(q)), ctypes.byref(_shape(k_pages)), *page_table.shape))

@@ -10,83 +10,19 @@
 #include <mutex>
 #include <vector>
 
+#include "checks.h"
 #include "tr_internal.h"
 
 namespace {
 
+using tr::check_tensor;
+using tr::check_written;
+using tr::elem_bytes;
+using tr::fail;
+using tr::overlaps;
+
 thread_local char g_err[512] = "";
 thread_local tr::TimingEvents g_timing = {nullptr, nullptr};
-
-tr_status fail(tr_status st, const char* fmt, ...) {
-  va_list ap;
-  va_start(ap, fmt);
-  vsnprintf(g_err, sizeof(g_err), fmt, ap);
-  va_end(ap);
-  return st;
-}
-
-int64_t elem_bytes(int32_t dtype) { return dtype == TR_BF16 ? 2 : 4; }
-
-// Number of elements from ptr to one past the last addressed element of the view.
-int64_t extent_elems(const tr_tensor* t) {
-  if (t->B == 0 || t->H == 0 || t->S == 0 || t->D == 0) return 0;
-  return (t->B - 1) * t->stride_b + (t->H - 1) * t->stride_h + (t->S - 1) * t->stride_s + t->D;
-}
-
-bool overlaps(const tr_tensor* a, const tr_tensor* b) {
-  const int64_t ea = extent_elems(a) * elem_bytes(a->dtype), eb = extent_elems(b) * elem_bytes(b->dtype);
-  if (ea == 0 || eb == 0) return false;
-  const uintptr_t a0 = (uintptr_t)a->ptr, b0 = (uintptr_t)b->ptr;
-  return a0 < b0 + (uintptr_t)eb && b0 < a0 + (uintptr_t)ea;
-}
-
-// Common checks of one descriptor. `row_align` = required multiple (in elements) of the strides
-// and byte alignment of the pointer for vector access.
-tr_status check_tensor(const char* name, const tr_tensor* t, bool allow_bf16, bool allow_f32, int row_align_bytes) {
-  if (!t) return fail(TR_ERR_NULL, "%s: descriptor is NULL", name);
-  if (t->dtype != TR_BF16 && t->dtype != TR_F32) return fail(TR_ERR_DTYPE, "%s: unknown dtype %d", name, (int)t->dtype);
-  if ((t->dtype == TR_BF16 && !allow_bf16) || (t->dtype == TR_F32 && !allow_f32))
-    return fail(TR_ERR_DTYPE, "%s: dtype %s not supported for this argument", name, t->dtype == TR_BF16 ? "bf16" : "fp32");
-  if (t->B < 0 || t->H < 0 || t->S < 0 || t->D < 0) return fail(TR_ERR_SHAPE, "%s: negative dimension", name);
-  if (t->B > INT32_MAX || t->H > INT32_MAX || t->S > (1 << 30) || t->D > INT32_MAX)
-    return fail(TR_ERR_SHAPE, "%s: dimension too large", name);
-  const bool empty = extent_elems(t) == 0;
-  if (!empty && !t->ptr) return fail(TR_ERR_NULL, "%s: data pointer is NULL", name);
-  if (t->stride_b < 0 || t->stride_h < 0 || t->stride_s < 0) return fail(TR_ERR_STRIDE, "%s: negative stride", name);
-  if (!empty) {
-    if (t->S > 1 && t->stride_s < t->D) return fail(TR_ERR_STRIDE, "%s: stride_s %lld smaller than D %lld", name, (long long)t->stride_s, (long long)t->D);
-    const int64_t eb = elem_bytes(t->dtype);
-    if (row_align_bytes > 1) {
-      if (((uintptr_t)t->ptr) % row_align_bytes) return fail(TR_ERR_STRIDE, "%s: pointer not %d-byte aligned", name, row_align_bytes);
-      if ((t->stride_b * eb) % row_align_bytes || (t->stride_h * eb) % row_align_bytes || (t->stride_s * eb) % row_align_bytes)
-        return fail(TR_ERR_STRIDE, "%s: strides must be multiples of %d bytes", name, row_align_bytes);
-    }
-  }
-  return TR_OK;
-}
-
-// A tensor the kernels write must not address one element through two index tuples (a zero or
-// too small stride on a dimension larger than 1): rows are updated by different waves, so an
-// overlapping view would race.  Sufficient test: ordered by stride, every dimension must step
-// over the whole extent of the dimensions inside it.
-tr_status check_written(const char* name, const tr_tensor* t) {
-  if (extent_elems(t) == 0) return TR_OK;
-  int64_t size[3] = {t->B, t->H, t->S}, stride[3] = {t->stride_b, t->stride_h, t->stride_s};
-  for (int i = 0; i < 3; i++)
-    for (int j = i + 1; j < 3; j++)
-      if (stride[j] < stride[i]) {
-        const int64_t a = size[i], b = stride[i];
-        size[i] = size[j]; stride[i] = stride[j];
-        size[j] = a; stride[j] = b;
-      }
-  int64_t inner = t->D;
-  for (int i = 0; i < 3; i++) {
-    if (size[i] <= 1) continue;
-    if (stride[i] < inner) return fail(TR_ERR_STRIDE, "%s: a written tensor must not overlap itself (stride %lld < %lld elements inside it)", name, (long long)stride[i], (long long)inner);
-    inner = stride[i] * (size[i] - 1) + inner;
-  }
-  return TR_OK;
-}
 
 // One block step of a schedule: Query segment qs attends K/V segment ks (equal segments of S),
 // or, with ks2 >= 0, the pair of K/V segments ks and ks2 as one key range.
@@ -728,6 +664,14 @@ size_t align_up(size_t x) { return (x + kWsAlign - 1) / kWsAlign * kWsAlign; }
 }  // namespace
 
 namespace tr {
+tr_status fail(tr_status st, const char* fmt, ...) {
+  va_list ap;
+  va_start(ap, fmt);
+  vsnprintf(g_err, sizeof(g_err), fmt, ap);
+  va_end(ap);
+  return st;
+}
+void clear_error() { g_err[0] = 0; }
 TimingEvents take_timing_events() {
   const TimingEvents ev = g_timing;
   g_timing = {nullptr, nullptr};

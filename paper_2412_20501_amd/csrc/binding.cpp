@@ -94,6 +94,132 @@ bool to_stream(PyObject* obj, void*& stream) {
   return ok;
 }
 
+// ---- operands of the operators on a paged cache: more types, arrays of int32, None for what is left out; all on the current GPU.
+
+// Checks where a tensor lies: -2: none seen yet.
+struct Place {
+  int device = -2;
+  bool take(const at::Tensor& t) {
+    const int at = t.is_cuda() ? (int)t.get_device() : -1;
+    if (device == -2) {
+      int64_t current = -1;
+      if (at >= 0 && get_device != Py_None) {
+        PyObject* now = PyObject_CallNoArgs(get_device);
+        const bool ok = now && to_int(now, current);
+        Py_XDECREF(now);
+        if (!ok) return false;
+      }
+      if (at < 0 || at != current) {
+        PyErr_SetString(PyExc_ValueError, "tensors must be on the current GPU");
+        return false;
+      }
+      device = at;
+    } else if (device != at) {
+      PyErr_SetString(PyExc_ValueError, "tensors are on different devices");
+      return false;
+    }
+    return true;
+  }
+};
+
+const at::Tensor* strided(PyObject* obj, Place& place) {
+  if (!THPVariable_Check(obj)) {
+    PyErr_Format(PyExc_TypeError, "a tensor is expected, not %s", Py_TYPE(obj)->tp_name);
+    return nullptr;
+  }
+  const at::Tensor& t = THPVariable_Unpack(obj);
+  if (t.layout() != at::kStrided) {
+    PyErr_SetString(PyExc_ValueError, "a strided tensor is expected");
+    return nullptr;
+  }
+  return place.take(t) ? &t : nullptr;
+}
+
+// [B,H,S,D] or [B,H,S]; optional: None gives no descriptor (at stays null).
+struct Operand {
+  tr_tensor d;
+  const tr_tensor* at = nullptr;
+  bool take(PyObject* obj, Place& place, bool optional = false) {
+    if (optional && obj == Py_None) return true;
+    try {
+      const at::Tensor* t = strided(obj, place);
+      if (!t) return false;
+      const auto type = t->scalar_type();
+      const int64_t n = t->dim();
+      if (type == at::kBFloat16) d.dtype = TR_BF16;
+      else if (type == at::kFloat) d.dtype = TR_F32;
+      else if (type == at::kFloat8_e4m3fn) d.dtype = TR_F8E4M3;
+      else if (type == at::kFloat8_e8m0fnu) d.dtype = TR_F8E8M0;
+      else {
+        PyErr_SetString(PyExc_TypeError, "unsupported dtype");
+        return false;
+      }
+      if (n != 3 && n != 4) {
+        PyErr_SetString(PyExc_ValueError, "expected a [B,H,S,D] or [B,H,S] tensor");
+        return false;
+      }
+      const auto size = t->sizes(), stride = t->strides();
+      if (n == 4 && size[3] > 1 && stride[3] != 1) {
+        PyErr_SetString(PyExc_ValueError, "innermost (D) stride must be 1");
+        return false;
+      }
+      d.ptr = t->data_ptr();
+      d.B = size[0]; d.H = size[1]; d.S = size[2]; d.D = n == 4 ? size[3] : 1;
+      d.stride_b = stride[0]; d.stride_h = stride[1]; d.stride_s = stride[2];
+      at = &d;
+      return true;
+    } catch (const std::exception& e) {   // no storage, symbolic sizes and the like
+      PyErr_SetString(PyExc_RuntimeError, e.what());
+      return false;
+    }
+  }
+};
+
+// An int32 array of `dims` dimensions whose last one is dense; elems (if not negative): its elements.
+bool indices(PyObject* obj, const char* name, int64_t dims, int64_t elems, Place& place, const at::Tensor*& t) {
+  t = strided(obj, place);
+  if (!t) return false;
+  if (t->scalar_type() != at::kInt) {
+    PyErr_Format(PyExc_TypeError, "%s must be int32", name);
+    return false;
+  }
+  if (t->dim() != dims || (t->size(dims - 1) > 1 && t->stride(dims - 1) != 1)) {
+    PyErr_Format(PyExc_ValueError, "%s must have %lld dimension(s), the last one dense", name, (long long)dims);
+    return false;
+  }
+  if (elems >= 0 && t->numel() != elems) {
+    PyErr_Format(PyExc_ValueError, "%s must have %lld elements, not %lld", name, (long long)elems, (long long)t->numel());
+    return false;
+  }
+  return true;
+}
+
+bool take_sequences(PyObject* table, PyObject* kv_len, PyObject* q_start, PyObject* q_pos, Place& place, tr_sequences& s) {
+  try {
+    const at::Tensor* t;
+    if (!indices(table, "page_table", 2, -1, place, t)) return false;
+    s.page_table = (const int32_t*)t->data_ptr();
+    s.n_seqs = t->size(0);
+    s.max_pages = t->size(1);
+    s.table_stride = s.n_seqs > 1 ? t->stride(0) : s.max_pages;
+    if (!indices(kv_len, "kv_len", 1, s.n_seqs, place, t)) return false;
+    s.kv_len = (const int32_t*)t->data_ptr();
+    s.q_start = s.q_pos = nullptr;
+    if (q_start) {
+      if (!indices(q_start, "q_start", 1, s.n_seqs + 1, place, t)) return false;
+      s.q_start = (const int32_t*)t->data_ptr();
+    }
+    if (q_pos && q_pos != Py_None) {
+      if (!indices(q_pos, "q_pos", 1, s.n_seqs, place, t)) return false;
+      s.q_pos = (const int32_t*)t->data_ptr();
+    }
+    return true;
+  } catch (const std::exception& e) {
+    PyErr_SetString(PyExc_RuntimeError, e.what());
+    return false;
+  }
+}
+
 bool argc_is(Py_ssize_t n, Py_ssize_t want) {
   if (n != want) PyErr_Format(PyExc_TypeError, "%zd arguments expected, %zd given", want, n);
   return n == want;
@@ -221,6 +347,59 @@ PyObject* ring_attn_blocks(PyObject*, PyObject* const* a, Py_ssize_t n) {   // q
     return tr_ring_attn_blocks(&t.q, &t.k, &t.v, (int)chunks, (int)causal, &t.out, &t.lse, scale, (int)dtype, (void*)(uintptr_t)ws, (size_t)bytes, stream);
   });
 }
+PyObject* cache_write(PyObject*, PyObject* const* a, Py_ssize_t n) {   // k, v, k_pages, v_pages, page_table, kv_len, q_start, k_scales, v_scales, q_pos, stream
+  Place place;
+  Operand k, v, kp, vp, ks, vs;
+  tr_sequences s;
+  void* stream;
+  if (!argc_is(n, 11) || !k.take(a[0], place) || !v.take(a[1], place) || !kp.take(a[2], place) || !vp.take(a[3], place) ||
+      !take_sequences(a[4], a[5], a[6], a[9], place, s) || !ks.take(a[7], place, true) || !vs.take(a[8], place, true) || !to_stream(a[10], stream))
+    return nullptr;
+  return call([&] { return tr_cache_write(k.at, v.at, kp.at, vp.at, ks.at, vs.at, &s, stream); });
+}
+PyObject* cache_read(PyObject*, PyObject* const* a, Py_ssize_t n) {   // k_pages, v_pages, page_table, kv_len, k, v, first, k_scales, v_scales, stream
+  Place place;
+  Operand k, v, kp, vp, ks, vs;
+  tr_sequences s;
+  int64_t first;
+  void* stream;
+  if (!argc_is(n, 10) || !kp.take(a[0], place) || !vp.take(a[1], place) || !take_sequences(a[2], a[3], nullptr, nullptr, place, s) ||
+      !k.take(a[4], place) || !v.take(a[5], place) || !to_int(a[6], first) || !ks.take(a[7], place, true) || !vs.take(a[8], place, true) ||
+      !to_stream(a[9], stream))
+    return nullptr;
+  return call([&] { return tr_cache_read(kp.at, vp.at, ks.at, vs.at, &s, first, k.at, v.at, stream); });
+}
+// q, k_pages, v_pages, page_table, kv_len, q_start, causal, scale, out, lse, k_scales, v_scales, q_pos, workspace, stream
+PyObject* paged_attn(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  Place place;
+  Operand q, kp, vp, out, lse, ks, vs;
+  tr_sequences s;
+  int64_t causal;
+  float scale;
+  void *stream, *ws = nullptr;
+  size_t bytes = 0;
+  if (!argc_is(n, 15) || !q.take(a[0], place) || !kp.take(a[1], place) || !vp.take(a[2], place) || !take_sequences(a[3], a[4], a[5], a[12], place, s) ||
+      !to_bool(a[6], causal) || !to_float(a[7], scale) || !out.take(a[8], place) || !lse.take(a[9], place) || !ks.take(a[10], place, true) ||
+      !vs.take(a[11], place, true))
+    return nullptr;
+  if (a[13] != Py_None) {
+    try {
+      const at::Tensor* t = strided(a[13], place);
+      if (!t) return nullptr;
+      if (!t->is_contiguous()) {
+        PyErr_SetString(PyExc_ValueError, "the workspace must be contiguous");
+        return nullptr;
+      }
+      ws = t->data_ptr();
+      bytes = (size_t)t->nbytes();
+    } catch (const std::exception& e) {
+      PyErr_SetString(PyExc_RuntimeError, e.what());
+      return nullptr;
+    }
+  }
+  if (!to_stream(a[14], stream)) return nullptr;
+  return call([&] { return tr_paged_attn(q.at, kp.at, vp.at, ks.at, vs.at, &s, (int)causal, scale, out.at, lse.at, ws, bytes, stream); });
+}
 PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t n) {
   if (!argc_is(n, 5)) return nullptr;
   PyObject** const slots[5] = {&packer, &is_initialized, &get_device, &raw_stream, &stream_of};
@@ -236,7 +415,7 @@ PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t n) {
 #define TR_METHOD(name) {#name, (PyCFunction)(void (*)(void))name, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {TR_METHOD(bind), TR_METHOD(block_attn), TR_METHOD(block_attn_merge), TR_METHOD(block_attn_causal_at), TR_METHOD(merge),
                          TR_METHOD(merge_n), TR_METHOD(ring_attn), TR_METHOD(ring_attn_noalloc), TR_METHOD(ring_attn_sched),
-                         TR_METHOD(ring_attn_blocks), {nullptr, nullptr, 0, nullptr}};
+                         TR_METHOD(ring_attn_blocks), TR_METHOD(cache_write), TR_METHOD(cache_read), TR_METHOD(paged_attn), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_native", "Calls into libtokenring with torch tensors; status codes come back.", -1, methods,
                       nullptr, nullptr, nullptr, nullptr};
 

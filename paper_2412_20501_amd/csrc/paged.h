@@ -1,0 +1,72 @@
+// Internal declarations of the operators on a paged cache.
+#pragma once
+#include "paged_plan.h"
+#include "tr_internal.h"
+
+namespace tr {
+
+// Arguments of the kernels that copy between dense tensors and pages.
+struct CacheCopyParams {
+  Sequences seq;
+  const char* k;   // new tokens, bf16
+  const char* v;
+  char* k_out;     // dense result, bf16
+  char* v_out;
+  char* k_pages;
+  char* v_pages;
+  unsigned char* k_scales;
+  unsigned char* v_scales;
+  int64_t d_sb, d_sh, d_ss;         // of the dense tensors, in elements
+  int64_t page_b, head_b, slot_b;   // of the pages, in bytes
+  int64_t scale_sp, scale_sh;
+  int heads;        // K/V heads
+  Divisor by_heads;
+  int rows;         // read: rows of a sequence's result
+  int64_t first;    // read: key of row 0
+};
+hipError_t launch_cache_write(const CacheCopyParams& p, int D, bool f8, hipStream_t stream);
+hipError_t launch_cache_read(const CacheCopyParams& p, int D, bool f8, hipStream_t stream);
+
+// Arguments of the attention kernel on pages and of its fold.
+struct PagedParams {
+  Sequences seq;
+  const __bf16* q;
+  void* out;     // bf16 or fp32
+  float* lse;
+  const char* k_pages;
+  const char* v_pages;
+  const unsigned char* k_scales;
+  const unsigned char* v_scales;
+  int64_t q_sh, q_ss, o_sh, o_ss, l_sh, l_ss;
+  int64_t page_b, head_b;   // bytes
+  int slot_b;               // bytes, at most 2^25
+  int64_t scale_sp, scale_sh;
+  int Hkv, gq;
+  Divisor by_gq;
+  int causal, out_f32;
+  float scale;
+  int target;      // workgroups among which the keys are shared out, 0: they are not
+  int least_part;  // keys of a part at least
+  float* part_out; // [2 * target slots][rows of a tile][D]
+  float* part_lse; // [2 * target slots][rows of a tile]
+};
+
+// How a call is launched: the form of its row tiles and the workgroups that share its keys.
+struct PagedLaunch {
+  int rows;        // of a tile
+  int target;      // as above, where a workspace is there
+  int64_t tiles;   // of all sequences and K/V heads, at most
+};
+PagedLaunch paged_launch(int64_t tokens, int64_t n_seqs, int64_t max_keys, int Hkv, int gq, int D);
+hipError_t launch_paged_attn(const PagedParams& p, const PagedLaunch& l, int D, bool f8, hipStream_t stream);
+
+#if defined(__HIPCC__)
+// Two e4m3 values (the upper ones of x, if upper) times 2^(scale - 127), as two bf16: the conversion takes the scale as the exponent of a float.
+// That float is 2^(scale - 127) for 1 .. 254; 0, whose 2^-127 no normal float has, goes through half of 2^-126, and 255 is a NaN.
+__device__ __forceinline__ unsigned f8_pair(unsigned x, bool upper, unsigned scale) {
+  const float s = __builtin_bit_cast(float, scale << 23);
+  return __builtin_bit_cast(unsigned, upper ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x, s, true) : __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x, s, false));
+}
+#endif
+
+}  // namespace tr

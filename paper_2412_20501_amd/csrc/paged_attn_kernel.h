@@ -1,0 +1,518 @@
+// Attention of new tokens on a paged cache (tr_paged_attn) for gfx950.
+#pragma once
+#include "paged.h"
+
+namespace tr {
+namespace {
+
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
+typedef unsigned u32x2 __attribute__((ext_vector_type(2)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+
+constexpr float kLog2e = 1.4426950408889634f;
+
+// ---- Which work a workgroup has.
+//
+// The lengths lie in device memory, so the launch does not know them: it has as many workgroups as the shapes allow work items, and every
+// workgroup finds its own item, by sums over the sequences that each of its waves takes for itself (64 sequences a load).  An item
+// is a row tile of a K/V head of a sequence on one part of the keys; parts are as long as makes all items about target (part_keys).
+__device__ __forceinline__ int wave_scan(int x) {   // sum over the lanes up to and including this one
+#pragma unroll
+  for (int d = 1; d < 64; d *= 2) {
+    const int y = __shfl_up(x, d);
+    if ((int)(threadIdx.x & 63) >= d) x += y;
+  }
+  return x;
+}
+__device__ __forceinline__ int64_t wave_sum(int64_t x) {
+#pragma unroll
+  for (int d = 32; d > 0; d /= 2) x += __shfl_xor(x, d);
+  return x;
+}
+__device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
+
+// Sums count(b) over the sequences up to the one that holds element `at`: true, and its b and the sum before it; false, and the sum of all.
+template <typename Count>
+__device__ __forceinline__ bool locate(int n, int at, Count count, int& b, int& before) {
+  const int lane = threadIdx.x & 63;
+  before = 0;
+  for (int b0 = 0; b0 < n; b0 += 64) {
+    const int c = b0 + lane < n ? count(b0 + lane) : 0, upto = wave_scan(c);
+    const unsigned long long over = __ballot(at < before + upto);
+    if (over) {
+      const int i = __builtin_ctzll(over);
+      b = b0 + i;
+      before += __builtin_amdgcn_readlane(upto - c, i);
+      return true;
+    }
+    before += __builtin_amdgcn_readlane(upto, 63);
+  }
+  return false;
+}
+
+// Keys of a part of this call.
+__device__ __forceinline__ int plan_part(const PagedParams& p, int tile) {
+  int64_t work = 0;
+  if (p.target > 0) {
+    for (int b = threadIdx.x & 63; b < p.seq.n; b += 64) {
+      const Sequence q = sequence(p.seq, b);
+      work += (int64_t)tiles_of(q.n * p.gq, tile) * q.len;
+    }
+    work = wave_sum(work) * p.Hkv;
+  }
+  return uniform(part_keys(work, p.target, p.least_part));
+}
+
+struct Item {
+  int b, hk, tile, part, n_parts;   // n_parts: live ones, those whose keys some row of the tile sees, and the first one
+  int k0, k1;                       // its keys
+  int slot;                         // of the scratch, if n_parts > 1
+  Sequence q;
+};
+
+// Rows of a tile see keys 0 .. limit(row) - 1; row r of a sequence and K/V head is query head r mod gq of token r / gq.
+__device__ __forceinline__ int row_limit(const PagedParams& p, const Sequence& q, int r) { return visible(q, divide(p.by_gq, r), p.causal); }
+
+// The item of workgroup `id` of `ids`; false: none.  The items of a K/V head and part lie next to each other, and each XCD has a contiguous
+// eighth of all, so that row tiles which read the same keys mostly share an L2.
+__device__ __forceinline__ bool find_item(const PagedParams& p, int tile, int id, Item& w) {
+  const int part = plan_part(p, tile);
+  auto items = [&](int b) {
+    const Sequence q = sequence(p.seq, b);
+    return tiles_of(q.n * p.gq, tile) * parts_of(q.len, part) * p.Hkv;
+  };
+  int before, b = 0;
+  locate(p.seq.n, 0x7fffffff, items, b, before);
+  const int total = before, each = (total + 7) >> 3, at = (id & 7) * each + (id >> 3);
+  if ((id >> 3) >= each || at >= total) return false;
+  if (!locate(p.seq.n, at, items, b, before)) return false;
+  w.b = uniform(b);
+  w.q = sequence(p.seq, w.b);
+  const int parts = uniform(parts_of(w.q.len, part)), tiles = uniform(tiles_of(w.q.n * p.gq, tile)), i = uniform(at - before);
+  const int unit = i / tiles;                 // K/V head, part
+  w.tile = tiles - 1 - (i - unit * tiles);    // the last tiles, which see the most keys, first
+  w.hk = unit / parts;
+  w.part = unit - w.hk * parts;
+  const int last = min((w.tile + 1) * tile, w.q.n * p.gq) - 1;
+  const int seen = row_limit(p, w.q, last);
+  w.n_parts = parts_of(seen, part);
+  w.k0 = w.part * part;
+  w.k1 = w.part + 1 < w.n_parts ? w.k0 + part : seen;
+  if (w.part >= w.n_parts) return false;
+  if (parts > 1) {   // its scratch slot: among the items of sequences whose keys are cut
+    auto cut = [&](int s) {
+      const Sequence q = sequence(p.seq, s);
+      const int n = parts_of(q.len, part);
+      return n > 1 ? tiles_of(q.n * p.gq, tile) * n * p.Hkv : 0;
+    };
+    int base = 0;
+    for (int b0 = 0; b0 < w.b; b0 += 64) {
+      const int s = b0 + (int)(threadIdx.x & 63);
+      base += __builtin_amdgcn_readlane(wave_scan(s < w.b ? cut(s) : 0), 63);
+    }
+    w.slot = base + (w.hk * tiles + w.tile) * parts + w.part;
+    if (w.slot < 0 || w.slot >= 2 * p.target) return false;   // (only where sequences overlap)
+  } else {
+    w.slot = 0;
+  }
+  return true;
+}
+
+// ---- Few rows.
+//
+// Items of at most 16 * RT rows (a decode step's query heads of a K/V head, drafted tokens).  Each of the four waves takes every fourth
+// stretch of 32 keys on its own, straight from memory into registers, and the waves' results are added up at the end.  Scores are computed
+// transposed, S^T = K Q^T, with 16x16x32 products: A is K as it lies in memory, lane (i = lane % 16, g = lane / 16) then holds
+// scores of row i for keys 4g .. 4g + 3 of each 16.  In this order the exponentials are the B operand of O^T = V^T P^T (a contraction index may
+// be permuted if both operands agree): its A operand needs 8 keys of one d in a lane, and a lane that loads D / 16 adjacent d's of those 8 keys has them after
+// one exchange of 16-bit halves.  No LDS, no barrier inside the loop.  Bound: HBM.
+template <int D, bool F8, int RT>
+struct Few {
+  static constexpr int TILE = 16 * RT, DL = D / 16;              // rows of a tile; d's of a lane in V
+  static constexpr int KL = F8 ? D / 64 : D / 32, VW = (F8 ? DL : 2 * DL) / 4;   // 16-byte loads of a K row's quarter, words of V a key
+  static constexpr int LDS = 4 * TILE * (D + 2) * 4;
+  struct Frag {
+    u32x4 k[2][KL];
+    unsigned v[8][VW];
+    unsigned ks[2], vs[2];
+    bool there[2];     // the two groups of 16 keys lie on pages
+  };
+};
+
+template <int D, bool F8, int RT, bool OUT_F32>
+__device__ __forceinline__ void few_rows(const PagedParams& p, const Item& w, char* lds) {
+  typedef Few<D, F8, RT> F;
+  typedef typename F::Frag Frag;
+  constexpr int TILE = F::TILE, DL = F::DL, KL = F::KL, VW = F::VW, QS = D / 32;
+  const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), i16 = lane & 15, g = lane >> 4;
+  const int row0 = w.tile * TILE, rows = min(TILE, w.q.n * p.gq - row0);
+  const int limit_lo = row_limit(p, w.q, row0), limit_hi = min(w.k1, row_limit(p, w.q, row0 + rows - 1));
+
+  bf16x8 qf[RT][QS];
+  int limit[RT];
+#pragma unroll
+  for (int rt = 0; rt < RT; rt++) {
+    const int r = row0 + min(rt * 16 + i16, rows - 1), t = divide(p.by_gq, r);
+    limit[rt] = min(w.k1, visible(w.q, t, p.causal));
+    const __bf16* const src = p.q + (int64_t)(w.hk * p.gq + r - t * p.gq) * p.q_sh + (int64_t)(w.q.start + t) * p.q_ss;
+#pragma unroll
+    for (int s = 0; s < QS; s++)   // d's in the order of the K loads
+      qf[rt][s] = *reinterpret_cast<const bf16x8*>(src + (F8 ? (s >> 1) * 64 + g * 16 + (s & 1) * 8 : s * 32 + g * 8));
+  }
+  const char* const kb = p.k_pages + (int64_t)w.hk * p.head_b;
+  const char* const vb = p.v_pages + (int64_t)w.hk * p.head_b;
+  const unsigned char* const ksb = p.k_scales + (int64_t)w.hk * p.scale_sh;
+  const unsigned char* const vsb = p.v_scales + (int64_t)w.hk * p.scale_sh;
+  const int k_lane = i16 * p.slot_b + g * 16, v_lane = g * 4 * p.slot_b + i16 * VW * 4;
+
+  // Pages of the wave's groups of 16 keys, 32 stretches ahead: lane 2 j + h has those of group h of stretch j.
+  const int steps = (w.k1 - w.k0 + 127) >> 7;
+  Slot at = {-1, 0};
+  auto find_pages = [&](int step) __attribute__((always_inline)) {
+    const int key = w.k0 + (step + (lane >> 1)) * 128 + wave * 32 + (lane & 1) * 16;
+    at = Slot{-1, 0};
+    if (key < w.k1) at = slot_of(p.seq, w.b, key);
+  };
+  auto load = [&](Frag& f, int step) __attribute__((always_inline)) {
+    if ((step & 31) == 0) find_pages(step);
+#pragma unroll
+    for (int h = 0; h < 2; h++) {
+      const int page = __builtin_amdgcn_readlane(at.page, ((step & 31) << 1) + h), slot = __builtin_amdgcn_readlane(at.slot, ((step & 31) << 1) + h);
+      f.there[h] = page >= 0;
+      if (page >= 0) {
+        const int64_t off = (int64_t)page * p.page_b + (int64_t)slot * p.slot_b;
+        const char* const kp = kb + off;
+        const char* const vp = vb + off;
+#pragma unroll
+        for (int l = 0; l < KL; l++) f.k[h][l] = *reinterpret_cast<const u32x4*>(kp + k_lane + l * 64);
+#pragma unroll
+        for (int e = 0; e < 4; e++) {
+          const char* const src = vp + v_lane + e * p.slot_b;
+          if constexpr (VW == 4) {
+            const u32x4 x = *reinterpret_cast<const u32x4*>(src);
+#pragma unroll
+            for (int i = 0; i < 4; i++) f.v[4 * h + e][i] = x[i];
+          } else if constexpr (VW == 2) {
+            const u32x2 x = *reinterpret_cast<const u32x2*>(src);
+            f.v[4 * h + e][0] = x[0];
+            f.v[4 * h + e][1] = x[1];
+          } else {
+            f.v[4 * h + e][0] = *reinterpret_cast<const unsigned*>(src);
+          }
+        }
+        if constexpr (F8) {
+          const int64_t s_off = (int64_t)page * p.scale_sp + slot;
+          f.ks[h] = ksb[s_off + i16];
+          f.vs[h] = *reinterpret_cast<const unsigned*>(vsb + s_off + 4 * g);
+        }
+      } else {
+#pragma unroll
+        for (int l = 0; l < KL; l++) f.k[h][l] = u32x4{0, 0, 0, 0};
+#pragma unroll
+        for (int e = 0; e < 4; e++)
+#pragma unroll
+          for (int i = 0; i < VW; i++) f.v[4 * h + e][i] = 0;
+        if constexpr (F8) {
+          f.ks[h] = 127;
+          f.vs[h] = 0x7f7f7f7f;
+        }
+      }
+    }
+  };
+
+  f32x4 acc[RT][DL];
+  float m_ref[RT], mc[RT], l_run[RT], cap[RT];
+  const float c2 = p.scale * kLog2e;
+#pragma unroll
+  for (int rt = 0; rt < RT; rt++) {
+    m_ref[rt] = -INFINITY;
+    mc[rt] = l_run[rt] = 0.f;
+    cap[rt] = -1.f;
+#pragma unroll
+    for (int j = 0; j < DL; j++) acc[rt][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+  }
+
+  unsigned taken_out = 0;
+  auto compute = [&](Frag& f, int step) __attribute__((always_inline)) {
+    const int key0 = w.k0 + step * 128 + wave * 32;
+    const bool edge = key0 + 32 > limit_lo || key0 + 32 > limit_hi || !f.there[0] || !f.there[1];
+    // scores
+    f32x4 s[RT][2];
+#pragma unroll
+    for (int rt = 0; rt < RT; rt++) s[rt][0] = s[rt][1] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int h = 0; h < 2; h++)
+#pragma unroll
+      for (int ks = 0; ks < QS; ks++) {
+        bf16x8 a;
+        if constexpr (F8) {
+          const u32x4 x = f.k[h][ks >> 1];
+          const unsigned lo = x[(ks & 1) * 2], hi = x[(ks & 1) * 2 + 1];
+          a = __builtin_bit_cast(bf16x8, u32x4{f8_pair(lo, false, f.ks[h]), f8_pair(lo, true, f.ks[h]), f8_pair(hi, false, f.ks[h]), f8_pair(hi, true, f.ks[h])});
+        } else {
+          a = __builtin_bit_cast(bf16x8, f.k[h][ks]);
+        }
+#pragma unroll
+        for (int rt = 0; rt < RT; rt++) s[rt][h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, qf[rt][ks], s[rt][h], 0, 0, 0);
+      }
+    // V^T: dl[2 n] and dl[2 n + 1] of key e lie in one word; pairs of keys of one d are what the product takes
+    unsigned vt[DL][4];
+#pragma unroll
+    for (int m = 0; m < 4; m++)
+#pragma unroll
+      for (int n = 0; n < DL / 2; n++) {
+        unsigned a, b;
+        if constexpr (F8) {
+          const int h = m >> 1;
+          a = f8_pair(f.v[2 * m][n >> 1], n & 1, f.vs[h] >> (16 * (m & 1)) & 255);
+          b = f8_pair(f.v[2 * m + 1][n >> 1], n & 1, f.vs[h] >> (16 * (m & 1) + 8) & 255);
+        } else {
+          a = f.v[2 * m][n];
+          b = f.v[2 * m + 1][n];
+        }
+        vt[2 * n][m] = __builtin_amdgcn_perm(b, a, 0x05040100);
+        vt[2 * n + 1][m] = __builtin_amdgcn_perm(b, a, 0x07060302);
+      }
+    if (edge) {
+#pragma unroll
+      for (int h = 0; h < 2; h++)
+#pragma unroll
+        for (int r = 0; r < 4; r++) {
+          const int key = key0 + 16 * h + 4 * g + r;
+#pragma unroll
+          for (int rt = 0; rt < RT; rt++)
+            if (key >= limit[rt] || !f.there[h]) s[rt][h][r] = -INFINITY;
+          // What no row sees takes part in the second product with weight 0: not a value that times 0 is NaN.
+          const unsigned keep = key < limit_hi ? 0xffffffffu : 0u, mask = r & 1 ? keep | 0xffffu : keep | 0xffff0000u;
+#pragma unroll
+          for (int j = 0; j < DL; j++) vt[j][2 * h + (r >> 1)] &= mask;
+        }
+      // A key that some rows see and others do not, with an infinity or NaN in V: taken out of the product, and added below to the rows that see it.
+      if (limit_lo < min(key0 + 32, limit_hi)) {
+        // (in integers: as conditions, 64 masks of lanes spill the scalar registers)
+#pragma unroll
+        for (int j = 0; j < DL; j++)
+#pragma unroll
+          for (int m = 0; m < 4; m++) {
+            const unsigned nf = ((vt[j][m] & 0x7f807f80u) + 0x00800080u) & 0x80008000u;   // a half's top bit: its exponent is all ones
+            taken_out |= nf;
+            vt[j][m] &= ~(nf | (nf - (nf >> 15)));
+          }
+      }
+    }
+    // Weights relative to a reference that is not the running maximum: any gives the same result, and one that the
+    // first scores set is replaced only where a sum of weights passes 2^80 (fp32 and bf16 hold them as well as small ones).
+#pragma unroll
+    for (int rt = 0; rt < RT; rt++) {
+      float e[8], sum = 0.f;
+#pragma unroll
+      for (int i = 0; i < 8; i++) {
+        e[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[rt][i >> 2][i & 3], c2, -mc[rt]));
+        sum += e[i];
+      }
+      if (__any(!(sum <= cap[rt]))) {
+        float top = s[rt][0][0];
+#pragma unroll
+        for (int i = 1; i < 8; i++) top = fmaxf(top, s[rt][i >> 2][i & 3]);
+        top = fmaxf(top, __shfl_xor(top, 16));
+        top = fmaxf(top, __shfl_xor(top, 32));
+        const float m_new = fmaxf(m_ref[rt], top);
+        const float a = m_ref[rt] == m_new ? 1.f : __builtin_amdgcn_exp2f((m_ref[rt] - m_new) * c2);
+        l_run[rt] *= a;
+        // acc holds this lane's row in every element, so the factor is the lane's own
+#pragma unroll
+        for (int j = 0; j < DL; j++)
+#pragma unroll
+          for (int r = 0; r < 4; r++) acc[rt][j][r] *= a;
+        m_ref[rt] = m_new;
+        mc[rt] = m_new == -INFINITY ? 0.f : m_new * c2;
+        cap[rt] = m_new == -INFINITY ? -1.f : 0x1p80f;
+        sum = 0.f;
+#pragma unroll
+        for (int i = 0; i < 8; i++) {
+          e[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[rt][i >> 2][i & 3], c2, -mc[rt]));
+          sum += e[i];
+        }
+      }
+      l_run[rt] += sum;
+      bf16x8 pf;   // (the sums take the weights as they are: rounded ones would put 2^-9 of error into lse)
+#pragma unroll
+      for (int i = 0; i < 8; i++) pf[i] = (__bf16)e[i];
+#pragma unroll
+      for (int j = 0; j < DL; j++)
+        acc[rt][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, u32x4{vt[j][0], vt[j][1], vt[j][2], vt[j][3]}), pf, acc[rt][j], 0, 0, 0);
+    }
+  };
+
+  {
+    Frag fa, fb;
+    if (steps > 0) load(fa, 0);
+    for (int step = 0; step < steps; step += 2) {
+      if (step + 1 < steps) load(fb, step + 1);
+      compute(fa, step);
+      if (step + 1 >= steps) break;
+      if (step + 2 < steps) load(fa, step + 2);
+      compute(fb, step + 1);
+    }
+  }
+  if (__any(taken_out != 0)) {   // (the rows they reach are infinite or NaN whatever else adds up)
+#pragma unroll 1
+    for (int key = w.k0 + wave * 32; key < limit_hi; key += (key & 31) == 31 ? 97 : 1) {
+      if (limit_lo >= min((key | 31) + 1, limit_hi)) continue;
+      const Slot one = slot_of(p.seq, w.b, key);
+      if (one.page < 0) continue;
+      const char* const vp = vb + (int64_t)one.page * p.page_b + (int64_t)one.slot * p.slot_b + g * 16 * VW;
+      const unsigned scale = F8 ? vsb[(int64_t)one.page * p.scale_sp + one.slot] : 0;
+#pragma unroll
+      for (int i = 0; i < 4 * VW; i++) {   // the lane's 4 * DL values, d = 4 g DL + ...
+        const unsigned x = reinterpret_cast<const unsigned*>(vp)[i];
+#pragma unroll
+        for (int n = 0; n < (F8 ? 2 : 1); n++) {
+          const unsigned pair = F8 ? f8_pair(x, n, scale) : x;
+          const int e = F8 ? 4 * i + 2 * n : 2 * i;
+#pragma unroll
+          for (int rt = 0; rt < RT; rt++) {
+            if (key < limit[rt] && (pair & 0x7f80u) == 0x7f80u) acc[rt][e % DL][e / DL] += __builtin_bit_cast(float, pair << 16);
+            if (key < limit[rt] && (pair & 0x7f800000u) == 0x7f800000u) acc[rt][e % DL + 1][e / DL] += __builtin_bit_cast(float, pair & 0xffff0000u);
+          }
+        }
+      }
+    }
+  }
+
+  // ---- the waves' results, added up in LDS: [wave][row][D] (16-byte pieces exchanged among each other by the row), then reference and sum of each
+  float* const ml = reinterpret_cast<float*>(lds + 4 * TILE * D * 4);
+#pragma unroll
+  for (int rt = 0; rt < RT; rt++) {
+    float l = l_run[rt];
+    l += __shfl_xor(l, 16);
+    l += __shfl_xor(l, 32);
+    const int r = rt * 16 + i16;
+    if (g == 0) {
+      ml[(wave * TILE + r) * 2] = m_ref[rt];
+      ml[(wave * TILE + r) * 2 + 1] = l;
+    }
+    char* const at_row = lds + (wave * TILE + r) * D * 4;
+#pragma unroll
+    for (int q = 0; q < 4; q++)
+#pragma unroll
+      for (int j = 0; j < DL; j += 4) {
+        const int c = ((4 * g + q) * DL + j) / 4;
+        *reinterpret_cast<f32x4*>(at_row + ((c ^ (r & 15)) << 4)) = f32x4{acc[rt][j][q], acc[rt][j + 1][q], acc[rt][j + 2][q], acc[rt][j + 3][q]};
+      }
+  }
+  __syncthreads();
+  constexpr int PIECES = D / 4;
+  for (int i = tid; i < rows * PIECES; i += 256) {
+    const int r = i / PIECES, c = i % PIECES;
+    float m[4], l[4], top = -INFINITY, total = 0.f;
+#pragma unroll
+    for (int v = 0; v < 4; v++) {
+      m[v] = ml[(v * TILE + r) * 2];
+      l[v] = ml[(v * TILE + r) * 2 + 1];
+      top = fmaxf(top, m[v]);
+    }
+    f32x4 o = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int v = 0; v < 4; v++) {
+      const float a = m[v] == -INFINITY ? 0.f : m[v] == top ? 1.f : __builtin_amdgcn_exp2f((m[v] - top) * c2);
+      const f32x4 x = *reinterpret_cast<const f32x4*>(lds + (v * TILE + r) * D * 4 + ((c ^ (r & 15)) << 4));
+      total += a * l[v];
+#pragma unroll
+      for (int k = 0; k < 4; k++) o[k] += a * x[k];
+    }
+    const float inv = total == 0.f ? 0.f : 1.f / total;
+    const float lse = total > 0.f ? top * p.scale + logf(total) : -INFINITY;
+#pragma unroll
+    for (int k = 0; k < 4; k++) o[k] *= inv;
+    if (w.n_parts > 1) {
+      const int64_t at_slot = (int64_t)w.slot * TILE + r;
+      *reinterpret_cast<f32x4*>(p.part_out + at_slot * D + 4 * c) = o;
+      if (c == 0) p.part_lse[at_slot] = total != total ? __builtin_nanf("") : lse;
+    } else {
+      const int t = divide(p.by_gq, row0 + r), head = w.hk * p.gq + row0 + r - t * p.gq;
+      const int64_t at_out = (int64_t)head * p.o_sh + (int64_t)(w.q.start + t) * p.o_ss + 4 * c;
+      if constexpr (OUT_F32) {
+        *reinterpret_cast<f32x4*>(reinterpret_cast<float*>(p.out) + at_out) = o;
+      } else {
+        bf16x4 ob;
+#pragma unroll
+        for (int k = 0; k < 4; k++) ob[k] = (__bf16)o[k];
+        *reinterpret_cast<bf16x4*>(reinterpret_cast<__bf16*>(p.out) + at_out) = ob;
+      }
+      if (c == 0) p.lse[(int64_t)head * p.l_sh + (int64_t)(w.q.start + t) * p.l_ss] = lse;
+    }
+  }
+}
+
+template <int D, bool F8, int RT, bool OUT_F32>
+__global__ void __launch_bounds__(256) paged_few_kernel(const PagedParams p) {
+  extern __shared__ __attribute__((aligned(1024))) char lds[];
+  Item w;
+  if (!find_item(p, 16 * RT, (int)blockIdx.x, w)) return;
+  few_rows<D, F8, RT, OUT_F32>(p, w, lds);
+}
+
+// ---- Row tiles whose keys were cut: out = sum of exp(lse_i - lse) out_i over their live parts.  One workgroup a tile and 1024 / D rows of it.
+template <int D, int TILE, bool OUT_F32>
+__global__ void __launch_bounds__(256) paged_fold_kernel(const PagedParams p) {
+  const int part = plan_part(p, TILE);
+  auto cut_tiles = [&](int b) {
+    const Sequence q = sequence(p.seq, b);
+    return parts_of(q.len, part) > 1 ? tiles_of(q.n * p.gq, TILE) * p.Hkv : 0;
+  };
+  int b, before, base = 0;
+  if (!locate(p.seq.n, (int)blockIdx.x, cut_tiles, b, before)) return;
+  b = uniform(b);
+  for (int b0 = 0; b0 < b; b0 += 64) {
+    const int s = b0 + (int)(threadIdx.x & 63);
+    int n = 0;
+    if (s < b) n = cut_tiles(s) * parts_of(sequence(p.seq, s).len, part);
+    base += __builtin_amdgcn_readlane(wave_scan(n), 63);
+  }
+  const Sequence q = sequence(p.seq, b);
+  const int parts = parts_of(q.len, part), tiles = tiles_of(q.n * p.gq, TILE), i = (int)blockIdx.x - before;
+  const int hk = i / tiles, tile = i - hk * tiles, row0 = tile * TILE, rows = min(TILE, q.n * p.gq - row0);
+  const int n_live = parts_of(row_limit(p, q, row0 + rows - 1), part);
+  const int r = (int)blockIdx.y * (1024 / D) + (int)threadIdx.x / (D / 4), c = (int)threadIdx.x % (D / 4);
+  if (n_live == 1 || r >= rows) return;   // one part: written already
+  if (base < 0 || base + (i + 1) * parts > 2 * p.target) return;   // (only where sequences overlap)
+  const int64_t slot_row = ((int64_t)base + (int64_t)i * parts) * TILE + r;
+  const float* const ls = p.part_lse + slot_row;
+  float top = -INFINITY, total = 0.f;
+  bool nan = false;
+  for (int k = 0; k < n_live; k++) {
+    const float x = ls[(int64_t)k * TILE];
+    nan |= x != x;
+    top = fmaxf(top, x);
+  }
+  f32x4 o = {0.f, 0.f, 0.f, 0.f};
+  for (int k = 0; k < n_live; k++) {
+    const float x = ls[(int64_t)k * TILE], a = x == -INFINITY ? 0.f : expf(x - top);
+    const f32x4 y = *reinterpret_cast<const f32x4*>(p.part_out + (slot_row + (int64_t)k * TILE) * D + 4 * c);
+    total += a;
+    if (x != -INFINITY) {
+#pragma unroll
+      for (int e = 0; e < 4; e++) o[e] += a * y[e];
+    }
+  }
+  const float inv = total == 0.f ? 0.f : 1.f / total;
+#pragma unroll
+  for (int e = 0; e < 4; e++) o[e] *= inv;
+  const int t = divide(p.by_gq, row0 + r), head = hk * p.gq + row0 + r - t * p.gq;
+  const int64_t at_out = (int64_t)head * p.o_sh + (int64_t)(q.start + t) * p.o_ss + 4 * c;
+  if constexpr (OUT_F32) {
+    *reinterpret_cast<f32x4*>(reinterpret_cast<float*>(p.out) + at_out) = o;
+  } else {
+    bf16x4 ob;
+#pragma unroll
+    for (int e = 0; e < 4; e++) ob[e] = (__bf16)o[e];
+    *reinterpret_cast<bf16x4*>(reinterpret_cast<__bf16*>(p.out) + at_out) = ob;
+  }
+  if (c == 0) p.lse[(int64_t)head * p.l_sh + (int64_t)(q.start + t) * p.l_ss] = nan || !(total > 0.f) ? -INFINITY : top + logf(total);
+}
+
+}  // namespace
+}  // namespace tr

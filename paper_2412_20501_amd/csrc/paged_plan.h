@@ -1,0 +1,64 @@
+// What the kernels on a paged cache read from the arrays of a tr_sequences, and how a launch's keys are shared out.  Plain C++: constexpr
+// functions are both the host's and the device's, so the bounds that keep every access inside the caller's arrays are tested on the host.
+#pragma once
+#include <stdint.h>
+
+#include "divisor.h"
+
+namespace tr {
+
+struct Sequences {
+  const int* table;      // [n][max_pages], rows table_stride apart
+  const int* kv_len;
+  const int* q_start;
+  const int* q_pos;      // or null
+  int64_t table_stride;
+  int n, max_pages;
+  int tokens;            // of the call's tensors (their S)
+  int n_pages, page_size;
+  Divisor by_page;       // of page_size
+};
+
+constexpr int kPosLimit = 1 << 30;
+constexpr int clamped(int x, int lo, int hi) { return x < lo ? lo : x > hi ? hi : x; }
+
+// A sequence, whatever its entries hold: 0 <= start, start + n <= tokens; 0 <= len <= max_pages * page_size; -2^30 <= pos < 2^30.
+struct Sequence { int start, n, len, pos; };
+constexpr Sequence sequence(const Sequences& s, int b) {
+  Sequence r = {0, 0, 0, 0};
+  r.start = clamped(s.q_start[b], 0, s.tokens);
+  r.n = clamped(s.q_start[b + 1], r.start, s.tokens) - r.start;
+  r.len = clamped(s.kv_len[b], 0, s.max_pages * s.page_size);   // (at most 2^30, see the entry points)
+  r.pos = clamped(s.q_pos ? s.q_pos[b] : r.len - r.n, -kPosLimit, kPosLimit - 1);   // (pos + tokens fits)
+  return r;
+}
+
+// Keys 0 .. visible(...) - 1 are those that token t of a sequence sees.
+constexpr int visible(const Sequence& q, int t, bool causal) { return causal ? clamped(q.pos + t + 1, 0, q.len) : q.len; }
+
+// Page (-1: none) and slot of key c, 0 <= c < max_pages * page_size.
+struct Slot { int page, slot; };
+constexpr Slot slot_of(const Sequences& s, int b, int c) {
+  const int i = divide(s.by_page, c), page = s.table[(int64_t)b * s.table_stride + i];
+  return Slot{page >= 0 && page < s.n_pages ? page : -1, c - i * s.page_size};
+}
+
+// Keys of a part.  work: sum over (sequence, K/V head) of row tiles x keys; target: workgroups that are to share it; 0: keys are not
+// shared out.  A multiple of kPartStep, so that parts begin on whole steps of a workgroup.
+// Row tiles whose keys are cut have ceil(keys / part) parts, fewer than 2 keys / part: all of them together fewer than 2 * target.
+constexpr int kPartStep = 128;
+constexpr int part_keys(int64_t work, int target, int least) {
+  if (target <= 0) return kPosLimit;   // (as many keys as a sequence has at most)
+  const int64_t keys = (work + target - 1) / target, up = (keys + kPartStep - 1) / kPartStep * kPartStep;
+  return up < least ? least : up > kPosLimit ? kPosLimit : (int)up;
+}
+constexpr int parts_of(int keys, int part) { return keys <= part ? 1 : (keys - 1) / part + 1; }
+constexpr int tiles_of(int rows, int tile) { return (rows + tile - 1) / tile; }
+
+// Row tiles that the sequences of `tokens` tokens have at most, `group` rows a token: a sequence with tokens has at most one that is not full.
+constexpr int64_t most_tiles(int64_t tokens, int64_t n_seqs, int64_t group, int tile) {
+  const int64_t some = tokens < n_seqs ? tokens : n_seqs;
+  return (tokens * group) / tile + some;
+}
+
+}  // namespace tr

@@ -1,0 +1,162 @@
+"""tr_paged_attn against a 64-bit implementation, within bounds that follow from its roundings (paged_util)."""
+import pytest
+import torch
+
+from paged_util import Cache, attention, check
+
+pytestmark = pytest.mark.gpu
+
+
+def _run(lib, c, Hq, causal=True, pos=None, out_dtype=torch.bfloat16, workspace=True, seed=1, scale=None, behind=0, q=None):
+    """(results of the call, found by the oracle); tokens `behind` the last sequence stay as they were."""
+    g = torch.Generator().manual_seed(seed)
+    if q is None:
+        q = torch.randn(1, c.tokens + behind, Hq, c.D, generator=g).bfloat16().cuda().transpose(1, 2)
+    out = torch.full((1, c.tokens + behind, Hq, c.D), 3.5, dtype=out_dtype, device="cuda").transpose(1, 2)
+    lse = torch.full((1, Hq, c.tokens + behind), 4.5, device="cuda")
+    scale = c.D ** -0.5 if scale is None else scale
+    ws = torch.full((lib.tr_paged_attn_workspace_bytes(q, c.pages["k"], c.table),), 255, dtype=torch.uint8, device="cuda") if workspace else None
+    p = None if pos is None else torch.tensor(pos, dtype=torch.int32, device="cuda")
+    lib.tr_paged_attn(q, *c.args(), c.q_start, causal, scale, out, lse, *c.scale_args(), q_pos=p, workspace=ws)
+    if behind:
+        assert (out[:, :, c.tokens:] == 3.5).all() and (lse[:, :, c.tokens:] == 4.5).all()
+    return q, out, lse, attention(c, q, scale, causal, pos)
+
+
+SHAPES = [
+    # keys, new tokens, Hkv, query heads a K/V head, page
+    ([1], [1], 1, 1, 16),
+    ([5], [1], 2, 4, 16),
+    ([31, 32, 33], [1, 1, 1], 2, 4, 16),
+    ([127, 128, 129, 130], [1, 2, 3, 4], 1, 5, 32),
+    ([300, 0, 17, 1], [1, 0, 1, 1], 2, 7, 48),
+    ([1000, 3], [3, 3], 2, 8, 64),
+    ([4500], [1], 1, 8, 16),
+    ([2000, 10, 1999], [1, 1, 1], 2, 16, 128),
+    ([5000, 33], [5, 33], 1, 4, 32),
+    ([90], [90], 2, 2, 16),
+    ([700, 650], [130, 257], 2, 3, 48),
+    ([1500, 40, 900], [513, 1, 64], 1, 4, 16),
+    ([600], [600], 2, 1, 32),
+]
+
+
+@pytest.mark.parametrize("f8", [False, True])
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("shape", SHAPES)
+def test_lengths(lib, shape, D, f8):
+    kv, q, Hkv, gq, page = shape
+    c = Cache(kv, q, Hkv, D, page, f8, "head" if len(kv) % 2 else "token", seed=D + len(kv))
+    for workspace in (True, False):
+        _, out, lse, found = _run(lib, c, Hkv * gq, workspace=workspace, behind=2)
+        print(check(found, out, lse))
+
+
+@pytest.mark.parametrize("f8", [False, True])
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("causal", [False, True])
+def test_fp32_results_and_no_mask(lib, D, causal, f8):
+    c = Cache([200, 4000, 77], [9, 2, 77], 2, D, 32, f8, "head", seed=5)
+    _, out, lse, found = _run(lib, c, 8, causal, out_dtype=torch.float32)
+    check(found, out, lse)
+
+
+@pytest.mark.parametrize("f8", [False, True])
+@pytest.mark.parametrize("n", [3, 70])
+def test_positions(lib, n, f8):
+    """New tokens in front of all keys (rows that see none), between them, and behind them."""
+    c = Cache([150, 2500, 64, 40], [n] * 4, 2, 128, 16, f8, "head", seed=6)
+    pos = [-2, 1000 - n, 64, -1000]
+    _, out, lse, found = _run(lib, c, 8, True, pos)
+    check(found, out, lse)
+    assert (out[:, :, c.starts[3]:] == 0).all() and torch.isneginf(lse[:, :, c.starts[3]:]).all()
+    assert (out[:, :, 0] == 0).all() and torch.isneginf(lse[:, :, 0]).all()
+
+
+@pytest.mark.parametrize("f8", [False, True])
+@pytest.mark.parametrize("n", [1, 70])
+def test_entries_that_are_no_pages(lib, n, f8):
+    c = Cache([500, 3000], [n, n], 2, 128, 16, f8, "token", seed=7)
+    c.table[0, 3], c.table[0, 30], c.table[1, 0], c.table[1, 100] = -1, c.n_pages, 2 ** 31 - 1, -2 ** 31
+    _, out, lse, found = _run(lib, c, 8)
+    check(found, out, lse)
+    c.table.fill_(-1)
+    _, out, lse, found = _run(lib, c, 8)
+    assert (out == 0).all() and torch.isneginf(lse).all()
+
+
+@pytest.mark.parametrize("f8", [False, True])
+@pytest.mark.parametrize("bad", [float("nan"), float("inf"), float("-inf")])
+@pytest.mark.parametrize("n", [4, 70])
+def test_bad_values_reach_the_rows_that_see_them(lib, n, bad, f8):
+    """An infinity or NaN in V of a new token: later rows have it, earlier ones nothing of it.  (e4m3 has no infinities: NaN.)"""
+    c = Cache([333, 2000], [n, n], 2, 128, 16, f8, "head", seed=8)
+    for b in range(2):
+        key = c.kv[b] - n // 2
+        page, slot = int(c.table[b, key // 16]), key % 16
+        if f8:
+            c.pages["v"].view(torch.uint8)[page, 1, slot, 5] = 127
+        else:
+            c.pages["v"][page, 1, slot, 5] = bad
+    _, out, lse, found = _run(lib, c, 8)
+    check(found, out, lse)
+    assert out[0, 4:, c.starts[1] - 1, 5].isfinite().sum() == 0 and out[0, :4].isfinite().all()
+
+
+def test_bad_scores(lib):
+    """A NaN in K of a key that all rows see: out = NaN, lse = -inf, as of a block step; other heads have nothing of it."""
+    for n, kv in ((1, 200), (1, 5000), (70, 500)):
+        c = Cache([kv], [n], 2, 128, 16, False, "head", seed=9)
+        c.pages["k"][int(c.table[0, 2]), 1, 3, 5] = float("nan")
+        _, out, lse, _ = _run(lib, c, 8)
+        assert out[:, 4:].isnan().all() and torch.isneginf(lse[:, 4:]).all()
+        assert out[:, :4].isfinite().all() and lse[:, :4].isfinite().all()
+
+
+@pytest.mark.parametrize("n", [1, 70])
+def test_scores_far_apart(lib, n):
+    """Scores that grow by hundreds along the keys, so that references are replaced again and again, and the other way round."""
+    for sign in (1.0, -1.0):
+        c = Cache([900], [n], 1, 64, 16, False, "head", seed=10, std=0.1)
+        for i in range(900):
+            c.pages["k"][int(c.table[0, i // 16]), 0, i % 16, 0] = sign * (i // 8)
+        q = torch.zeros(1, 4, n, 64, dtype=torch.bfloat16, device="cuda")
+        q[..., 0] = 8.0
+        _, out, lse, found = _run(lib, c, 4, scale=1.0, q=q)
+        check(found, out, lse)
+
+
+def test_sequences_that_share_pages(lib):
+    """Two sequences with the same first pages, and one page twice in a table."""
+    c = Cache([160, 160, 64], [1, 20, 5], 2, 128, 16, False, "head", seed=12)
+    c.table[1, :6] = c.table[0, :6]
+    c.table[2, 1] = c.table[2, 0]
+    _, out, lse, found = _run(lib, c, 8)
+    check(found, out, lse)
+
+
+def test_many_sequences(lib):
+    """More sequences than a wave has lanes, most without new tokens or keys."""
+    kv = [(37 * i) % 700 if i % 3 else 0 for i in range(200)]
+    q = [[1, 0, 2, 30][i % 4] if i % 5 else 0 for i in range(200)]
+    kv = [max(a, b) for a, b in zip(kv, q)]
+    kv[150] = 6000
+    c = Cache(kv, q, 2, 64, 32, True, "head", seed=13)
+    _, out, lse, found = _run(lib, c, 8, behind=3)
+    check(found, out, lse)
+
+
+def test_arrays_with_wrong_entries(lib):
+    """Lengths and starts out of range are taken as the nearest that is: nothing else is touched."""
+    c = Cache([48, 48, 48], [2, 2, 2], 1, 128, 16, False, "head", seed=14, poison=False)
+    q = torch.randn(1, 4, 6, 128, device="cuda").bfloat16()
+    out, lse = torch.full((1, 4, 6, 128), 3.5, device="cuda"), torch.full((1, 4, 6), 4.5, device="cuda")
+    lens = torch.tensor([-5, 1 << 30, 48], dtype=torch.int32, device="cuda")
+    starts = torch.tensor([-3, 2, 4, 1 << 30], dtype=torch.int32, device="cuda")
+    lib.tr_paged_attn(q, *c.args()[:3], lens, starts, True, 0.1, out, lse)
+    assert (out[:, :, :2] == 0).all() and torch.isneginf(lse[:, :, :2]).all() and out.isfinite().all()
+    lib.tr_cache_write(q[:, :1], q[:, 1:2], *c.args()[:3], lens, starts)
+    backwards = torch.tensor([6, 4, 2, 0], dtype=torch.int32, device="cuda")
+    out.fill_(3.5)
+    lib.tr_paged_attn(q, *c.args(), backwards, True, 0.1, out, lse)
+    assert (out == 3.5).all()
