@@ -52,8 +52,9 @@ struct PagedParams {
 };
 
 // How a call is launched: the form of its row tiles and the workgroups that share its keys.
+constexpr TileRows kMixed = {16, 256};   // few rows and many in one launch
 struct PagedLaunch {
-  int rows;        // of a tile
+  TileRows tile;   // few == many: one form; else kMixed
   int target;      // as above, where a workspace is there
   int64_t tiles;   // of all sequences and K/V heads, at most
 };

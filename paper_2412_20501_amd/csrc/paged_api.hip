@@ -242,7 +242,7 @@ size_t tr_paged_attn_workspace_bytes(const tr_tensor* q, const tr_tensor* k_page
   if (k_pages->S < 16 || n_seqs < 0 || max_pages < 0 || max_pages > kMaxKeys / k_pages->S || n_seqs > (1 << 24) || q->S * q->H >= ((int64_t)1 << 31)) return 0;
   if (q->S == 0 || q->H == 0 || n_seqs == 0) return 0;
   const tr::PagedLaunch l = tr::paged_launch(q->S, n_seqs, max_pages * k_pages->S, (int)k_pages->H, (int)(q->H / k_pages->H), (int)q->D);
-  return (size_t)l.target * 2 * l.rows * (size_t)(q->D + 1) * 4;
+  return (size_t)l.target * 2 * l.tile.many * (size_t)(q->D + 1) * 4;
 }
 
 tr_status tr_paged_attn(const tr_tensor* q_, const tr_tensor* k_pages_, const tr_tensor* v_pages_, const tr_tensor* k_scales_,
@@ -315,7 +315,7 @@ tr_status tr_paged_attn(const tr_tensor* q_, const tr_tensor* k_pages_, const tr
   p.target = l.target;
   p.least_part = 256;
   p.part_out = (float*)workspace;
-  p.part_lse = p.part_out ? p.part_out + (int64_t)2 * l.target * l.rows * D : nullptr;
+  p.part_lse = p.part_out ? p.part_out + (int64_t)2 * l.target * l.tile.many * D : nullptr;
   const hipError_t e = tr::launch_paged_attn(p, l, D, k_scales != nullptr, (hipStream_t)hip_stream);
   if (e != hipSuccess) return fail(TR_ERR_HIP, "paged attention launch failed: %s", hipGetErrorString(e));
   return TR_OK;

@@ -1,0 +1,6 @@
+// Attention on a paged cache at head dim 128, pages of e4m3.
+#include "paged_launch.h"
+
+namespace tr {
+template hipError_t launch_paged_form<128, true>(const PagedParams&, const PagedLaunch&, hipStream_t);
+}  // namespace tr

@@ -53,19 +53,23 @@ __device__ __forceinline__ bool locate(int n, int at, Count count, int& b, int& 
 }
 
 // Keys of a part of this call.
-__device__ __forceinline__ int plan_part(const PagedParams& p, int tile) {
-  int64_t work = 0;
+__device__ __forceinline__ int plan_part(const PagedParams& p, TileRows tile) {
+  int64_t work = 0, tiles = 0;
   if (p.target > 0) {
     for (int b = threadIdx.x & 63; b < p.seq.n; b += 64) {
       const Sequence q = sequence(p.seq, b);
-      work += (int64_t)tiles_of(q.n * p.gq, tile) * q.len;
+      const int n = tiles_of(q.n * p.gq, tile);
+      work += (int64_t)n * q.len;
+      tiles += n;
     }
     work = wave_sum(work) * p.Hkv;
+    tiles = wave_sum(tiles) * p.Hkv;
   }
-  return uniform(part_keys(work, p.target, p.least_part));
+  return uniform(part_keys(work, tiles, p.target, p.least_part));
 }
 
 struct Item {
+  int rows, rows_of_tile;           // of the sequence and a K/V head; of its tiles, but the last
   int b, hk, tile, part, n_parts;   // n_parts: live ones, those whose keys some row of the tile sees, and the first one
   int k0, k1;                       // its keys
   int slot;                         // of the scratch, if n_parts > 1
@@ -77,7 +81,7 @@ __device__ __forceinline__ int row_limit(const PagedParams& p, const Sequence& q
 
 // The item of workgroup `id` of `ids`; false: none.  The items of a K/V head and part lie next to each other, and each XCD has a contiguous
 // eighth of all, so that row tiles which read the same keys mostly share an L2.
-__device__ __forceinline__ bool find_item(const PagedParams& p, int tile, int id, Item& w) {
+__device__ __forceinline__ bool find_item(const PagedParams& p, TileRows tile, int id, Item& w) {
   const int part = plan_part(p, tile);
   auto items = [&](int b) {
     const Sequence q = sequence(p.seq, b);
@@ -90,13 +94,16 @@ __device__ __forceinline__ bool find_item(const PagedParams& p, int tile, int id
   if (!locate(p.seq.n, at, items, b, before)) return false;
   w.b = uniform(b);
   w.q = sequence(p.seq, w.b);
+  w.q = Sequence{uniform(w.q.start), uniform(w.q.n), uniform(w.q.len), uniform(w.q.pos)};   // (loaded by vectors: in scalar registers from here on)
   const int parts = uniform(parts_of(w.q.len, part)), tiles = uniform(tiles_of(w.q.n * p.gq, tile)), i = uniform(at - before);
-  const int unit = i / tiles;                 // K/V head, part
+  const int unit = uniform(i / tiles);        // K/V head, part
   w.tile = tiles - 1 - (i - unit * tiles);    // the last tiles, which see the most keys, first
-  w.hk = unit / parts;
+  w.hk = uniform(unit / parts);
   w.part = unit - w.hk * parts;
-  const int last = min((w.tile + 1) * tile, w.q.n * p.gq) - 1;
-  const int seen = row_limit(p, w.q, last);
+  w.rows = uniform(w.q.n * p.gq);
+  w.rows_of_tile = rows_of(w.rows, tile);
+  const int last = min((w.tile + 1) * w.rows_of_tile, w.rows) - 1;
+  const int seen = uniform(row_limit(p, w.q, last));
   w.n_parts = parts_of(seen, part);
   w.k0 = w.part * part;
   w.k1 = w.part + 1 < w.n_parts ? w.k0 + part : seen;
@@ -120,6 +127,28 @@ __device__ __forceinline__ bool find_item(const PagedParams& p, int tile, int id
   return true;
 }
 
+// 16 bytes (fp32) of a row's result, piece c of row row0 + r of the item, to where they belong; with piece 0 the row's lse (NaN: a weight was one).
+template <int D, bool OUT_F32>
+__device__ __forceinline__ void store_piece(const PagedParams& p, const Item& w, int row0, int slot_row, int r, int c, f32x4 o, float lse) {
+  if (w.n_parts > 1) {
+    const int64_t at = (int64_t)slot_row + r;
+    *reinterpret_cast<f32x4*>(p.part_out + at * D + 4 * c) = o;
+    if (c == 0) p.part_lse[at] = lse;
+    return;
+  }
+  const int t = divide(p.by_gq, row0 + r), head = w.hk * p.gq + row0 + r - t * p.gq;
+  const int64_t at = (int64_t)head * p.o_sh + (int64_t)(w.q.start + t) * p.o_ss + 4 * c;
+  if constexpr (OUT_F32) {
+    *reinterpret_cast<f32x4*>(reinterpret_cast<float*>(p.out) + at) = o;
+  } else {
+    bf16x4 ob;
+#pragma unroll
+    for (int k = 0; k < 4; k++) ob[k] = (__bf16)o[k];
+    *reinterpret_cast<bf16x4*>(reinterpret_cast<__bf16*>(p.out) + at) = ob;
+  }
+  if (c == 0) p.lse[(int64_t)head * p.l_sh + (int64_t)(w.q.start + t) * p.l_ss] = lse != lse ? -INFINITY : lse;
+}
+
 // ---- Few rows.
 //
 // Items of at most 16 * RT rows (a decode step's query heads of a K/V head, drafted tokens).  Each of the four waves takes every fourth
@@ -128,11 +157,11 @@ __device__ __forceinline__ bool find_item(const PagedParams& p, int tile, int id
 // scores of row i for keys 4g .. 4g + 3 of each 16.  In this order the exponentials are the B operand of O^T = V^T P^T (a contraction index may
 // be permuted if both operands agree): its A operand needs 8 keys of one d in a lane, and a lane that loads D / 16 adjacent d's of those 8 keys has them after
 // one exchange of 16-bit halves.  No LDS, no barrier inside the loop.  Bound: HBM.
-template <int D, bool F8, int RT>
+template <int D, bool F8, int RT, int W>
 struct Few {
   static constexpr int TILE = 16 * RT, DL = D / 16;              // rows of a tile; d's of a lane in V
   static constexpr int KL = F8 ? D / 64 : D / 32, VW = (F8 ? DL : 2 * DL) / 4;   // 16-byte loads of a K row's quarter, words of V a key
-  static constexpr int LDS = 4 * TILE * (D + 2) * 4;
+  static constexpr int LDS = W * TILE * (D + 2) * 4;
   struct Frag {
     u32x4 k[2][KL];
     unsigned v[8][VW];
@@ -141,13 +170,14 @@ struct Few {
   };
 };
 
-template <int D, bool F8, int RT, bool OUT_F32>
-__device__ __forceinline__ void few_rows(const PagedParams& p, const Item& w, char* lds) {
-  typedef Few<D, F8, RT> F;
+template <int D, bool F8, int RT, int W, int DEPTH, bool OUT_F32>
+__device__ __forceinline__ void few_rows(const PagedParams& p, const Item& w, int row0, int slot_row, char* lds) {
+  typedef Few<D, F8, RT, W> F;
+  constexpr int STEP = 32 * W;   // keys of a step of the workgroup
   typedef typename F::Frag Frag;
   constexpr int TILE = F::TILE, DL = F::DL, KL = F::KL, VW = F::VW, QS = D / 32;
   const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), i16 = lane & 15, g = lane >> 4;
-  const int row0 = w.tile * TILE, rows = min(TILE, w.q.n * p.gq - row0);
+  const int rows = min(TILE, w.q.n * p.gq - row0);
   const int limit_lo = row_limit(p, w.q, row0), limit_hi = min(w.k1, row_limit(p, w.q, row0 + rows - 1));
 
   bf16x8 qf[RT][QS];
@@ -168,10 +198,10 @@ __device__ __forceinline__ void few_rows(const PagedParams& p, const Item& w, ch
   const int k_lane = i16 * p.slot_b + g * 16, v_lane = g * 4 * p.slot_b + i16 * VW * 4;
 
   // Pages of the wave's groups of 16 keys, 32 stretches ahead: lane 2 j + h has those of group h of stretch j.
-  const int steps = (w.k1 - w.k0 + 127) >> 7;
+  const int steps = (w.k1 - w.k0 + STEP - 1) / STEP;
   Slot at = {-1, 0};
   auto find_pages = [&](int step) __attribute__((always_inline)) {
-    const int key = w.k0 + (step + (lane >> 1)) * 128 + wave * 32 + (lane & 1) * 16;
+    const int key = w.k0 + (step + (lane >> 1)) * STEP + wave * 32 + (lane & 1) * 16;
     at = Slot{-1, 0};
     if (key < w.k1) at = slot_of(p.seq, w.b, key);
   };
@@ -236,7 +266,7 @@ __device__ __forceinline__ void few_rows(const PagedParams& p, const Item& w, ch
 
   unsigned taken_out = 0;
   auto compute = [&](Frag& f, int step) __attribute__((always_inline)) {
-    const int key0 = w.k0 + step * 128 + wave * 32;
+    const int key0 = w.k0 + step * STEP + wave * 32;
     const bool edge = key0 + 32 > limit_lo || key0 + 32 > limit_hi || !f.there[0] || !f.there[1];
     // scores
     f32x4 s[RT][2];
@@ -346,7 +376,7 @@ __device__ __forceinline__ void few_rows(const PagedParams& p, const Item& w, ch
     }
   };
 
-  {
+  if constexpr (DEPTH == 2) {
     Frag fa, fb;
     if (steps > 0) load(fa, 0);
     for (int step = 0; step < steps; step += 2) {
@@ -356,10 +386,17 @@ __device__ __forceinline__ void few_rows(const PagedParams& p, const Item& w, ch
       if (step + 2 < steps) load(fa, step + 2);
       compute(fb, step + 1);
     }
+  } else {
+    Frag f;
+#pragma unroll 1
+    for (int step = 0; step < steps; step++) {
+      load(f, step);
+      compute(f, step);
+    }
   }
   if (__any(taken_out != 0)) {   // (the rows they reach are infinite or NaN whatever else adds up)
 #pragma unroll 1
-    for (int key = w.k0 + wave * 32; key < limit_hi; key += (key & 31) == 31 ? 97 : 1) {
+    for (int key = w.k0 + wave * 32; key < limit_hi; key += (key & 31) == 31 ? STEP - 31 : 1) {
       if (limit_lo >= min((key | 31) + 1, limit_hi)) continue;
       const Slot one = slot_of(p.seq, w.b, key);
       if (one.page < 0) continue;
@@ -383,7 +420,7 @@ __device__ __forceinline__ void few_rows(const PagedParams& p, const Item& w, ch
   }
 
   // ---- the waves' results, added up in LDS: [wave][row][D] (16-byte pieces exchanged among each other by the row), then reference and sum of each
-  float* const ml = reinterpret_cast<float*>(lds + 4 * TILE * D * 4);
+  float* const ml = reinterpret_cast<float*>(lds + W * TILE * D * 4);
 #pragma unroll
   for (int rt = 0; rt < RT; rt++) {
     float l = l_run[rt];
@@ -405,18 +442,18 @@ __device__ __forceinline__ void few_rows(const PagedParams& p, const Item& w, ch
   }
   __syncthreads();
   constexpr int PIECES = D / 4;
-  for (int i = tid; i < rows * PIECES; i += 256) {
+  for (int i = tid; i < rows * PIECES; i += 64 * W) {
     const int r = i / PIECES, c = i % PIECES;
-    float m[4], l[4], top = -INFINITY, total = 0.f;
+    float m[W], l[W], top = -INFINITY, total = 0.f;
 #pragma unroll
-    for (int v = 0; v < 4; v++) {
+    for (int v = 0; v < W; v++) {
       m[v] = ml[(v * TILE + r) * 2];
       l[v] = ml[(v * TILE + r) * 2 + 1];
       top = fmaxf(top, m[v]);
     }
     f32x4 o = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int v = 0; v < 4; v++) {
+    for (int v = 0; v < W; v++) {
       const float a = m[v] == -INFINITY ? 0.f : m[v] == top ? 1.f : __builtin_amdgcn_exp2f((m[v] - top) * c2);
       const f32x4 x = *reinterpret_cast<const f32x4*>(lds + (v * TILE + r) * D * 4 + ((c ^ (r & 15)) << 4));
       total += a * l[v];
@@ -427,41 +464,25 @@ __device__ __forceinline__ void few_rows(const PagedParams& p, const Item& w, ch
     const float lse = total > 0.f ? top * p.scale + logf(total) : -INFINITY;
 #pragma unroll
     for (int k = 0; k < 4; k++) o[k] *= inv;
-    if (w.n_parts > 1) {
-      const int64_t at_slot = (int64_t)w.slot * TILE + r;
-      *reinterpret_cast<f32x4*>(p.part_out + at_slot * D + 4 * c) = o;
-      if (c == 0) p.part_lse[at_slot] = total != total ? __builtin_nanf("") : lse;
-    } else {
-      const int t = divide(p.by_gq, row0 + r), head = w.hk * p.gq + row0 + r - t * p.gq;
-      const int64_t at_out = (int64_t)head * p.o_sh + (int64_t)(w.q.start + t) * p.o_ss + 4 * c;
-      if constexpr (OUT_F32) {
-        *reinterpret_cast<f32x4*>(reinterpret_cast<float*>(p.out) + at_out) = o;
-      } else {
-        bf16x4 ob;
-#pragma unroll
-        for (int k = 0; k < 4; k++) ob[k] = (__bf16)o[k];
-        *reinterpret_cast<bf16x4*>(reinterpret_cast<__bf16*>(p.out) + at_out) = ob;
-      }
-      if (c == 0) p.lse[(int64_t)head * p.l_sh + (int64_t)(w.q.start + t) * p.l_ss] = lse;
-    }
+    store_piece<D, OUT_F32>(p, w, row0, slot_row, r, c, o, total != total ? __builtin_nanf("") : lse);
   }
 }
 
 template <int D, bool F8, int RT, bool OUT_F32>
-__global__ void __launch_bounds__(256) paged_few_kernel(const PagedParams p) {
+__global__ void __launch_bounds__(256, 2) paged_few_kernel(const PagedParams p) {
   extern __shared__ __attribute__((aligned(1024))) char lds[];
   Item w;
-  if (!find_item(p, 16 * RT, (int)blockIdx.x, w)) return;
-  few_rows<D, F8, RT, OUT_F32>(p, w, lds);
+  if (!find_item(p, TileRows{16 * RT, 16 * RT}, (int)blockIdx.x, w)) return;
+  few_rows<D, F8, RT, 4, 1, OUT_F32>(p, w, w.tile * 16 * RT, w.slot * 16 * RT, lds);
 }
 
-// ---- Row tiles whose keys were cut: out = sum of exp(lse_i - lse) out_i over their live parts.  One workgroup a tile and 1024 / D rows of it.
-template <int D, int TILE, bool OUT_F32>
-__global__ void __launch_bounds__(256) paged_fold_kernel(const PagedParams p) {
-  const int part = plan_part(p, TILE);
+// ---- Row tiles whose keys were cut: out = sum of exp(lse_i - lse) out_i over their live parts.  A workgroup has 1024 / D rows of a tile.
+template <int D, bool OUT_F32>
+__global__ void __launch_bounds__(256) paged_fold_kernel(const PagedParams p, TileRows tile) {
+  const int part = plan_part(p, tile);
   auto cut_tiles = [&](int b) {
     const Sequence q = sequence(p.seq, b);
-    return parts_of(q.len, part) > 1 ? tiles_of(q.n * p.gq, TILE) * p.Hkv : 0;
+    return parts_of(q.len, part) > 1 ? tiles_of(q.n * p.gq, tile) * p.Hkv : 0;
   };
   int b, before, base = 0;
   if (!locate(p.seq.n, (int)blockIdx.x, cut_tiles, b, before)) return;
@@ -472,26 +493,30 @@ __global__ void __launch_bounds__(256) paged_fold_kernel(const PagedParams p) {
     if (s < b) n = cut_tiles(s) * parts_of(sequence(p.seq, s).len, part);
     base += __builtin_amdgcn_readlane(wave_scan(n), 63);
   }
-  const Sequence q = sequence(p.seq, b);
-  const int parts = parts_of(q.len, part), tiles = tiles_of(q.n * p.gq, TILE), i = (int)blockIdx.x - before;
-  const int hk = i / tiles, tile = i - hk * tiles, row0 = tile * TILE, rows = min(TILE, q.n * p.gq - row0);
-  const int n_live = parts_of(row_limit(p, q, row0 + rows - 1), part);
+  Item w;
+  w.q = sequence(p.seq, b);
+  w.rows = w.q.n * p.gq;
+  const int parts = parts_of(w.q.len, part), tiles = tiles_of(w.rows, tile), i = (int)blockIdx.x - before, size = rows_of(w.rows, tile);
+  w.hk = i / tiles;
+  const int row0 = (i - w.hk * tiles) * size, rows = min(size, w.rows - row0);
+  const int n_live = parts_of(row_limit(p, w.q, row0 + rows - 1), part);
   const int r = (int)blockIdx.y * (1024 / D) + (int)threadIdx.x / (D / 4), c = (int)threadIdx.x % (D / 4);
   if (n_live == 1 || r >= rows) return;   // one part: written already
   if (base < 0 || base + (i + 1) * parts > 2 * p.target) return;   // (only where sequences overlap)
-  const int64_t slot_row = ((int64_t)base + (int64_t)i * parts) * TILE + r;
+  w.n_parts = 1;   // what follows is stored for good
+  const int64_t slot_row = ((int64_t)base + (int64_t)i * parts) * tile.many + r;
   const float* const ls = p.part_lse + slot_row;
   float top = -INFINITY, total = 0.f;
   bool nan = false;
   for (int k = 0; k < n_live; k++) {
-    const float x = ls[(int64_t)k * TILE];
+    const float x = ls[(int64_t)k * tile.many];
     nan |= x != x;
     top = fmaxf(top, x);
   }
   f32x4 o = {0.f, 0.f, 0.f, 0.f};
   for (int k = 0; k < n_live; k++) {
-    const float x = ls[(int64_t)k * TILE], a = x == -INFINITY ? 0.f : expf(x - top);
-    const f32x4 y = *reinterpret_cast<const f32x4*>(p.part_out + (slot_row + (int64_t)k * TILE) * D + 4 * c);
+    const float x = ls[(int64_t)k * tile.many], a = x == -INFINITY ? 0.f : expf(x - top);
+    const f32x4 y = *reinterpret_cast<const f32x4*>(p.part_out + (slot_row + (int64_t)k * tile.many) * D + 4 * c);
     total += a;
     if (x != -INFINITY) {
 #pragma unroll
@@ -501,17 +526,7 @@ __global__ void __launch_bounds__(256) paged_fold_kernel(const PagedParams p) {
   const float inv = total == 0.f ? 0.f : 1.f / total;
 #pragma unroll
   for (int e = 0; e < 4; e++) o[e] *= inv;
-  const int t = divide(p.by_gq, row0 + r), head = hk * p.gq + row0 + r - t * p.gq;
-  const int64_t at_out = (int64_t)head * p.o_sh + (int64_t)(q.start + t) * p.o_ss + 4 * c;
-  if constexpr (OUT_F32) {
-    *reinterpret_cast<f32x4*>(reinterpret_cast<float*>(p.out) + at_out) = o;
-  } else {
-    bf16x4 ob;
-#pragma unroll
-    for (int e = 0; e < 4; e++) ob[e] = (__bf16)o[e];
-    *reinterpret_cast<bf16x4*>(reinterpret_cast<__bf16*>(p.out) + at_out) = ob;
-  }
-  if (c == 0) p.lse[(int64_t)head * p.l_sh + (int64_t)(q.start + t) * p.l_ss] = nan || !(total > 0.f) ? -INFINITY : top + logf(total);
+  store_piece<D, OUT_F32>(p, w, row0, 0, r, c, o, nan ? __builtin_nanf("") : total > 0.f ? top + logf(total) : -INFINITY);
 }
 
 }  // namespace

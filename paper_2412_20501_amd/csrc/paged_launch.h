@@ -1,0 +1,45 @@
+// Launches of one head dim and type of the pages (one .hip each, so that they compile side by side).
+#pragma once
+#include <atomic>
+
+#include "paged_tile.h"
+
+namespace tr {
+namespace {
+
+// A launch that asks for more LDS than the default limit: raised once for each device and kernel.
+template <typename Kernel, typename... Args>
+hipError_t launch_lds(Kernel kernel, std::atomic<uint64_t>& raised, dim3 grid, dim3 block, int lds_bytes, hipStream_t stream, Args... args) {
+  int dev = 0;
+  hipError_t e = hipGetDevice(&dev);
+  if (e != hipSuccess) return e;
+  const uint64_t bit = dev >= 0 && dev < 64 ? (uint64_t)1 << dev : 0;
+  if (!(raised.load(std::memory_order_acquire) & bit)) {
+    e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, lds_bytes);
+    if (e != hipSuccess) return e;
+    raised.fetch_or(bit, std::memory_order_release);
+  }
+  return launch_kernel(kernel, grid, block, lds_bytes, stream, args...);
+}
+
+template <int D, bool F8, bool OUT_F32>
+hipError_t launch_out(const PagedParams& p, const PagedLaunch& l, hipStream_t stream) {
+  static std::atomic<uint64_t> raised[3];
+  const dim3 items((unsigned)((l.tiles + p.target + 7) / 8 * 8));   // an eighth of the items for every XCD, rounded up
+  hipError_t e;
+  if (l.tile.many == kMixed.many) e = launch_lds(paged_mixed_kernel<D, F8, OUT_F32>, raised[0], items, dim3(512), Tile<D>::LDS, stream, p);
+  else if (l.tile.many == 32) e = launch_lds(paged_few_kernel<D, F8, 2, OUT_F32>, raised[1], items, dim3(256), Few<D, F8, 2, 4>::LDS, stream, p);
+  else e = launch_lds(paged_few_kernel<D, F8, 1, OUT_F32>, raised[2], items, dim3(256), Few<D, F8, 1, 4>::LDS, stream, p);
+  if (e != hipSuccess || p.target == 0) return e;
+  const unsigned cut = (unsigned)(l.tiles < p.target ? l.tiles : p.target);   // a cut tile has two parts at least
+  return launch_kernel(paged_fold_kernel<D, OUT_F32>, dim3(cut, (l.tile.many * D + 1023) / 1024), dim3(256), 0, stream, p, l.tile);
+}
+
+}  // namespace
+
+template <int D, bool F8>
+hipError_t launch_paged_form(const PagedParams& p, const PagedLaunch& l, hipStream_t stream) {
+  return p.out_f32 ? launch_out<D, F8, true>(p, l, stream) : launch_out<D, F8, false>(p, l, stream);
+}
+
+}  // namespace tr

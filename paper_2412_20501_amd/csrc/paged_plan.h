@@ -43,22 +43,28 @@ constexpr Slot slot_of(const Sequences& s, int b, int c) {
   return Slot{page >= 0 && page < s.n_pages ? page : -1, c - i * s.page_size};
 }
 
-// Keys of a part.  work: sum over (sequence, K/V head) of row tiles x keys; target: workgroups that are to share it; 0: keys are not
-// shared out.  A multiple of kPartStep, so that parts begin on whole steps of a workgroup.
+// Rows of the tiles that a sequence's rows (of one K/V head) are cut into: few of them are one tile's, more are tiles of `many`.
+struct TileRows { int few, many; };
+constexpr int rows_of(int rows, TileRows t) { return rows <= t.few ? t.few : t.many; }
+constexpr int tiles_of(int rows, TileRows t) { return (rows + rows_of(rows, t) - 1) / rows_of(rows, t); }
+
+// Keys of a part.  work: sum over (sequence, K/V head) of row tiles x keys; tiles: sum of row tiles; target: workgroups that run at once, among which the
+// keys are to be shared out so that they run in one round, 0: keys are not shared out.  A tile's last part is half a part on average, so that many
+// parts fall away.  A multiple of kPartStep, so that parts begin on whole steps of a workgroup.
 // Row tiles whose keys are cut have ceil(keys / part) parts, fewer than 2 keys / part: all of them together fewer than 2 * target.
 constexpr int kPartStep = 128;
-constexpr int part_keys(int64_t work, int target, int least) {
+constexpr int part_keys(int64_t work, int64_t tiles, int target, int least) {
   if (target <= 0) return kPosLimit;   // (as many keys as a sequence has at most)
-  const int64_t keys = (work + target - 1) / target, up = (keys + kPartStep - 1) / kPartStep * kPartStep;
+  const int64_t n = target - (tiles < target ? tiles : target) / 2;
+  const int64_t keys = (work + n - 1) / n, up = (keys + kPartStep - 1) / kPartStep * kPartStep;
   return up < least ? least : up > kPosLimit ? kPosLimit : (int)up;
 }
 constexpr int parts_of(int keys, int part) { return keys <= part ? 1 : (keys - 1) / part + 1; }
-constexpr int tiles_of(int rows, int tile) { return (rows + tile - 1) / tile; }
 
 // Row tiles that the sequences of `tokens` tokens have at most, `group` rows a token: a sequence with tokens has at most one that is not full.
-constexpr int64_t most_tiles(int64_t tokens, int64_t n_seqs, int64_t group, int tile) {
+constexpr int64_t most_tiles(int64_t tokens, int64_t n_seqs, int64_t group, TileRows t) {
   const int64_t some = tokens < n_seqs ? tokens : n_seqs;
-  return (tokens * group) / tile + some;
+  return (tokens * group) / t.many + some;
 }
 
 }  // namespace tr
