@@ -45,21 +45,27 @@ struct PagedParams {
   Divisor by_gq;
   int causal, out_f32;
   float scale;
+  RowClass rows;   // of the launch
   int target;      // workgroups among which the keys are shared out, 0: they are not
   int least_part;  // keys of a part at least
   float* part_out; // [2 * target slots][rows of a tile][D]
   float* part_lse; // [2 * target slots][rows of a tile]
 };
 
-// How a call is launched: the form of its row tiles and the workgroups that share its keys.
-constexpr TileRows kMixed = {16, 256};   // few rows and many in one launch
+// How a call is launched: one launch for each class of sequences.
+constexpr int kManyRows = 256;   // rows of the tiles of sequences with many
 struct PagedLaunch {
-  TileRows tile;   // few == many: one form; else kMixed
-  int target;      // as above, where a workspace is there
-  int64_t tiles;   // of all sequences and K/V heads, at most
+  int n;
+  struct Part {
+    RowClass rows;
+    int target;      // as above, where a workspace is there
+    int64_t tiles;   // of all sequences and K/V heads, at most
+    int64_t floats(int D) const { return (int64_t)target * 2 * rows.tile * (D + 1); }   // of the workspace
+  } part[2];
 };
 PagedLaunch paged_launch(int64_t tokens, int64_t n_seqs, int64_t max_keys, int Hkv, int gq, int D);
-hipError_t launch_paged_attn(const PagedParams& p, const PagedLaunch& l, int D, bool f8, hipStream_t stream);
+// p without what belongs to a launch (rows, target, scratch); workspace: null or the floats of all parts
+hipError_t launch_paged_attn(PagedParams& p, const PagedLaunch& l, int D, bool f8, float* workspace, hipStream_t stream);
 
 #if defined(__HIPCC__)
 // Two e4m3 values (the upper ones of x, if upper) times 2^(scale - 127), as two bf16: the conversion takes the scale as the exponent of a float.

@@ -242,7 +242,9 @@ size_t tr_paged_attn_workspace_bytes(const tr_tensor* q, const tr_tensor* k_page
   if (k_pages->S < 16 || n_seqs < 0 || max_pages < 0 || max_pages > kMaxKeys / k_pages->S || n_seqs > (1 << 24) || q->S * q->H >= ((int64_t)1 << 31)) return 0;
   if (q->S == 0 || q->H == 0 || n_seqs == 0) return 0;
   const tr::PagedLaunch l = tr::paged_launch(q->S, n_seqs, max_pages * k_pages->S, (int)k_pages->H, (int)(q->H / k_pages->H), (int)q->D);
-  return (size_t)l.target * 2 * l.tile.many * (size_t)(q->D + 1) * 4;
+  int64_t floats = 0;
+  for (int i = 0; i < l.n; i++) floats += l.part[i].floats((int)q->D);
+  return (size_t)floats * 4;
 }
 
 tr_status tr_paged_attn(const tr_tensor* q_, const tr_tensor* k_pages_, const tr_tensor* v_pages_, const tr_tensor* k_scales_,
@@ -280,8 +282,9 @@ tr_status tr_paged_attn(const tr_tensor* q_, const tr_tensor* k_pages_, const tr
   if (q->H == 0 || q->S == 0 || p.seq.n == 0) return TR_OK;
 
   const int gq = (int)(q->H / k_pages->H), D = (int)q->D;
-  tr::PagedLaunch l = tr::paged_launch(q->S, p.seq.n, (int64_t)p.seq.max_pages * p.seq.page_size, (int)k_pages->H, gq, D);
-  if (l.tiles + l.target >= ((int64_t)1 << 24)) return fail(TR_ERR_SHAPE, "too many workgroups for one launch");
+  const tr::PagedLaunch l = tr::paged_launch(q->S, p.seq.n, (int64_t)p.seq.max_pages * p.seq.page_size, (int)k_pages->H, gq, D);
+  for (int i = 0; i < l.n; i++)
+    if (l.part[i].tiles + l.part[i].target >= ((int64_t)1 << 23)) return fail(TR_ERR_SHAPE, "too many workgroups for one launch");   // (of 512 threads, fewer than 2^32 in all)
   const size_t need = tr_paged_attn_workspace_bytes(q, k_pages, seqs->n_seqs, seqs->max_pages);
   if (workspace && need > 0) {
     if ((uintptr_t)workspace % 256) return fail(TR_ERR_WORKSPACE, "workspace must be 256-byte aligned");
@@ -294,8 +297,6 @@ tr_status tr_paged_attn(const tr_tensor* q_, const tr_tensor* k_pages_, const tr
     const tr_tensor* const ws[] = {&all};
     const tr_tensor* const others[] = {q, k_pages, v_pages, k_scales, v_scales, out, lse};
     if (check_apart(ws, 1, others, 7, views) != TR_OK) return fail(TR_ERR_ALIAS, "workspace overlaps a tensor argument");
-  } else {
-    l.target = 0;
   }
   p.q = (const __bf16*)q->ptr; p.out = out->ptr; p.lse = (float*)lse->ptr;
   p.q_sh = q->stride_h; p.q_ss = q->stride_s;
@@ -312,11 +313,8 @@ tr_status tr_paged_attn(const tr_tensor* q_, const tr_tensor* k_pages_, const tr
   p.by_gq = tr::make_divisor((unsigned)gq);
   p.causal = causal != 0; p.out_f32 = out->dtype == TR_F32;
   p.scale = scale;
-  p.target = l.target;
   p.least_part = 256;
-  p.part_out = (float*)workspace;
-  p.part_lse = p.part_out ? p.part_out + (int64_t)2 * l.target * l.tile.many * D : nullptr;
-  const hipError_t e = tr::launch_paged_attn(p, l, D, k_scales != nullptr, (hipStream_t)hip_stream);
+  const hipError_t e = tr::launch_paged_attn(p, l, D, k_scales != nullptr, need > 0 ? (float*)workspace : nullptr, (hipStream_t)hip_stream);
   if (e != hipSuccess) return fail(TR_ERR_HIP, "paged attention launch failed: %s", hipGetErrorString(e));
   return TR_OK;
 }

@@ -2,5 +2,5 @@
 #include "paged_launch.h"
 
 namespace tr {
-template hipError_t launch_paged_form<128, false>(const PagedParams&, const PagedLaunch&, hipStream_t);
+template hipError_t launch_paged_form<128, false>(PagedParams&, const PagedLaunch&, float*, hipStream_t);
 }  // namespace tr

@@ -53,12 +53,12 @@ __device__ __forceinline__ bool locate(int n, int at, Count count, int& b, int& 
 }
 
 // Keys of a part of this call.
-__device__ __forceinline__ int plan_part(const PagedParams& p, TileRows tile) {
+__device__ __forceinline__ int plan_part(const PagedParams& p) {
   int64_t work = 0, tiles = 0;
   if (p.target > 0) {
     for (int b = threadIdx.x & 63; b < p.seq.n; b += 64) {
       const Sequence q = sequence(p.seq, b);
-      const int n = tiles_of(q.n * p.gq, tile);
+      const int n = tiles_of(q.n * p.gq, p.rows);
       work += (int64_t)n * q.len;
       tiles += n;
     }
@@ -69,7 +69,7 @@ __device__ __forceinline__ int plan_part(const PagedParams& p, TileRows tile) {
 }
 
 struct Item {
-  int rows, rows_of_tile;           // of the sequence and a K/V head; of its tiles, but the last
+  int rows;                         // of the sequence and a K/V head
   int b, hk, tile, part, n_parts;   // n_parts: live ones, those whose keys some row of the tile sees, and the first one
   int k0, k1;                       // its keys
   int slot;                         // of the scratch, if n_parts > 1
@@ -81,11 +81,11 @@ __device__ __forceinline__ int row_limit(const PagedParams& p, const Sequence& q
 
 // The item of workgroup `id` of `ids`; false: none.  The items of a K/V head and part lie next to each other, and each XCD has a contiguous
 // eighth of all, so that row tiles which read the same keys mostly share an L2.
-__device__ __forceinline__ bool find_item(const PagedParams& p, TileRows tile, int id, Item& w) {
-  const int part = plan_part(p, tile);
+__device__ __forceinline__ bool find_item(const PagedParams& p, int id, Item& w) {
+  const int part = plan_part(p);
   auto items = [&](int b) {
     const Sequence q = sequence(p.seq, b);
-    return tiles_of(q.n * p.gq, tile) * parts_of(q.len, part) * p.Hkv;
+    return tiles_of(q.n * p.gq, p.rows) * parts_of(q.len, part) * p.Hkv;
   };
   int before, b = 0;
   locate(p.seq.n, 0x7fffffff, items, b, before);
@@ -95,14 +95,13 @@ __device__ __forceinline__ bool find_item(const PagedParams& p, TileRows tile, i
   w.b = uniform(b);
   w.q = sequence(p.seq, w.b);
   w.q = Sequence{uniform(w.q.start), uniform(w.q.n), uniform(w.q.len), uniform(w.q.pos)};   // (loaded by vectors: in scalar registers from here on)
-  const int parts = uniform(parts_of(w.q.len, part)), tiles = uniform(tiles_of(w.q.n * p.gq, tile)), i = uniform(at - before);
+  const int parts = uniform(parts_of(w.q.len, part)), tiles = uniform(tiles_of(w.q.n * p.gq, p.rows)), i = uniform(at - before);
   const int unit = uniform(i / tiles);        // K/V head, part
   w.tile = tiles - 1 - (i - unit * tiles);    // the last tiles, which see the most keys, first
   w.hk = uniform(unit / parts);
   w.part = unit - w.hk * parts;
   w.rows = uniform(w.q.n * p.gq);
-  w.rows_of_tile = rows_of(w.rows, tile);
-  const int last = min((w.tile + 1) * w.rows_of_tile, w.rows) - 1;
+  const int last = min((w.tile + 1) * p.rows.tile, w.rows) - 1;
   const int seen = uniform(row_limit(p, w.q, last));
   w.n_parts = parts_of(seen, part);
   w.k0 = w.part * part;
@@ -112,7 +111,7 @@ __device__ __forceinline__ bool find_item(const PagedParams& p, TileRows tile, i
     auto cut = [&](int s) {
       const Sequence q = sequence(p.seq, s);
       const int n = parts_of(q.len, part);
-      return n > 1 ? tiles_of(q.n * p.gq, tile) * n * p.Hkv : 0;
+      return n > 1 ? tiles_of(q.n * p.gq, p.rows) * n * p.Hkv : 0;
     };
     int base = 0;
     for (int b0 = 0; b0 < w.b; b0 += 64) {
@@ -472,17 +471,17 @@ template <int D, bool F8, int RT, bool OUT_F32>
 __global__ void __launch_bounds__(256, 2) paged_few_kernel(const PagedParams p) {
   extern __shared__ __attribute__((aligned(1024))) char lds[];
   Item w;
-  if (!find_item(p, TileRows{16 * RT, 16 * RT}, (int)blockIdx.x, w)) return;
+  if (!find_item(p, (int)blockIdx.x, w)) return;
   few_rows<D, F8, RT, 4, 1, OUT_F32>(p, w, w.tile * 16 * RT, w.slot * 16 * RT, lds);
 }
 
 // ---- Row tiles whose keys were cut: out = sum of exp(lse_i - lse) out_i over their live parts.  A workgroup has 1024 / D rows of a tile.
 template <int D, bool OUT_F32>
-__global__ void __launch_bounds__(256) paged_fold_kernel(const PagedParams p, TileRows tile) {
-  const int part = plan_part(p, tile);
+__global__ void __launch_bounds__(256) paged_fold_kernel(const PagedParams p) {
+  const int part = plan_part(p), size = p.rows.tile;
   auto cut_tiles = [&](int b) {
     const Sequence q = sequence(p.seq, b);
-    return parts_of(q.len, part) > 1 ? tiles_of(q.n * p.gq, tile) * p.Hkv : 0;
+    return parts_of(q.len, part) > 1 ? tiles_of(q.n * p.gq, p.rows) * p.Hkv : 0;
   };
   int b, before, base = 0;
   if (!locate(p.seq.n, (int)blockIdx.x, cut_tiles, b, before)) return;
@@ -496,7 +495,7 @@ __global__ void __launch_bounds__(256) paged_fold_kernel(const PagedParams p, Ti
   Item w;
   w.q = sequence(p.seq, b);
   w.rows = w.q.n * p.gq;
-  const int parts = parts_of(w.q.len, part), tiles = tiles_of(w.rows, tile), i = (int)blockIdx.x - before, size = rows_of(w.rows, tile);
+  const int parts = parts_of(w.q.len, part), tiles = tiles_of(w.rows, p.rows), i = (int)blockIdx.x - before;
   w.hk = i / tiles;
   const int row0 = (i - w.hk * tiles) * size, rows = min(size, w.rows - row0);
   const int n_live = parts_of(row_limit(p, w.q, row0 + rows - 1), part);
@@ -504,19 +503,19 @@ __global__ void __launch_bounds__(256) paged_fold_kernel(const PagedParams p, Ti
   if (n_live == 1 || r >= rows) return;   // one part: written already
   if (base < 0 || base + (i + 1) * parts > 2 * p.target) return;   // (only where sequences overlap)
   w.n_parts = 1;   // what follows is stored for good
-  const int64_t slot_row = ((int64_t)base + (int64_t)i * parts) * tile.many + r;
+  const int64_t slot_row = ((int64_t)base + (int64_t)i * parts) * size + r;
   const float* const ls = p.part_lse + slot_row;
   float top = -INFINITY, total = 0.f;
   bool nan = false;
   for (int k = 0; k < n_live; k++) {
-    const float x = ls[(int64_t)k * tile.many];
+    const float x = ls[(int64_t)k * size];
     nan |= x != x;
     top = fmaxf(top, x);
   }
   f32x4 o = {0.f, 0.f, 0.f, 0.f};
   for (int k = 0; k < n_live; k++) {
-    const float x = ls[(int64_t)k * tile.many], a = x == -INFINITY ? 0.f : expf(x - top);
-    const f32x4 y = *reinterpret_cast<const f32x4*>(p.part_out + (slot_row + (int64_t)k * tile.many) * D + 4 * c);
+    const float x = ls[(int64_t)k * size], a = x == -INFINITY ? 0.f : expf(x - top);
+    const f32x4 y = *reinterpret_cast<const f32x4*>(p.part_out + (slot_row + (int64_t)k * size) * D + 4 * c);
     total += a;
     if (x != -INFINITY) {
 #pragma unroll

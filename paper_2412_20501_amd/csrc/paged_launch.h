@@ -23,23 +23,34 @@ hipError_t launch_lds(Kernel kernel, std::atomic<uint64_t>& raised, dim3 grid, d
 }
 
 template <int D, bool F8, bool OUT_F32>
-hipError_t launch_out(const PagedParams& p, const PagedLaunch& l, hipStream_t stream) {
+hipError_t launch_out(PagedParams& p, const PagedLaunch& l, float* workspace, hipStream_t stream) {
   static std::atomic<uint64_t> raised[3];
-  const dim3 items((unsigned)((l.tiles + p.target + 7) / 8 * 8));   // an eighth of the items for every XCD, rounded up
-  hipError_t e;
-  if (l.tile.many == kMixed.many) e = launch_lds(paged_mixed_kernel<D, F8, OUT_F32>, raised[0], items, dim3(512), Tile<D>::LDS, stream, p);
-  else if (l.tile.many == 32) e = launch_lds(paged_few_kernel<D, F8, 2, OUT_F32>, raised[1], items, dim3(256), Few<D, F8, 2, 4>::LDS, stream, p);
-  else e = launch_lds(paged_few_kernel<D, F8, 1, OUT_F32>, raised[2], items, dim3(256), Few<D, F8, 1, 4>::LDS, stream, p);
-  if (e != hipSuccess || p.target == 0) return e;
-  const unsigned cut = (unsigned)(l.tiles < p.target ? l.tiles : p.target);   // a cut tile has two parts at least
-  return launch_kernel(paged_fold_kernel<D, OUT_F32>, dim3(cut, (l.tile.many * D + 1023) / 1024), dim3(256), 0, stream, p, l.tile);
+  for (int i = 0; i < l.n; i++) {
+    const PagedLaunch::Part& c = l.part[i];
+    p.rows = c.rows;
+    p.target = workspace ? c.target : 0;
+    p.part_out = workspace;
+    p.part_lse = workspace ? workspace + (int64_t)2 * c.target * c.rows.tile * D : nullptr;
+    if (workspace) workspace += c.floats(D);
+    const dim3 items((unsigned)((c.tiles + p.target + 7) / 8 * 8));   // an eighth of the items for every XCD, rounded up
+    hipError_t e;
+    if (c.rows.tile == kManyRows) e = launch_lds(paged_many_kernel<D, F8, OUT_F32>, raised[0], items, dim3(512), Tile<D>::LDS, stream, p);
+    else if (c.rows.tile == 32) e = launch_lds(paged_few_kernel<D, F8, 2, OUT_F32>, raised[1], items, dim3(256), Few<D, F8, 2, 4>::LDS, stream, p);
+    else e = launch_lds(paged_few_kernel<D, F8, 1, OUT_F32>, raised[2], items, dim3(256), Few<D, F8, 1, 4>::LDS, stream, p);
+    if (e != hipSuccess) return e;
+    if (p.target == 0) continue;
+    const unsigned cut = (unsigned)(c.tiles < p.target ? c.tiles : p.target);   // a cut tile has two parts at least
+    e = launch_kernel(paged_fold_kernel<D, OUT_F32>, dim3(cut, (c.rows.tile * D + 1023) / 1024), dim3(256), 0, stream, p);
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
 }
 
 }  // namespace
 
 template <int D, bool F8>
-hipError_t launch_paged_form(const PagedParams& p, const PagedLaunch& l, hipStream_t stream) {
-  return p.out_f32 ? launch_out<D, F8, true>(p, l, stream) : launch_out<D, F8, false>(p, l, stream);
+hipError_t launch_paged_form(PagedParams& p, const PagedLaunch& l, float* workspace, hipStream_t stream) {
+  return p.out_f32 ? launch_out<D, F8, true>(p, l, workspace, stream) : launch_out<D, F8, false>(p, l, workspace, stream);
 }
 
 }  // namespace tr

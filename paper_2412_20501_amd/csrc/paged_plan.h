@@ -43,10 +43,9 @@ constexpr Slot slot_of(const Sequences& s, int b, int c) {
   return Slot{page >= 0 && page < s.n_pages ? page : -1, c - i * s.page_size};
 }
 
-// Rows of the tiles that a sequence's rows (of one K/V head) are cut into: few of them are one tile's, more are tiles of `many`.
-struct TileRows { int few, many; };
-constexpr int rows_of(int rows, TileRows t) { return rows <= t.few ? t.few : t.many; }
-constexpr int tiles_of(int rows, TileRows t) { return (rows + rows_of(rows, t) - 1) / rows_of(rows, t); }
+// The sequences that a launch serves: those with more than `over` and at most `most` rows a K/V head, in tiles of `tile` rows.
+struct RowClass { int tile, over, most; };
+constexpr int tiles_of(int rows, RowClass c) { return rows > c.over && rows <= c.most ? (rows + c.tile - 1) / c.tile : 0; }
 
 // Keys of a part.  work: sum over (sequence, K/V head) of row tiles x keys; tiles: sum of row tiles; target: workgroups that run at once, among which the
 // keys are to be shared out so that they run in one round, 0: keys are not shared out.  A tile's last part is half a part on average, so that many
@@ -61,10 +60,10 @@ constexpr int part_keys(int64_t work, int64_t tiles, int target, int least) {
 }
 constexpr int parts_of(int keys, int part) { return keys <= part ? 1 : (keys - 1) / part + 1; }
 
-// Row tiles that the sequences of `tokens` tokens have at most, `group` rows a token: a sequence with tokens has at most one that is not full.
-constexpr int64_t most_tiles(int64_t tokens, int64_t n_seqs, int64_t group, TileRows t) {
-  const int64_t some = tokens < n_seqs ? tokens : n_seqs;
-  return (tokens * group) / t.many + some;
+// Row tiles that the sequences of `tokens` tokens have at most, `group` rows a token: each has at most one that is not full.
+constexpr int64_t most_tiles(int64_t tokens, int64_t n_seqs, int64_t group, RowClass c) {
+  const int64_t some = tokens * group / (c.over + 1);
+  return tokens * group / c.tile + (some < n_seqs ? some : n_seqs);
 }
 
 }  // namespace tr

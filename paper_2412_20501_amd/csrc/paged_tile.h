@@ -44,7 +44,7 @@ __device__ __forceinline__ float halves_sum(float x) {
 // by few_rows, 16 rows at a time, which holds nothing of either against it.
 template <int D>
 struct Tile {
-  static constexpr int RB = 2 * D, BN = D == 64 ? 128 : 64, NS = 4, TILE_BYTES = BN * RB, ROWS = 256;
+  static constexpr int RB = 2 * D, BN = D == 64 ? 128 : 64, NS = 4, TILE_BYTES = BN * RB, ROWS = kManyRows;
   static constexpr int RINGS = 2 * NS * TILE_BYTES, FLAG = RINGS, LSE = RINGS + 64, LDS = LSE + ROWS * 4;
   static_assert(TILE_BYTES == 16384 && 8 * 32 * 4 * D <= RINGS, "the waves' results lie where the rings were");
 };
@@ -486,19 +486,15 @@ __device__ __forceinline__ bool tile_rows(const PagedParams& p, const Item& w, i
 }
 
 template <int D, bool F8, bool OUT_F32>
-__global__ void __launch_bounds__(512, 2) paged_mixed_kernel(const PagedParams p) {
+__global__ void __launch_bounds__(512, 2) paged_many_kernel(const PagedParams p) {
   extern __shared__ __attribute__((aligned(1024))) char lds[];
   Item w;
-  if (!find_item(p, kMixed, (int)blockIdx.x, w)) return;
-  const int slot_row = w.slot * kMixed.many;
-  if (w.rows > kMixed.few) {
-    if (tile_rows<D, F8, OUT_F32>(p, w, slot_row, lds)) return;
+  if (!find_item(p, (int)blockIdx.x, w)) return;
+  const int row0 = w.tile * kManyRows, slot_row = w.slot * kManyRows, n = min(kManyRows, w.rows - row0);
+  if (tile_rows<D, F8, OUT_F32>(p, w, slot_row, lds)) return;
+  for (int r = 0; r < n; r += 16) {
     __syncthreads();
-  }
-  const int row0 = w.tile * w.rows_of_tile, n = min(w.rows_of_tile, w.rows - row0);
-  for (int r = 0; r < n; r += kMixed.few) {
-    few_rows<D, F8, kMixed.few / 16, 8, 1, OUT_F32>(p, w, row0 + r, slot_row + r, lds);
-    __syncthreads();
+    few_rows<D, F8, 1, 8, 1, OUT_F32>(p, w, row0 + r, slot_row + r, lds);
   }
 }
 

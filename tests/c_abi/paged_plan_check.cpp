@@ -31,7 +31,7 @@ int main() {
     s.table = table.data(); s.kv_len = len.data(); s.q_start = start.data(); s.q_pos = with_pos ? pos.data() : nullptr;
     s.table_stride = max_pages; s.n = n; s.max_pages = max_pages; s.tokens = tokens; s.n_pages = n_pages; s.page_size = page_size;
     s.by_page = tr::make_divisor((unsigned)page_size);
-    for (tr::TileRows tile : {tr::TileRows{16, 16}, tr::TileRows{32, 32}, tr::TileRows{16, 256}, tr::TileRows{32, 128}})
+    for (tr::RowClass tile : {tr::RowClass{16, 0, 1 << 30}, tr::RowClass{32, 0, 1 << 30}, tr::RowClass{32, 0, 32}, tr::RowClass{256, 32, 1 << 30}})
       for (int target : {0, 8, 512}) {
         int64_t work = 0, tiles = 0;
         for (int b = 0; b < n; b++) {
