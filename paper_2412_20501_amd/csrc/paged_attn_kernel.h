@@ -18,28 +18,65 @@ constexpr float kLog2e = 1.4426950408889634f;
 // The lengths lie in device memory, so the launch does not know them: it has as many workgroups as the shapes allow work items, and every
 // workgroup finds its own item, by sums over the sequences that each of its waves takes for itself (64 sequences a load).  An item
 // is a row tile of a K/V head of a sequence on one part of the keys; parts are as long as makes all items about target (part_keys).
+template <int CONTROL, int ROWS>
+__device__ __forceinline__ int from_lane(int x) { return __builtin_amdgcn_update_dpp(0, x, CONTROL, ROWS, 0xf, false); }   // 0 where no lane is
 __device__ __forceinline__ int wave_scan(int x) {   // sum over the lanes up to and including this one
-#pragma unroll
-  for (int d = 1; d < 64; d *= 2) {
-    const int y = __shfl_up(x, d);
-    if ((int)(threadIdx.x & 63) >= d) x += y;
-  }
+  x += from_lane<0x111, 0xf>(x);   // rows of 16 lanes: from 1, 2, 4, 8 below,
+  x += from_lane<0x112, 0xf>(x);
+  x += from_lane<0x114, 0xf>(x);
+  x += from_lane<0x118, 0xf>(x);
+  x += from_lane<0x142, 0xa>(x);   // then a row's last lane to the next row,
+  x += from_lane<0x143, 0xc>(x);   // and the lower half's to the upper
   return x;
 }
+template <int CONTROL, int ROWS>
+__device__ __forceinline__ int64_t add_from(int64_t x) {
+  return x + (int64_t)(((uint64_t)(unsigned)from_lane<CONTROL, ROWS>((int)(x >> 32)) << 32) | (unsigned)from_lane<CONTROL, ROWS>((int)x));
+}
 __device__ __forceinline__ int64_t wave_sum(int64_t x) {
-#pragma unroll
-  for (int d = 32; d > 0; d /= 2) x += __shfl_xor(x, d);
-  return x;
+  x = add_from<0x118, 0xf>(add_from<0x114, 0xf>(add_from<0x112, 0xf>(add_from<0x111, 0xf>(x))));
+  x = add_from<0x143, 0xc>(add_from<0x142, 0xa>(x));
+  return (int64_t)(((uint64_t)(unsigned)__builtin_amdgcn_readlane((int)(x >> 32), 63) << 32) | (unsigned)__builtin_amdgcn_readlane((int)x, 63));
 }
 __device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
 
-// Sums count(b) over the sequences up to the one that holds element `at`: true, and its b and the sum before it; false, and the sum of all.
-template <typename Count>
-__device__ __forceinline__ bool locate(int n, int at, Count count, int& b, int& before) {
+// What the sums are over.  Lane i has sequence i in registers; further ones are loaded when their 64 come up.
+struct Plan {
+  int n;            // sequences
+  int part;         // keys of a part
+  Sequence first;   // sequence `lane` (empty if there is none)
+};
+__device__ __forceinline__ Sequence lane_sequence(const PagedParams& p, const Plan& plan, int b0) {
+  const int b = b0 + (int)(threadIdx.x & 63);
+  return b0 == 0 ? plan.first : b < plan.n ? sequence(p.seq, b) : Sequence{0, 0, 0, 0};
+}
+__device__ __forceinline__ Plan make_plan(const PagedParams& p) {
+  Plan plan;
   const int lane = threadIdx.x & 63;
+  plan.n = p.seq.n;
+  plan.first = Sequence{0, 0, 0, 0};
+  if (lane < plan.n) plan.first = sequence(p.seq, lane);
+  int64_t work = 0, tiles = 0;
+  if (p.target > 0) {
+    for (int b0 = 0; b0 < plan.n; b0 += 64) {
+      const Sequence q = lane_sequence(p, plan, b0);
+      const int n = tiles_of(q.n * p.gq, p.rows);
+      work += (int64_t)n * steps_of(q.len);
+      tiles += n;
+    }
+    work = wave_sum(work) * p.Hkv;
+    tiles = wave_sum(tiles) * p.Hkv;
+  }
+  plan.part = uniform(part_keys(work, tiles, p.target, p.least_part));
+  return plan;
+}
+
+// Sums count(sequence) over the sequences up to the one that holds element `at`: true, and its number and the sum before it; false, and the sum of all.
+template <typename Count>
+__device__ __forceinline__ bool locate(const PagedParams& p, const Plan& plan, int at, Count count, int& b, int& before) {
   before = 0;
-  for (int b0 = 0; b0 < n; b0 += 64) {
-    const int c = b0 + lane < n ? count(b0 + lane) : 0, upto = wave_scan(c);
+  for (int b0 = 0; b0 < plan.n; b0 += 64) {
+    const int c = count(lane_sequence(p, plan, b0)), upto = wave_scan(c);
     const unsigned long long over = __ballot(at < before + upto);
     if (over) {
       const int i = __builtin_ctzll(over);
@@ -51,21 +88,15 @@ __device__ __forceinline__ bool locate(int n, int at, Count count, int& b, int& 
   }
   return false;
 }
-
-// Keys of a part of this call.
-__device__ __forceinline__ int plan_part(const PagedParams& p) {
-  int64_t work = 0, tiles = 0;
-  if (p.target > 0) {
-    for (int b = threadIdx.x & 63; b < p.seq.n; b += 64) {
-      const Sequence q = sequence(p.seq, b);
-      const int n = tiles_of(q.n * p.gq, p.rows);
-      work += (int64_t)n * q.len;
-      tiles += n;
-    }
-    work = wave_sum(work) * p.Hkv;
-    tiles = wave_sum(tiles) * p.Hkv;
+// The sum of count over the sequences in front of b.
+template <typename Count>
+__device__ __forceinline__ int sum_before(const PagedParams& p, const Plan& plan, int end, Count count) {
+  int sum = 0;
+  for (int b0 = 0; b0 < end; b0 += 64) {
+    const int c = b0 + (int)(threadIdx.x & 63) < end ? count(lane_sequence(p, plan, b0)) : 0;
+    sum += __builtin_amdgcn_readlane(wave_scan(c), 63);
   }
-  return uniform(part_keys(work, tiles, p.target, p.least_part));
+  return sum;
 }
 
 struct Item {
@@ -78,50 +109,44 @@ struct Item {
 
 // Rows of a tile see keys 0 .. limit(row) - 1; row r of a sequence and K/V head is query head r mod gq of token r / gq.
 __device__ __forceinline__ int row_limit(const PagedParams& p, const Sequence& q, int r) { return visible(q, divide(p.by_gq, r), p.causal); }
+__device__ __forceinline__ Sequence uniform_sequence(const PagedParams& p, int b) {   // (loaded by vectors, in scalar registers from here on)
+  const Sequence q = sequence(p.seq, b);
+  return Sequence{uniform(q.start), uniform(q.n), uniform(q.len), uniform(q.pos)};
+}
 
 // The item of workgroup `id` of `ids`; false: none.  The items of a K/V head and part lie next to each other, and each XCD has a contiguous
 // eighth of all, so that row tiles which read the same keys mostly share an L2.
 __device__ __forceinline__ bool find_item(const PagedParams& p, int id, Item& w) {
-  const int part = plan_part(p);
-  auto items = [&](int b) {
-    const Sequence q = sequence(p.seq, b);
-    return tiles_of(q.n * p.gq, p.rows) * parts_of(q.len, part) * p.Hkv;
-  };
+  const Plan plan = make_plan(p);
+  const int part = plan.part;
+  auto items = [&](const Sequence& q) { return tiles_of(q.n * p.gq, p.rows) * parts_of(q.len, part) * p.Hkv; };
   int before, b = 0;
-  locate(p.seq.n, 0x7fffffff, items, b, before);
+  locate(p, plan, 0x7fffffff, items, b, before);
   const int total = before, each = (total + 7) >> 3, at = (id & 7) * each + (id >> 3);
   if ((id >> 3) >= each || at >= total) return false;
-  if (!locate(p.seq.n, at, items, b, before)) return false;
+  if (!locate(p, plan, at, items, b, before)) return false;
   w.b = uniform(b);
-  w.q = sequence(p.seq, w.b);
-  w.q = Sequence{uniform(w.q.start), uniform(w.q.n), uniform(w.q.len), uniform(w.q.pos)};   // (loaded by vectors: in scalar registers from here on)
-  const int parts = uniform(parts_of(w.q.len, part)), tiles = uniform(tiles_of(w.q.n * p.gq, p.rows)), i = uniform(at - before);
+  w.q = uniform_sequence(p, w.b);
+  w.rows = uniform(w.q.n * p.gq);
+  const int parts = uniform(parts_of(w.q.len, part)), tiles = uniform(tiles_of(w.rows, p.rows)), i = uniform(at - before);
   const int unit = uniform(i / tiles);        // K/V head, part
   w.tile = tiles - 1 - (i - unit * tiles);    // the last tiles, which see the most keys, first
   w.hk = uniform(unit / parts);
   w.part = unit - w.hk * parts;
-  w.rows = uniform(w.q.n * p.gq);
   const int last = min((w.tile + 1) * p.rows.tile, w.rows) - 1;
   const int seen = uniform(row_limit(p, w.q, last));
   w.n_parts = parts_of(seen, part);
   w.k0 = w.part * part;
   w.k1 = w.part + 1 < w.n_parts ? w.k0 + part : seen;
   if (w.part >= w.n_parts) return false;
+  w.slot = 0;
   if (parts > 1) {   // its scratch slot: among the items of sequences whose keys are cut
-    auto cut = [&](int s) {
-      const Sequence q = sequence(p.seq, s);
+    const int base = sum_before(p, plan, w.b, [&](const Sequence& q) {
       const int n = parts_of(q.len, part);
       return n > 1 ? tiles_of(q.n * p.gq, p.rows) * n * p.Hkv : 0;
-    };
-    int base = 0;
-    for (int b0 = 0; b0 < w.b; b0 += 64) {
-      const int s = b0 + (int)(threadIdx.x & 63);
-      base += __builtin_amdgcn_readlane(wave_scan(s < w.b ? cut(s) : 0), 63);
-    }
+    });
     w.slot = base + (w.hk * tiles + w.tile) * parts + w.part;
     if (w.slot < 0 || w.slot >= 2 * p.target) return false;   // (only where sequences overlap)
-  } else {
-    w.slot = 0;
   }
   return true;
 }
@@ -475,57 +500,69 @@ __global__ void __launch_bounds__(256, 2) paged_few_kernel(const PagedParams p) 
   few_rows<D, F8, RT, 4, 1, OUT_F32>(p, w, w.tile * 16 * RT, w.slot * 16 * RT, lds);
 }
 
-// ---- Row tiles whose keys were cut: out = sum of exp(lse_i - lse) out_i over their live parts.  A workgroup has 1024 / D rows of a tile.
+// ---- Row tiles whose keys were cut: out = sum of exp(lse_i - lse) out_i over their live parts, in their order.
+// A workgroup has a tile and, in turns of gridDim.y, 1024 / D of its rows, D / 4 lanes a row.  What bounds it is latency: the lanes of a row
+// fetch the lse of one part each, and pieces of eight parts are on their way at a time.
 template <int D, bool OUT_F32>
 __global__ void __launch_bounds__(256) paged_fold_kernel(const PagedParams p) {
-  const int part = plan_part(p), size = p.rows.tile;
-  auto cut_tiles = [&](int b) {
-    const Sequence q = sequence(p.seq, b);
-    return parts_of(q.len, part) > 1 ? tiles_of(q.n * p.gq, p.rows) * p.Hkv : 0;
-  };
-  int b, before, base = 0;
-  if (!locate(p.seq.n, (int)blockIdx.x, cut_tiles, b, before)) return;
-  b = uniform(b);
-  for (int b0 = 0; b0 < b; b0 += 64) {
-    const int s = b0 + (int)(threadIdx.x & 63);
-    int n = 0;
-    if (s < b) n = cut_tiles(s) * parts_of(sequence(p.seq, s).len, part);
-    base += __builtin_amdgcn_readlane(wave_scan(n), 63);
-  }
+  constexpr int LANES = D / 4, ROWS = 256 / LANES, AHEAD = 8;
+  const Plan plan = make_plan(p);
+  const int part = plan.part, size = p.rows.tile;
+  auto cut_tiles = [&](const Sequence& q) { return parts_of(q.len, part) > 1 ? tiles_of(q.n * p.gq, p.rows) * p.Hkv : 0; };
+  int b, before;
+  if (!locate(p, plan, (int)blockIdx.x, cut_tiles, b, before)) return;
   Item w;
-  w.q = sequence(p.seq, b);
-  w.rows = w.q.n * p.gq;
-  const int parts = parts_of(w.q.len, part), tiles = tiles_of(w.rows, p.rows), i = (int)blockIdx.x - before;
-  w.hk = i / tiles;
+  w.q = uniform_sequence(p, uniform(b));
+  w.rows = uniform(w.q.n * p.gq);
+  const int base = sum_before(p, plan, uniform(b), [&](const Sequence& q) { return cut_tiles(q) * parts_of(q.len, part); });
+  const int parts = uniform(parts_of(w.q.len, part)), tiles = uniform(tiles_of(w.rows, p.rows)), i = uniform((int)blockIdx.x - before);
+  w.hk = uniform(i / tiles);
   const int row0 = (i - w.hk * tiles) * size, rows = min(size, w.rows - row0);
-  const int n_live = parts_of(row_limit(p, w.q, row0 + rows - 1), part);
-  const int r = (int)blockIdx.y * (1024 / D) + (int)threadIdx.x / (D / 4), c = (int)threadIdx.x % (D / 4);
-  if (n_live == 1 || r >= rows) return;   // one part: written already
+  const int n_live = uniform(parts_of(row_limit(p, w.q, row0 + rows - 1), part));
+  if (n_live == 1) return;   // one part: written already
   if (base < 0 || base + (i + 1) * parts > 2 * p.target) return;   // (only where sequences overlap)
   w.n_parts = 1;   // what follows is stored for good
-  const int64_t slot_row = ((int64_t)base + (int64_t)i * parts) * size + r;
-  const float* const ls = p.part_lse + slot_row;
-  float top = -INFINITY, total = 0.f;
-  bool nan = false;
-  for (int k = 0; k < n_live; k++) {
-    const float x = ls[(int64_t)k * size];
-    nan |= x != x;
-    top = fmaxf(top, x);
-  }
-  f32x4 o = {0.f, 0.f, 0.f, 0.f};
-  for (int k = 0; k < n_live; k++) {
-    const float x = ls[(int64_t)k * size], a = x == -INFINITY ? 0.f : expf(x - top);
-    const f32x4 y = *reinterpret_cast<const f32x4*>(p.part_out + (slot_row + (int64_t)k * size) * D + 4 * c);
-    total += a;
-    if (x != -INFINITY) {
-#pragma unroll
-      for (int e = 0; e < 4; e++) o[e] += a * y[e];
+  const int c = (int)threadIdx.x % LANES;
+  for (int r = (int)blockIdx.y * ROWS + (int)threadIdx.x / LANES; r < rows; r += (int)gridDim.y * ROWS) {
+    const int64_t slot_row = ((int64_t)base + (int64_t)i * parts) * size + r;
+    const float* const ls = p.part_lse + slot_row;
+    const float* const out = p.part_out + slot_row * D + 4 * c;
+    float top = -INFINITY;
+    bool nan = false;
+    for (int k = c; k < n_live; k += LANES) {
+      const float x = ls[(int64_t)k * size];
+      nan |= x != x;
+      top = fmaxf(top, x);
     }
-  }
-  const float inv = total == 0.f ? 0.f : 1.f / total;
 #pragma unroll
-  for (int e = 0; e < 4; e++) o[e] *= inv;
-  store_piece<D, OUT_F32>(p, w, row0, 0, r, c, o, nan ? __builtin_nanf("") : total > 0.f ? top + logf(total) : -INFINITY);
+    for (int d = 1; d < LANES; d *= 2) {
+      top = fmaxf(top, __shfl_xor(top, d));
+      nan |= __shfl_xor((int)nan, d) != 0;
+    }
+    f32x4 o = {0.f, 0.f, 0.f, 0.f};
+    float total = 0.f;
+    for (int k0 = 0; k0 < n_live; k0 += LANES) {
+      float mine = -INFINITY;   // weight of part k0 + c; -inf, in its place, of a part without a visible key, whose result says nothing
+      if (k0 + c < n_live) mine = ls[(int64_t)(k0 + c) * size];
+      mine = mine == -INFINITY ? 0.f : expf(mine - top);
+      for (int k1 = k0; k1 < min(k0 + LANES, n_live); k1 += AHEAD) {
+        f32x4 y[AHEAD];
+#pragma unroll
+        for (int j = 0; j < AHEAD; j++) y[j] = *reinterpret_cast<const f32x4*>(out + (int64_t)min(k1 + j, n_live - 1) * size * D);
+#pragma unroll
+        for (int j = 0; j < AHEAD; j++) {
+          const float a = k1 + j < n_live ? __shfl(mine, k1 - k0 + j, LANES) : 0.f;
+          total += a;
+#pragma unroll
+          for (int e = 0; e < 4; e++) o[e] += a == 0.f ? 0.f : a * y[j][e];
+        }
+      }
+    }
+    const float inv = total == 0.f ? 0.f : 1.f / total;
+#pragma unroll
+    for (int e = 0; e < 4; e++) o[e] *= inv;
+    store_piece<D, OUT_F32>(p, w, row0, 0, r, c, o, nan ? __builtin_nanf("") : total > 0.f ? top + logf(total) : -INFINITY);
+  }
 }
 
 }  // namespace

@@ -40,7 +40,7 @@ hipError_t launch_out(PagedParams& p, const PagedLaunch& l, float* workspace, hi
     if (e != hipSuccess) return e;
     if (p.target == 0) continue;
     const unsigned cut = (unsigned)(c.tiles < p.target ? c.tiles : p.target);   // a cut tile has two parts at least
-    e = launch_kernel(paged_fold_kernel<D, OUT_F32>, dim3(cut, (c.rows.tile * D + 1023) / 1024), dim3(256), 0, stream, p);
+    e = launch_kernel(paged_fold_kernel<D, OUT_F32>, dim3(cut, c.rows.tile == kManyRows ? 8 : c.rows.tile * D / 1024), dim3(256), 0, stream, p);
     if (e != hipSuccess) return e;
   }
   return hipSuccess;

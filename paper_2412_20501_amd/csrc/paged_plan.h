@@ -47,16 +47,16 @@ constexpr Slot slot_of(const Sequences& s, int b, int c) {
 struct RowClass { int tile, over, most; };
 constexpr int tiles_of(int rows, RowClass c) { return rows > c.over && rows <= c.most ? (rows + c.tile - 1) / c.tile : 0; }
 
-// Keys of a part.  work: sum over (sequence, K/V head) of row tiles x keys; tiles: sum of row tiles; target: workgroups that run at once, among which the
-// keys are to be shared out so that they run in one round, 0: keys are not shared out.  A tile's last part is half a part on average, so that many
-// parts fall away.  A multiple of kPartStep, so that parts begin on whole steps of a workgroup.
+// Keys of a part, a multiple of kPartStep, so that parts begin on whole steps of a workgroup.  work: sum over (sequence, K/V head) of row tiles x
+// steps_of(keys); tiles: sum of row tiles; target: workgroups that run at once, among which the keys are to be shared out so that they run
+// in one round, 0: keys are not shared out.  (A tile's last part is half a part on average, so that many parts fall away.)
 // Row tiles whose keys are cut have ceil(keys / part) parts, fewer than 2 keys / part: all of them together fewer than 2 * target.
 constexpr int kPartStep = 128;
+constexpr int steps_of(int keys) { return (keys + kPartStep - 1) / kPartStep; }
 constexpr int part_keys(int64_t work, int64_t tiles, int target, int least) {
-  if (target <= 0) return kPosLimit;   // (as many keys as a sequence has at most)
-  const int64_t n = target - (tiles < target ? tiles : target) / 2;
-  const int64_t keys = (work + n - 1) / n, up = (keys + kPartStep - 1) / kPartStep * kPartStep;
-  return up < least ? least : up > kPosLimit ? kPosLimit : (int)up;
+  if (target <= 0 || work > 0x7fffffff) return kPosLimit;   // (as many keys as a sequence has at most)
+  const unsigned n = (unsigned)(target - (int)(tiles < target ? tiles : target) / 2), steps = ((unsigned)work + n - 1) / n;
+  return steps >= kPosLimit / kPartStep ? kPosLimit : (int)steps * kPartStep < least ? least : (int)steps * kPartStep;
 }
 constexpr int parts_of(int keys, int part) { return keys <= part ? 1 : (keys - 1) / part + 1; }
 

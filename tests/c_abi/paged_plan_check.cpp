@@ -38,7 +38,7 @@ int main() {
           const tr::Sequence q = tr::sequence(s, b);
           EXPECT(q.start >= 0 && q.n >= 0 && q.start + q.n <= tokens && q.len >= 0 && q.len <= max_pages * page_size);
           EXPECT(q.pos >= -(1 << 30) && q.pos < (1 << 30));
-          work += (int64_t)tr::tiles_of(q.n * gq, tile) * q.len;
+          work += (int64_t)tr::tiles_of(q.n * gq, tile) * tr::steps_of(q.len);
           tiles += tr::tiles_of(q.n * gq, tile);
           int before = 0;
           for (int t = 0; t < q.n; t++) {
