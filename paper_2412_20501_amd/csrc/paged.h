@@ -20,7 +20,7 @@ struct CacheCopyParams {
   int64_t page_b, head_b, slot_b;   // of the pages, in bytes
   int64_t scale_sp, scale_sh;
   int heads;        // K/V heads
-  Divisor by_heads;
+  Divisor by_heads;   // of 2 * heads
   int rows;         // read: rows of a sequence's result
   int64_t first;    // read: key of row 0
 };

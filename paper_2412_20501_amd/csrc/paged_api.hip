@@ -157,7 +157,7 @@ void set_pages(tr::CacheCopyParams& p, const tr_tensor* kp, const tr_tensor* vp,
     p.scale_sp = ks->stride_b; p.scale_sh = ks->stride_h;
   }
   p.heads = (int)kp->H;
-  p.by_heads = tr::make_divisor((unsigned)kp->H);
+  p.by_heads = tr::make_divisor((unsigned)kp->H * 2);
 }
 
 }  // namespace
@@ -221,7 +221,7 @@ tr_status tr_cache_read(const tr_tensor* k_pages_, const tr_tensor* v_pages_, co
   SeqViews views;
   if ((st = take_sequences(seqs, k_pages, -1, p.seq, views)) != TR_OK) return st;
   if (k->B != seqs->n_seqs) return fail(TR_ERR_SHAPE, "k has %lld batch entries for %lld sequences", (long long)k->B, (long long)seqs->n_seqs);
-  if (k->B * k->H >= ((int64_t)1 << 31)) return fail(TR_ERR_SHAPE, "too many (sequence, head) pairs");
+  if (k->S * k->H * 2 >= ((int64_t)1 << 31)) return fail(TR_ERR_SHAPE, "too many rows for one call (2 * S * Hkv must stay below 2^31)");
   const tr_tensor* const written[] = {k, v};
   const tr_tensor* const read[] = {k_pages, v_pages, k_scales, v_scales};
   if ((st = check_apart(written, 2, read, 4, views)) != TR_OK) return st;
