@@ -42,7 +42,13 @@ template <int D, bool F8>
 __global__ void __launch_bounds__(kThreads) cache_write_kernel(const CacheCopyParams p) {
   typedef Rows<D> R;
   const int lane = threadIdx.x & 63, c = lane % R::LANES;
-  const WaveRows w = wave_rows(p, (int64_t)blockIdx.x * (kThreads / 64) + (threadIdx.x >> 6));
+  WaveRows w;
+  {
+    const int g = divide(p.by_heads, (int)blockIdx.x), other = (int)blockIdx.x - g * 2 * p.heads;
+    w.rows = (g * (kThreads / 64) + (int)(threadIdx.x >> 6)) * 16;
+    w.is_v = other >= p.heads;
+    w.head = w.is_v ? other - p.heads : other;
+  }
   if (w.rows >= p.seq.tokens) return;
   // the places of its tokens, -1: nowhere
   int64_t to = -1, scale_to = -1;
@@ -158,8 +164,8 @@ __global__ void __launch_bounds__(kThreads) cache_read_kernel(const CacheCopyPar
 }  // namespace
 
 hipError_t launch_cache_write(const CacheCopyParams& p, int D, bool f8, hipStream_t stream) {
-  const int64_t waves = ((int64_t)p.seq.tokens + 15) / 16 * 2 * p.heads;
-  const dim3 grid((unsigned)((waves + kThreads / 64 - 1) / (kThreads / 64))), block(kThreads);
+  const int64_t groups = ((int64_t)p.seq.tokens + kThreads / 4 - 1) / (kThreads / 4) * 2 * p.heads;
+  const dim3 grid((unsigned)groups), block(kThreads);
   if (D == 128) return f8 ? launch_kernel(cache_write_kernel<128, true>, grid, block, 0, stream, p) : launch_kernel(cache_write_kernel<128, false>, grid, block, 0, stream, p);
   return f8 ? launch_kernel(cache_write_kernel<64, true>, grid, block, 0, stream, p) : launch_kernel(cache_write_kernel<64, false>, grid, block, 0, stream, p);
 }

@@ -46,25 +46,27 @@ struct PagedParams {
   int causal, out_f32;
   float scale;
   RowClass rows;   // of the launch
-  int target;      // workgroups among which the keys are shared out, 0: they are not
-  int least_part;  // keys of a part at least
-  float* part_out; // [2 * target slots][rows of a tile][D]
-  float* part_lse; // [2 * target slots][rows of a tile]
+  Share share;     // of the keys among workgroups
+  int slots;       // of the scratch
+  float* part_out; // [slots][rows of a tile][D]
+  float* part_lse; // [slots][rows of a tile]
 };
 
 // How a call is launched: one launch for each class of sequences.
+// Waves a SIMD of the kernel for tiles of 16 * rt rows, which are workgroups (of four waves) a compute unit.
+constexpr int paged_few_waves(int D, int rt) { return D == 128 ? (rt == 1 ? 3 : 2) : rt == 1 ? 4 : 3; }
 constexpr int kManyRows = 256;   // rows of the tiles of sequences with many
 struct PagedLaunch {
   int n;
   struct Part {
     RowClass rows;
-    int target;      // as above, where a workspace is there
+    Share share;     // where a workspace is there
     int64_t tiles;   // of all sequences and K/V heads, at most
-    int64_t floats(int D) const { return (int64_t)target * 2 * rows.tile * (D + 1); }   // of the workspace
+    int64_t floats(int D) const { return (int64_t)share.slots(tiles) * rows.tile * (D + 1); }   // of the workspace
   } part[2];
 };
 PagedLaunch paged_launch(int64_t tokens, int64_t n_seqs, int64_t max_keys, int Hkv, int gq, int D);
-// p without what belongs to a launch (rows, target, scratch); workspace: null or the floats of all parts
+// p without what belongs to a launch (rows, share, scratch); workspace: null or the floats of all parts
 hipError_t launch_paged_attn(PagedParams& p, const PagedLaunch& l, int D, bool f8, float* workspace, hipStream_t stream);
 
 #if defined(__HIPCC__)

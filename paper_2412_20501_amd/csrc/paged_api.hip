@@ -284,7 +284,7 @@ tr_status tr_paged_attn(const tr_tensor* q_, const tr_tensor* k_pages_, const tr
   const int gq = (int)(q->H / k_pages->H), D = (int)q->D;
   const tr::PagedLaunch l = tr::paged_launch(q->S, p.seq.n, (int64_t)p.seq.max_pages * p.seq.page_size, (int)k_pages->H, gq, D);
   for (int i = 0; i < l.n; i++)
-    if (l.part[i].tiles + l.part[i].target >= ((int64_t)1 << 23)) return fail(TR_ERR_SHAPE, "too many workgroups for one launch");   // (of 512 threads, fewer than 2^32 in all)
+    if (l.part[i].tiles + l.part[i].share.at_once * l.part[i].share.rounds >= ((int64_t)1 << 23)) return fail(TR_ERR_SHAPE, "too many workgroups for one launch");   // (of 512 threads, fewer than 2^32 in all)
   const size_t need = tr_paged_attn_workspace_bytes(q, k_pages, seqs->n_seqs, seqs->max_pages);
   if (workspace && need > 0) {
     if ((uintptr_t)workspace % 256) return fail(TR_ERR_WORKSPACE, "workspace must be 256-byte aligned");
@@ -313,7 +313,6 @@ tr_status tr_paged_attn(const tr_tensor* q_, const tr_tensor* k_pages_, const tr
   p.by_gq = tr::make_divisor((unsigned)gq);
   p.causal = causal != 0; p.out_f32 = out->dtype == TR_F32;
   p.scale = scale;
-  p.least_part = 256;
   const hipError_t e = tr::launch_paged_attn(p, l, D, k_scales != nullptr, need > 0 ? (float*)workspace : nullptr, (hipStream_t)hip_stream);
   if (e != hipSuccess) return fail(TR_ERR_HIP, "paged attention launch failed: %s", hipGetErrorString(e));
   return TR_OK;

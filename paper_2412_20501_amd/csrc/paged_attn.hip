@@ -3,6 +3,8 @@
 
 namespace tr {
 
+constexpr int kUnits = 256;   // compute units
+
 #define TR_PAGED(D, F8) extern template hipError_t launch_paged_form<D, F8>(PagedParams&, const PagedLaunch&, float*, hipStream_t);
 TR_PAGED(64, false) TR_PAGED(64, true) TR_PAGED(128, false) TR_PAGED(128, true)
 #undef TR_PAGED
@@ -22,7 +24,9 @@ PagedLaunch paged_launch(int64_t tokens, int64_t n_seqs, int64_t max_keys, int H
   for (int i = 0; i < l.n; i++) {
     PagedLaunch::Part& c = l.part[i];
     c.tiles = most_tiles(tokens, n_seqs, gq, c.rows) * Hkv;
-    c.target = max_keys <= 256 ? 0 : c.rows.tile == kManyRows ? 256 : c.rows.tile == 32 ? 512 : 768;   // as many as run at once
+    // workgroups that run at once: what the registers of each kernel allow a compute unit (paged_few_waves); what an item and the fold cost, measured
+    const Share cut = c.rows.tile == kManyRows ? Share{kUnits, 2, 20, 32} : Share{kUnits * paged_few_waves(D, c.rows.tile / 16), 4, 5, 10};
+    c.share = max_keys <= 2 * kPartStep ? Share{0, 0, 0, 0} : cut;
   }
   return l;
 }

@@ -17,7 +17,7 @@ constexpr float kLog2e = 1.4426950408889634f;
 //
 // The lengths lie in device memory, so the launch does not know them: it has as many workgroups as the shapes allow work items, and every
 // workgroup finds its own item, by sums over the sequences that each of its waves takes for itself (64 sequences a load).  An item
-// is a row tile of a K/V head of a sequence on one part of the keys; parts are as long as makes all items about target (part_keys).
+// is a row tile of a K/V head of a sequence on one part of the keys (part_keys).
 template <int CONTROL, int ROWS>
 __device__ __forceinline__ int from_lane(int x) { return __builtin_amdgcn_update_dpp(0, x, CONTROL, ROWS, 0xf, false); }   // 0 where no lane is
 __device__ __forceinline__ int wave_scan(int x) {   // sum over the lanes up to and including this one
@@ -38,6 +38,14 @@ __device__ __forceinline__ int64_t wave_sum(int64_t x) {
   x = add_from<0x143, 0xc>(add_from<0x142, 0xa>(x));
   return (int64_t)(((uint64_t)(unsigned)__builtin_amdgcn_readlane((int)(x >> 32), 63) << 32) | (unsigned)__builtin_amdgcn_readlane((int)x, 63));
 }
+__device__ __forceinline__ int wave_max(int x) {   // of numbers that are not negative
+  x = max(x, from_lane<0x111, 0xf>(x));
+  x = max(x, from_lane<0x112, 0xf>(x));
+  x = max(x, from_lane<0x114, 0xf>(x));
+  x = max(x, from_lane<0x118, 0xf>(x));
+  x = max(x, from_lane<0x142, 0xa>(x));
+  return __builtin_amdgcn_readlane(max(x, from_lane<0x143, 0xc>(x)), 63);
+}
 __device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
 
 // What the sums are over.  Lane i has sequence i in registers; further ones are loaded when their 64 come up.
@@ -57,17 +65,20 @@ __device__ __forceinline__ Plan make_plan(const PagedParams& p) {
   plan.first = Sequence{0, 0, 0, 0};
   if (lane < plan.n) plan.first = sequence(p.seq, lane);
   int64_t work = 0, tiles = 0;
-  if (p.target > 0) {
+  int longest = 0;
+  if (p.share.at_once > 0) {
     for (int b0 = 0; b0 < plan.n; b0 += 64) {
       const Sequence q = lane_sequence(p, plan, b0);
       const int n = tiles_of(q.n * p.gq, p.rows);
       work += (int64_t)n * steps_of(q.len);
       tiles += n;
+      if (n > 0) longest = max(longest, steps_of(q.len));
     }
     work = wave_sum(work) * p.Hkv;
     tiles = wave_sum(tiles) * p.Hkv;
+    longest = wave_max(longest);
   }
-  plan.part = uniform(part_keys(work, tiles, p.target, p.least_part));
+  plan.part = part_keys(work, tiles, longest, p.share);
   return plan;
 }
 
@@ -146,7 +157,7 @@ __device__ __forceinline__ bool find_item(const PagedParams& p, int id, Item& w)
       return n > 1 ? tiles_of(q.n * p.gq, p.rows) * n * p.Hkv : 0;
     });
     w.slot = base + (w.hk * tiles + w.tile) * parts + w.part;
-    if (w.slot < 0 || w.slot >= 2 * p.target) return false;   // (only where sequences overlap)
+    if (w.slot < 0 || w.slot >= p.slots) return false;   // (only where sequences overlap)
   }
   return true;
 }
@@ -186,19 +197,12 @@ struct Few {
   static constexpr int TILE = 16 * RT, DL = D / 16;              // rows of a tile; d's of a lane in V
   static constexpr int KL = F8 ? D / 64 : D / 32, VW = (F8 ? DL : 2 * DL) / 4;   // 16-byte loads of a K row's quarter, words of V a key
   static constexpr int LDS = W * TILE * (D + 2) * 4;
-  struct Frag {
-    u32x4 k[2][KL];
-    unsigned v[8][VW];
-    unsigned ks[2], vs[2];
-    bool there[2];     // the two groups of 16 keys lie on pages
-  };
 };
 
-template <int D, bool F8, int RT, int W, int DEPTH, bool OUT_F32>
+template <int D, bool F8, int RT, int W, bool OUT_F32>
 __device__ __forceinline__ void few_rows(const PagedParams& p, const Item& w, int row0, int slot_row, char* lds) {
   typedef Few<D, F8, RT, W> F;
   constexpr int STEP = 32 * W;   // keys of a step of the workgroup
-  typedef typename F::Frag Frag;
   constexpr int TILE = F::TILE, DL = F::DL, KL = F::KL, VW = F::VW, QS = D / 32;
   const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), i16 = lane & 15, g = lane >> 4;
   const int rows = min(TILE, w.q.n * p.gq - row0);
@@ -229,49 +233,57 @@ __device__ __forceinline__ void few_rows(const PagedParams& p, const Item& w, in
     at = Slot{-1, 0};
     if (key < w.k1) at = slot_of(p.seq, w.b, key);
   };
-  auto load = [&](Frag& f, int step) __attribute__((always_inline)) {
+  // A stretch's K and V, each renewed as soon as its product has been taken: K of the next stretch is on its way beside this one's weights and second
+  // product, V beside the next one's first.
+  u32x4 kr[2][KL];
+  unsigned vr[8][VW], k_scale[2], v_scale[2];
+  bool k_there[2];     // the two groups of 16 keys lie on pages
+  auto load_k = [&](int step) __attribute__((always_inline)) {
     if ((step & 31) == 0) find_pages(step);
 #pragma unroll
     for (int h = 0; h < 2; h++) {
       const int page = __builtin_amdgcn_readlane(at.page, ((step & 31) << 1) + h), slot = __builtin_amdgcn_readlane(at.slot, ((step & 31) << 1) + h);
-      f.there[h] = page >= 0;
+      k_there[h] = page >= 0;
       if (page >= 0) {
-        const int64_t off = (int64_t)page * p.page_b + (int64_t)slot * p.slot_b;
-        const char* const kp = kb + off;
-        const char* const vp = vb + off;
+        const char* const kp = kb + (int64_t)page * p.page_b + (int64_t)slot * p.slot_b;
 #pragma unroll
-        for (int l = 0; l < KL; l++) f.k[h][l] = *reinterpret_cast<const u32x4*>(kp + k_lane + l * 64);
+        for (int l = 0; l < KL; l++) kr[h][l] = *reinterpret_cast<const u32x4*>(kp + k_lane + l * 64);
+        if constexpr (F8) k_scale[h] = ksb[(int64_t)page * p.scale_sp + slot + i16];
+      } else {
+#pragma unroll
+        for (int l = 0; l < KL; l++) kr[h][l] = u32x4{0, 0, 0, 0};
+        if constexpr (F8) k_scale[h] = 127;
+      }
+    }
+  };
+  auto load_v = [&](int step) __attribute__((always_inline)) {
+#pragma unroll
+    for (int h = 0; h < 2; h++) {
+      const int page = __builtin_amdgcn_readlane(at.page, ((step & 31) << 1) + h), slot = __builtin_amdgcn_readlane(at.slot, ((step & 31) << 1) + h);
+      if (page >= 0) {
+        const char* const vp = vb + (int64_t)page * p.page_b + (int64_t)slot * p.slot_b;
 #pragma unroll
         for (int e = 0; e < 4; e++) {
           const char* const src = vp + v_lane + e * p.slot_b;
           if constexpr (VW == 4) {
             const u32x4 x = *reinterpret_cast<const u32x4*>(src);
 #pragma unroll
-            for (int i = 0; i < 4; i++) f.v[4 * h + e][i] = x[i];
+            for (int i = 0; i < 4; i++) vr[4 * h + e][i] = x[i];
           } else if constexpr (VW == 2) {
             const u32x2 x = *reinterpret_cast<const u32x2*>(src);
-            f.v[4 * h + e][0] = x[0];
-            f.v[4 * h + e][1] = x[1];
+            vr[4 * h + e][0] = x[0];
+            vr[4 * h + e][1] = x[1];
           } else {
-            f.v[4 * h + e][0] = *reinterpret_cast<const unsigned*>(src);
+            vr[4 * h + e][0] = *reinterpret_cast<const unsigned*>(src);
           }
         }
-        if constexpr (F8) {
-          const int64_t s_off = (int64_t)page * p.scale_sp + slot;
-          f.ks[h] = ksb[s_off + i16];
-          f.vs[h] = *reinterpret_cast<const unsigned*>(vsb + s_off + 4 * g);
-        }
+        if constexpr (F8) v_scale[h] = *reinterpret_cast<const unsigned*>(vsb + (int64_t)page * p.scale_sp + slot + 4 * g);
       } else {
-#pragma unroll
-        for (int l = 0; l < KL; l++) f.k[h][l] = u32x4{0, 0, 0, 0};
 #pragma unroll
         for (int e = 0; e < 4; e++)
 #pragma unroll
-          for (int i = 0; i < VW; i++) f.v[4 * h + e][i] = 0;
-        if constexpr (F8) {
-          f.ks[h] = 127;
-          f.vs[h] = 0x7f7f7f7f;
-        }
+          for (int i = 0; i < VW; i++) vr[4 * h + e][i] = 0;
+        if constexpr (F8) v_scale[h] = 0x7f7f7f7f;
       }
     }
   };
@@ -289,9 +301,15 @@ __device__ __forceinline__ void few_rows(const PagedParams& p, const Item& w, in
   }
 
   unsigned taken_out = 0;
-  auto compute = [&](Frag& f, int step) __attribute__((always_inline)) {
+  if (steps > 0) {
+    load_k(0);
+    load_v(0);
+  }
+#pragma unroll 1
+  for (int step = 0; step < steps; step++) {
     const int key0 = w.k0 + step * STEP + wave * 32;
-    const bool edge = key0 + 32 > limit_lo || key0 + 32 > limit_hi || !f.there[0] || !f.there[1];
+    const bool there[2] = {k_there[0], k_there[1]};
+    const bool edge = key0 + 32 > limit_lo || key0 + 32 > limit_hi || !there[0] || !there[1];
     // scores
     f32x4 s[RT][2];
 #pragma unroll
@@ -302,62 +320,28 @@ __device__ __forceinline__ void few_rows(const PagedParams& p, const Item& w, in
       for (int ks = 0; ks < QS; ks++) {
         bf16x8 a;
         if constexpr (F8) {
-          const u32x4 x = f.k[h][ks >> 1];
-          const unsigned lo = x[(ks & 1) * 2], hi = x[(ks & 1) * 2 + 1];
-          a = __builtin_bit_cast(bf16x8, u32x4{f8_pair(lo, false, f.ks[h]), f8_pair(lo, true, f.ks[h]), f8_pair(hi, false, f.ks[h]), f8_pair(hi, true, f.ks[h])});
+          const u32x4 x = kr[h][ks >> 1];
+          const unsigned lo = x[(ks & 1) * 2], hi = x[(ks & 1) * 2 + 1], e = k_scale[h];
+          a = __builtin_bit_cast(bf16x8, u32x4{f8_pair(lo, false, e), f8_pair(lo, true, e), f8_pair(hi, false, e), f8_pair(hi, true, e)});
         } else {
-          a = __builtin_bit_cast(bf16x8, f.k[h][ks]);
+          a = __builtin_bit_cast(bf16x8, kr[h][ks]);
         }
 #pragma unroll
         for (int rt = 0; rt < RT; rt++) s[rt][h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, qf[rt][ks], s[rt][h], 0, 0, 0);
       }
-    // V^T: dl[2 n] and dl[2 n + 1] of key e lie in one word; pairs of keys of one d are what the product takes
-    unsigned vt[DL][4];
-#pragma unroll
-    for (int m = 0; m < 4; m++)
-#pragma unroll
-      for (int n = 0; n < DL / 2; n++) {
-        unsigned a, b;
-        if constexpr (F8) {
-          const int h = m >> 1;
-          a = f8_pair(f.v[2 * m][n >> 1], n & 1, f.vs[h] >> (16 * (m & 1)) & 255);
-          b = f8_pair(f.v[2 * m + 1][n >> 1], n & 1, f.vs[h] >> (16 * (m & 1) + 8) & 255);
-        } else {
-          a = f.v[2 * m][n];
-          b = f.v[2 * m + 1][n];
-        }
-        vt[2 * n][m] = __builtin_amdgcn_perm(b, a, 0x05040100);
-        vt[2 * n + 1][m] = __builtin_amdgcn_perm(b, a, 0x07060302);
-      }
+    if (step + 1 < steps) load_k(step + 1);
     if (edge) {
 #pragma unroll
       for (int h = 0; h < 2; h++)
 #pragma unroll
-        for (int r = 0; r < 4; r++) {
-          const int key = key0 + 16 * h + 4 * g + r;
+        for (int r = 0; r < 4; r++)
 #pragma unroll
           for (int rt = 0; rt < RT; rt++)
-            if (key >= limit[rt] || !f.there[h]) s[rt][h][r] = -INFINITY;
-          // What no row sees takes part in the second product with weight 0: not a value that times 0 is NaN.
-          const unsigned keep = key < limit_hi ? 0xffffffffu : 0u, mask = r & 1 ? keep | 0xffffu : keep | 0xffff0000u;
-#pragma unroll
-          for (int j = 0; j < DL; j++) vt[j][2 * h + (r >> 1)] &= mask;
-        }
-      // A key that some rows see and others do not, with an infinity or NaN in V: taken out of the product, and added below to the rows that see it.
-      if (limit_lo < min(key0 + 32, limit_hi)) {
-        // (in integers: as conditions, 64 masks of lanes spill the scalar registers)
-#pragma unroll
-        for (int j = 0; j < DL; j++)
-#pragma unroll
-          for (int m = 0; m < 4; m++) {
-            const unsigned nf = ((vt[j][m] & 0x7f807f80u) + 0x00800080u) & 0x80008000u;   // a half's top bit: its exponent is all ones
-            taken_out |= nf;
-            vt[j][m] &= ~(nf | (nf - (nf >> 15)));
-          }
-      }
+            if (key0 + 16 * h + 4 * g + r >= limit[rt] || !there[h]) s[rt][h][r] = -INFINITY;
     }
     // Weights relative to a reference that is not the running maximum: any gives the same result, and one that the
     // first scores set is replaced only where a sum of weights passes 2^80 (fp32 and bf16 hold them as well as small ones).
+    bf16x8 pf[RT];
 #pragma unroll
     for (int rt = 0; rt < RT; rt++) {
       float e[8], sum = 0.f;
@@ -390,33 +374,57 @@ __device__ __forceinline__ void few_rows(const PagedParams& p, const Item& w, in
           sum += e[i];
         }
       }
-      l_run[rt] += sum;
-      bf16x8 pf;   // (the sums take the weights as they are: rounded ones would put 2^-9 of error into lse)
+      l_run[rt] += sum;   // (the sums take the weights as they are: rounded ones would put 2^-9 of error into lse)
 #pragma unroll
-      for (int i = 0; i < 8; i++) pf[i] = (__bf16)e[i];
+      for (int i = 0; i < 8; i++) pf[rt][i] = (__bf16)e[i];
+    }
+    // What no row sees takes part in the second product with weight 0: not a value that times 0 is NaN.
+    if (edge) {
 #pragma unroll
-      for (int j = 0; j < DL; j++)
-        acc[rt][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, u32x4{vt[j][0], vt[j][1], vt[j][2], vt[j][3]}), pf, acc[rt][j], 0, 0, 0);
+      for (int e = 0; e < 8; e++) {
+        const bool seen = key0 + 16 * (e >> 2) + 4 * g + (e & 3) < limit_hi;
+#pragma unroll
+        for (int n = 0; n < VW; n++) vr[e][n] = seen ? vr[e][n] : 0;
+        if (F8) v_scale[e >> 2] = seen ? v_scale[e >> 2] : v_scale[e >> 2] & ~(128u << 8 * (e & 3));   // (no scale of NaN)
+      }
     }
-  };
-
-  if constexpr (DEPTH == 2) {
-    Frag fa, fb;
-    if (steps > 0) load(fa, 0);
-    for (int step = 0; step < steps; step += 2) {
-      if (step + 1 < steps) load(fb, step + 1);
-      compute(fa, step);
-      if (step + 1 >= steps) break;
-      if (step + 2 < steps) load(fa, step + 2);
-      compute(fb, step + 1);
+    const bool partly = limit_lo < min(key0 + 32, limit_hi);   // some rows see what others do not
+    // V^T: d's 2 n and 2 n + 1 of a key lie in one word; pairs of keys of one d are what the product takes
+#pragma unroll
+    for (int n = 0; n < DL / 2; n++) {
+      unsigned vt[2][4];
+#pragma unroll
+      for (int m = 0; m < 4; m++) {
+        unsigned a, b;
+        if constexpr (F8) {
+          const int h = m >> 1;
+          a = f8_pair(vr[2 * m][n >> 1], n & 1, v_scale[h] >> (16 * (m & 1)) & 255);
+          b = f8_pair(vr[2 * m + 1][n >> 1], n & 1, v_scale[h] >> (16 * (m & 1) + 8) & 255);
+        } else {
+          a = vr[2 * m][n];
+          b = vr[2 * m + 1][n];
+        }
+        vt[0][m] = __builtin_amdgcn_perm(b, a, 0x05040100);
+        vt[1][m] = __builtin_amdgcn_perm(b, a, 0x07060302);
+      }
+      // A key that some rows see and others do not, with an infinity or NaN in V: taken out of the product, and added below to the rows that see it.
+      if (partly) {
+#pragma unroll
+        for (int j = 0; j < 2; j++)
+#pragma unroll
+          for (int m = 0; m < 4; m++) {
+            const unsigned nf = ((vt[j][m] & 0x7f807f80u) + 0x00800080u) & 0x80008000u;   // a half's top bit: its exponent is all ones (as conditions, they spill the scalar registers)
+            taken_out |= nf;
+            vt[j][m] &= ~(nf | (nf - (nf >> 15)));
+          }
+      }
+#pragma unroll
+      for (int j = 0; j < 2; j++)
+#pragma unroll
+        for (int rt = 0; rt < RT; rt++)
+          acc[rt][2 * n + j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, u32x4{vt[j][0], vt[j][1], vt[j][2], vt[j][3]}), pf[rt], acc[rt][2 * n + j], 0, 0, 0);
     }
-  } else {
-    Frag f;
-#pragma unroll 1
-    for (int step = 0; step < steps; step++) {
-      load(f, step);
-      compute(f, step);
-    }
+    if (step + 1 < steps) load_v(step + 1);
   }
   if (__any(taken_out != 0)) {   // (the rows they reach are infinite or NaN whatever else adds up)
 #pragma unroll 1
@@ -493,11 +501,11 @@ __device__ __forceinline__ void few_rows(const PagedParams& p, const Item& w, in
 }
 
 template <int D, bool F8, int RT, bool OUT_F32>
-__global__ void __launch_bounds__(256, 2) paged_few_kernel(const PagedParams p) {
+__global__ void __launch_bounds__(256, paged_few_waves(D, RT)) paged_few_kernel(const PagedParams p) {
   extern __shared__ __attribute__((aligned(1024))) char lds[];
   Item w;
   if (!find_item(p, (int)blockIdx.x, w)) return;
-  few_rows<D, F8, RT, 4, 1, OUT_F32>(p, w, w.tile * 16 * RT, w.slot * 16 * RT, lds);
+  few_rows<D, F8, RT, 4, OUT_F32>(p, w, w.tile * 16 * RT, w.slot * 16 * RT, lds);
 }
 
 // ---- Row tiles whose keys were cut: out = sum of exp(lse_i - lse) out_i over their live parts, in their order.
@@ -520,7 +528,7 @@ __global__ void __launch_bounds__(256) paged_fold_kernel(const PagedParams p) {
   const int row0 = (i - w.hk * tiles) * size, rows = min(size, w.rows - row0);
   const int n_live = uniform(parts_of(row_limit(p, w.q, row0 + rows - 1), part));
   if (n_live == 1) return;   // one part: written already
-  if (base < 0 || base + (i + 1) * parts > 2 * p.target) return;   // (only where sequences overlap)
+  if (base < 0 || base + (i + 1) * parts > p.slots) return;   // (only where sequences overlap)
   w.n_parts = 1;   // what follows is stored for good
   const int c = (int)threadIdx.x % LANES;
   for (int r = (int)blockIdx.y * ROWS + (int)threadIdx.x / LANES; r < rows; r += (int)gridDim.y * ROWS) {

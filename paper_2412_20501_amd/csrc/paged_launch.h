@@ -28,18 +28,20 @@ hipError_t launch_out(PagedParams& p, const PagedLaunch& l, float* workspace, hi
   for (int i = 0; i < l.n; i++) {
     const PagedLaunch::Part& c = l.part[i];
     p.rows = c.rows;
-    p.target = workspace ? c.target : 0;
+    p.share = workspace ? c.share : Share{0, 0, 0, 0};
+    p.slots = p.share.slots(c.tiles);
     p.part_out = workspace;
-    p.part_lse = workspace ? workspace + (int64_t)2 * c.target * c.rows.tile * D : nullptr;
+    p.part_lse = workspace ? workspace + (int64_t)p.slots * c.rows.tile * D : nullptr;
     if (workspace) workspace += c.floats(D);
-    const dim3 items((unsigned)((c.tiles + p.target + 7) / 8 * 8));   // an eighth of the items for every XCD, rounded up
+    const int64_t most = (int64_t)p.share.at_once * p.share.rounds;   // items that cutting adds
+    const dim3 items((unsigned)((c.tiles + most + 7) / 8 * 8));       // an eighth of the items for every XCD, rounded up
     hipError_t e;
     if (c.rows.tile == kManyRows) e = launch_lds(paged_many_kernel<D, F8, OUT_F32>, raised[0], items, dim3(512), Tile<D>::LDS, stream, p);
     else if (c.rows.tile == 32) e = launch_lds(paged_few_kernel<D, F8, 2, OUT_F32>, raised[1], items, dim3(256), Few<D, F8, 2, 4>::LDS, stream, p);
     else e = launch_lds(paged_few_kernel<D, F8, 1, OUT_F32>, raised[2], items, dim3(256), Few<D, F8, 1, 4>::LDS, stream, p);
     if (e != hipSuccess) return e;
-    if (p.target == 0) continue;
-    const unsigned cut = (unsigned)(c.tiles < p.target ? c.tiles : p.target);   // a cut tile has two parts at least
+    if (most == 0) continue;
+    const unsigned cut = (unsigned)(c.tiles < most ? c.tiles : most);   // tiles that are cut, at most
     e = launch_kernel(paged_fold_kernel<D, OUT_F32>, dim3(cut, c.rows.tile == kManyRows ? 8 : c.rows.tile * D / 1024), dim3(256), 0, stream, p);
     if (e != hipSuccess) return e;
   }

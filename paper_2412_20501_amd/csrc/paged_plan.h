@@ -47,16 +47,39 @@ constexpr Slot slot_of(const Sequences& s, int b, int c) {
 struct RowClass { int tile, over, most; };
 constexpr int tiles_of(int rows, RowClass c) { return rows > c.over && rows <= c.most ? (rows + c.tile - 1) / c.tile : 0; }
 
-// Keys of a part, a multiple of kPartStep, so that parts begin on whole steps of a workgroup.  work: sum over (sequence, K/V head) of row tiles x
-// steps_of(keys); tiles: sum of row tiles; target: workgroups that run at once, among which the keys are to be shared out so that they run
-// in one round, 0: keys are not shared out.  (A tile's last part is half a part on average, so that many parts fall away.)
-// Row tiles whose keys are cut have ceil(keys / part) parts, fewer than 2 keys / part: all of them together fewer than 2 * target.
-constexpr int kPartStep = 128;
+// Keys of a part, a multiple of kPartStep, so that parts begin on whole steps of a workgroup.
+//   work     sum over (sequence, K/V head) of row tiles x steps_of(keys); tiles: of row tiles; longest: largest steps_of(keys)
+//   share    how the keys may be shared out
+// Uncut, the row tiles take as long as rounds of the longest or, where they are of different lengths, an even share and the longest behind it.  Cut for r rounds of
+// `at_once` workgroups a tile's last part is half a part on average, so that parts are work / (r at_once - tiles / 2).  What is estimated to end first is
+// taken, costs beside the keys' being those of an item and of the fold, in sixteenths of a step.
+// Tiles that are cut have fewer than steps / part + 1 parts: all of them together at most share.slots(tiles).
+constexpr int kPartStep = 128, kMostRounds = 4;
 constexpr int steps_of(int keys) { return (keys + kPartStep - 1) / kPartStep; }
-constexpr int part_keys(int64_t work, int64_t tiles, int target, int least) {
-  if (target <= 0 || work > 0x7fffffff) return kPosLimit;   // (as many keys as a sequence has at most)
-  const unsigned n = (unsigned)(target - (int)(tiles < target ? tiles : target) / 2), steps = ((unsigned)work + n - 1) / n;
-  return steps >= kPosLimit / kPartStep ? kPosLimit : (int)steps * kPartStep < least ? least : (int)steps * kPartStep;
+struct Share {
+  int at_once;      // workgroups that run at once, 0: keys are not shared out
+  int rounds;       // at most
+  int item, fold;   // costs
+  constexpr int slots(int64_t tiles) const { return at_once * rounds + (int)(tiles < at_once * rounds ? tiles : at_once * rounds); }
+};
+constexpr int part_keys(int64_t work, int64_t tiles, int longest, Share share) {
+  if (share.at_once <= 0 || work <= 0 || work > 0x3ffffff) return kPosLimit;   // (as many keys as a sequence has at most)
+  const unsigned w = (unsigned)work, at_once = (unsigned)share.at_once, n_tiles = (unsigned)(tiles < 0x3ffffff ? tiles : 0x3ffffff);
+  const unsigned full = (n_tiles + at_once - 1) / at_once;
+  const unsigned even = 16 * w / at_once + 16 * (unsigned)longest, rounds = full < 0x3ff && longest < 0x3fff ? 16 * full * (unsigned)longest : even;
+  unsigned best = (even < rounds ? even : rounds) + (unsigned)share.item * (full < 64 ? full : 64);
+  int part = kPosLimit;
+  for (int r = 1; r <= share.rounds; r++) {
+    const unsigned all = (unsigned)r * at_once;
+    if (all <= n_tiles / 2) continue;
+    const unsigned n = all - n_tiles / 2, steps = (w + n - 1) / n < 2 ? 2 : (w + n - 1) / n;
+    const unsigned time = (unsigned)r * (16 * steps + (unsigned)share.item) + (unsigned)share.fold;
+    if (steps < (unsigned)longest && time < best) {
+      best = time;
+      part = (int)steps * kPartStep;
+    }
+  }
+  return part;
 }
 constexpr int parts_of(int keys, int part) { return keys <= part ? 1 : (keys - 1) / part + 1; }
 

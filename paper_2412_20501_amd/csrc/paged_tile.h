@@ -494,7 +494,7 @@ __global__ void __launch_bounds__(512, 2) paged_many_kernel(const PagedParams p)
   if (tile_rows<D, F8, OUT_F32>(p, w, slot_row, lds)) return;
   for (int r = 0; r < n; r += 16) {
     __syncthreads();
-    few_rows<D, F8, 1, 8, 1, OUT_F32>(p, w, row0 + r, slot_row + r, lds);
+    few_rows<D, F8, 1, 8, OUT_F32>(p, w, row0 + r, slot_row + r, lds);
   }
 }
 

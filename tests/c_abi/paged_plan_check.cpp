@@ -32,14 +32,17 @@ int main() {
     s.table_stride = max_pages; s.n = n; s.max_pages = max_pages; s.tokens = tokens; s.n_pages = n_pages; s.page_size = page_size;
     s.by_page = tr::make_divisor((unsigned)page_size);
     for (tr::RowClass tile : {tr::RowClass{16, 0, 1 << 30}, tr::RowClass{32, 0, 1 << 30}, tr::RowClass{32, 0, 32}, tr::RowClass{256, 32, 1 << 30}})
-      for (int target : {0, 8, 512}) {
+      for (int at_once : {0, 8, 512}) {
+        const tr::Share share = {at_once, 1 + round % 4, 5 * (round % 7), 10 * (round % 5)};
         int64_t work = 0, tiles = 0;
+        int longest = 0;
         for (int b = 0; b < n; b++) {
           const tr::Sequence q = tr::sequence(s, b);
           EXPECT(q.start >= 0 && q.n >= 0 && q.start + q.n <= tokens && q.len >= 0 && q.len <= max_pages * page_size);
           EXPECT(q.pos >= -(1 << 30) && q.pos < (1 << 30));
           work += (int64_t)tr::tiles_of(q.n * gq, tile) * tr::steps_of(q.len);
           tiles += tr::tiles_of(q.n * gq, tile);
+          if (tr::tiles_of(q.n * gq, tile) > 0 && tr::steps_of(q.len) > longest) longest = tr::steps_of(q.len);
           int before = 0;
           for (int t = 0; t < q.n; t++) {
             const int v = tr::visible(q, t, causal);
@@ -53,8 +56,8 @@ int main() {
           }
         }
         if (!wild) EXPECT(tiles <= tr::most_tiles(tokens, n, gq, tile));
-        const int part = tr::part_keys(work * Hkv, tiles * Hkv, target, 256);
-        EXPECT(part > 0 && (target == 0 || part % tr::kPartStep == 0));
+        const int part = tr::part_keys(work * Hkv, tiles * Hkv, longest, share);
+        EXPECT(part > 0 && (part == tr::kPosLimit || part % tr::kPartStep == 0) && (at_once > 0 || part == tr::kPosLimit));
         int64_t items = 0, slots = 0;
         for (int b = 0; b < n; b++) {
           const tr::Sequence q = tr::sequence(s, b);
@@ -63,8 +66,8 @@ int main() {
           items += mine;
           if (parts > 1) slots += mine;
         }
-        EXPECT(slots <= 2 * target);
-        EXPECT(items <= tiles * Hkv + target);
+        EXPECT(slots <= share.slots(tiles * Hkv));
+        EXPECT(items <= tiles * Hkv + at_once * share.rounds);
       }
   }
   printf("paged plan ok\n");
