@@ -275,8 +275,8 @@ def tr_ring_attn_noalloc(q, k, v, n_chunks, causal, out, lse, scale=0.0, stream=
 
 
 def _shape(t: torch.Tensor) -> TrTensor:
-    """Descriptor of sizes alone, for questions about them."""
-    return TrTensor(None, 0, *t.shape, 0, 0, 0)
+    """Descriptor of type and sizes alone, for questions about them."""
+    return TrTensor(None, TR_F8E4M3 if t.dtype == torch.float8_e4m3fn else _DTYPES.get(t.dtype, -1), *t.shape, 0, 0, 0)
 
 
 def tr_cache_write(k, v, k_pages, v_pages, page_table, kv_len, q_start, k_scales=None, v_scales=None, q_pos=None, stream=None):

@@ -241,7 +241,7 @@ size_t tr_paged_attn_workspace_bytes(const tr_tensor* q, const tr_tensor* k_page
   if (!q || !k_pages || q->S < 0 || q->S > kMaxKeys || q->H < 0 || q->H > INT32_MAX || k_pages->H < 1 || q->H % k_pages->H || (q->D != 64 && q->D != 128)) return 0;
   if (k_pages->S < 16 || n_seqs < 0 || max_pages < 0 || max_pages > kMaxKeys / k_pages->S || n_seqs > (1 << 24) || q->S * q->H >= ((int64_t)1 << 31)) return 0;
   if (q->S == 0 || q->H == 0 || n_seqs == 0) return 0;
-  const tr::PagedLaunch l = tr::paged_launch(q->S, n_seqs, max_pages * k_pages->S, (int)k_pages->H, (int)(q->H / k_pages->H), (int)q->D);
+  const tr::PagedLaunch l = tr::paged_launch(q->S, n_seqs, max_pages * k_pages->S, (int)k_pages->H, (int)(q->H / k_pages->H), (int)q->D, k_pages->dtype == TR_F8E4M3);
   int64_t floats = 0;
   for (int i = 0; i < l.n; i++) floats += l.part[i].floats((int)q->D);
   return (size_t)floats * 4;
@@ -282,9 +282,9 @@ tr_status tr_paged_attn(const tr_tensor* q_, const tr_tensor* k_pages_, const tr
   if (q->H == 0 || q->S == 0 || p.seq.n == 0) return TR_OK;
 
   const int gq = (int)(q->H / k_pages->H), D = (int)q->D;
-  const tr::PagedLaunch l = tr::paged_launch(q->S, p.seq.n, (int64_t)p.seq.max_pages * p.seq.page_size, (int)k_pages->H, gq, D);
+  const tr::PagedLaunch l = tr::paged_launch(q->S, p.seq.n, (int64_t)p.seq.max_pages * p.seq.page_size, (int)k_pages->H, gq, D, k_scales != nullptr);
   for (int i = 0; i < l.n; i++)
-    if (l.part[i].tiles + l.part[i].share.at_once * l.part[i].share.rounds >= ((int64_t)1 << 23)) return fail(TR_ERR_SHAPE, "too many workgroups for one launch");   // (of 512 threads, fewer than 2^32 in all)
+    if (l.part[i].tiles + l.part[i].share.most() >= ((int64_t)1 << 23)) return fail(TR_ERR_SHAPE, "too many workgroups for one launch");   // (of 512 threads, fewer than 2^32 in all)
   const size_t need = tr_paged_attn_workspace_bytes(q, k_pages, seqs->n_seqs, seqs->max_pages);
   if (workspace && need > 0) {
     if ((uintptr_t)workspace % 256) return fail(TR_ERR_WORKSPACE, "workspace must be 256-byte aligned");

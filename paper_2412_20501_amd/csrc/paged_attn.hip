@@ -3,8 +3,6 @@
 
 namespace tr {
 
-constexpr int kUnits = 256;   // compute units
-
 #define TR_PAGED(D, F8) extern template hipError_t launch_paged_form<D, F8>(PagedParams&, const PagedLaunch&, float*, hipStream_t);
 TR_PAGED(64, false) TR_PAGED(64, true) TR_PAGED(128, false) TR_PAGED(128, true)
 #undef TR_PAGED
@@ -12,7 +10,7 @@ TR_PAGED(64, false) TR_PAGED(64, true) TR_PAGED(128, false) TR_PAGED(128, true)
 // The launches of a call.  The lengths are not known here, so it goes by the average rows of a sequence and K/V head: up to 32, sequences are taken to be
 // of single tokens and drafts, and workgroups of 16 or 32 rows serve them all; a lone sequence of more is one of many rows; several are a mixture,
 // a launch for either kind.
-PagedLaunch paged_launch(int64_t tokens, int64_t n_seqs, int64_t max_keys, int Hkv, int gq, int D) {
+PagedLaunch paged_launch(int64_t tokens, int64_t n_seqs, int64_t max_keys, int Hkv, int gq, int D, bool f8) {
   PagedLaunch l;
   const int64_t rows = tokens * gq;
   constexpr int any = 0x7fffffff;
@@ -24,9 +22,13 @@ PagedLaunch paged_launch(int64_t tokens, int64_t n_seqs, int64_t max_keys, int H
   for (int i = 0; i < l.n; i++) {
     PagedLaunch::Part& c = l.part[i];
     c.tiles = most_tiles(tokens, n_seqs, gq, c.rows) * Hkv;
-    // workgroups that run at once: what the registers of each kernel allow a compute unit (paged_few_waves); what an item and the fold cost, measured
-    const Share cut = c.rows.tile == kManyRows ? Share{kUnits, 2, 20, 32} : Share{kUnits * paged_few_waves(D, c.rows.tile / 16), 4, 5, 10};
-    c.share = max_keys <= 2 * kPartStep ? Share{0, 0, 0, 0} : cut;
+    // Workgroups that the registers of each kernel allow a compute unit; what an item, the fold and its parts cost, measured.  More rounds than one only
+    // for launches that may have more row tiles than a part of one round.
+    const int per_unit = c.rows.tile == kManyRows ? 1 : paged_few_waves(D, f8, c.rows.tile / 16);
+    const int rounds = 2 * c.tiles <= kUnits * per_unit ? 1 : c.rows.tile == kManyRows ? 2 : 4;
+    const Share cut = c.rows.tile == kManyRows ? Share{1, rounds, 20, 32, 2} : Share{per_unit, rounds, 36, 64, 2};
+    c.parts = std::max<int64_t>(1, (max_keys + 2 * kPartStep - 1) / (2 * kPartStep));
+    c.share = c.parts == 1 ? Share{0, 0, 0, 0, 0} : cut;
   }
   return l;
 }

@@ -66,7 +66,7 @@ __device__ __forceinline__ Plan make_plan(const PagedParams& p) {
   if (lane < plan.n) plan.first = sequence(p.seq, lane);
   int64_t work = 0, tiles = 0;
   int longest = 0;
-  if (p.share.at_once > 0) {
+  if (p.share.most_per_unit > 0) {
     for (int b0 = 0; b0 < plan.n; b0 += 64) {
       const Sequence q = lane_sequence(p, plan, b0);
       const int n = tiles_of(q.n * p.gq, p.rows);
@@ -78,7 +78,7 @@ __device__ __forceinline__ Plan make_plan(const PagedParams& p) {
     tiles = wave_sum(tiles) * p.Hkv;
     longest = wave_max(longest);
   }
-  plan.part = part_keys(work, tiles, longest, p.share);
+  plan.part = uniform(part_keys(work, tiles, longest, p.share));
   return plan;
 }
 
@@ -162,6 +162,9 @@ __device__ __forceinline__ bool find_item(const PagedParams& p, int id, Item& w)
   return true;
 }
 
+// Of two bf16: the top bit of each half whose exponent is all ones.  (In integers: as conditions, many of them spill the scalar registers.)
+__device__ __forceinline__ unsigned not_finite(unsigned pair) { return ((pair & 0x7f807f80u) + 0x00800080u) & 0x80008000u; }
+
 // 16 bytes (fp32) of a row's result, piece c of row row0 + r of the item, to where they belong; with piece 0 the row's lse (NaN: a weight was one).
 template <int D, bool OUT_F32>
 __device__ __forceinline__ void store_piece(const PagedParams& p, const Item& w, int row0, int slot_row, int r, int c, f32x4 o, float lse) {
@@ -199,7 +202,7 @@ struct Few {
   static constexpr int LDS = W * TILE * (D + 2) * 4;
 };
 
-template <int D, bool F8, int RT, int W, bool OUT_F32>
+template <int D, bool F8, int RT, int W, bool AHEAD, bool OUT_F32>   // AHEAD: the next stretch is on its way beside the products (it takes registers)
 __device__ __forceinline__ void few_rows(const PagedParams& p, const Item& w, int row0, int slot_row, char* lds) {
   typedef Few<D, F8, RT, W> F;
   constexpr int STEP = 32 * W;   // keys of a step of the workgroup
@@ -301,13 +304,14 @@ __device__ __forceinline__ void few_rows(const PagedParams& p, const Item& w, in
   }
 
   unsigned taken_out = 0;
-  if (steps > 0) {
+  if (AHEAD && steps > 0) {
     load_k(0);
     load_v(0);
   }
 #pragma unroll 1
   for (int step = 0; step < steps; step++) {
     const int key0 = w.k0 + step * STEP + wave * 32;
+    if (!AHEAD) load_k(step);
     const bool there[2] = {k_there[0], k_there[1]};
     const bool edge = key0 + 32 > limit_lo || key0 + 32 > limit_hi || !there[0] || !there[1];
     // scores
@@ -329,7 +333,7 @@ __device__ __forceinline__ void few_rows(const PagedParams& p, const Item& w, in
 #pragma unroll
         for (int rt = 0; rt < RT; rt++) s[rt][h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, qf[rt][ks], s[rt][h], 0, 0, 0);
       }
-    if (step + 1 < steps) load_k(step + 1);
+    if (AHEAD && step + 1 < steps) load_k(step + 1);
     if (edge) {
 #pragma unroll
       for (int h = 0; h < 2; h++)
@@ -378,6 +382,7 @@ __device__ __forceinline__ void few_rows(const PagedParams& p, const Item& w, in
 #pragma unroll
       for (int i = 0; i < 8; i++) pf[rt][i] = (__bf16)e[i];
     }
+    if (!AHEAD) load_v(step);
     // What no row sees takes part in the second product with weight 0: not a value that times 0 is NaN.
     if (edge) {
 #pragma unroll
@@ -388,7 +393,28 @@ __device__ __forceinline__ void few_rows(const PagedParams& p, const Item& w, in
         if (F8) v_scale[e >> 2] = seen ? v_scale[e >> 2] : v_scale[e >> 2] & ~(128u << 8 * (e & 3));   // (no scale of NaN)
       }
     }
-    const bool partly = limit_lo < min(key0 + 32, limit_hi);   // some rows see what others do not
+    // A key that some rows see and others do not, with an infinity or NaN in V: taken out of the product, and added below to the rows that see it.
+    if (limit_lo < min(key0 + 32, limit_hi)) {
+#pragma unroll
+      for (int e = 0; e < 8; e++) {
+#pragma unroll
+        for (int n = 0; n < VW; n++) {
+          if constexpr (F8) {
+#pragma unroll
+            for (int u = 0; u < 2; u++) {
+              const unsigned nf = not_finite(f8_pair(vr[e][n], u, v_scale[e >> 2] >> (8 * (e & 3)) & 255));
+              taken_out |= nf;
+              vr[e][n] &= ~(((nf >> 15 & 1) * 0xffu | (nf >> 31) * 0xff00u) << 16 * u);
+            }
+          } else {
+            const unsigned nf = not_finite(vr[e][n]);
+            taken_out |= nf;
+            vr[e][n] &= ~(nf | (nf - (nf >> 15)));
+          }
+        }
+        if (F8 && (v_scale[e >> 2] >> (8 * (e & 3)) & 255) == 255) v_scale[e >> 2] &= ~(128u << 8 * (e & 3));   // (all of the row is out)
+      }
+    }
     // V^T: d's 2 n and 2 n + 1 of a key lie in one word; pairs of keys of one d are what the product takes
 #pragma unroll
     for (int n = 0; n < DL / 2; n++) {
@@ -407,24 +433,13 @@ __device__ __forceinline__ void few_rows(const PagedParams& p, const Item& w, in
         vt[0][m] = __builtin_amdgcn_perm(b, a, 0x05040100);
         vt[1][m] = __builtin_amdgcn_perm(b, a, 0x07060302);
       }
-      // A key that some rows see and others do not, with an infinity or NaN in V: taken out of the product, and added below to the rows that see it.
-      if (partly) {
-#pragma unroll
-        for (int j = 0; j < 2; j++)
-#pragma unroll
-          for (int m = 0; m < 4; m++) {
-            const unsigned nf = ((vt[j][m] & 0x7f807f80u) + 0x00800080u) & 0x80008000u;   // a half's top bit: its exponent is all ones (as conditions, they spill the scalar registers)
-            taken_out |= nf;
-            vt[j][m] &= ~(nf | (nf - (nf >> 15)));
-          }
-      }
 #pragma unroll
       for (int j = 0; j < 2; j++)
 #pragma unroll
         for (int rt = 0; rt < RT; rt++)
           acc[rt][2 * n + j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, u32x4{vt[j][0], vt[j][1], vt[j][2], vt[j][3]}), pf[rt], acc[rt][2 * n + j], 0, 0, 0);
     }
-    if (step + 1 < steps) load_v(step + 1);
+    if (AHEAD && step + 1 < steps) load_v(step + 1);
   }
   if (__any(taken_out != 0)) {   // (the rows they reach are infinite or NaN whatever else adds up)
 #pragma unroll 1
@@ -501,11 +516,11 @@ __device__ __forceinline__ void few_rows(const PagedParams& p, const Item& w, in
 }
 
 template <int D, bool F8, int RT, bool OUT_F32>
-__global__ void __launch_bounds__(256, paged_few_waves(D, RT)) paged_few_kernel(const PagedParams p) {
+__global__ void __launch_bounds__(256, paged_few_waves(D, F8, RT)) paged_few_kernel(const PagedParams p) {
   extern __shared__ __attribute__((aligned(1024))) char lds[];
   Item w;
   if (!find_item(p, (int)blockIdx.x, w)) return;
-  few_rows<D, F8, RT, 4, OUT_F32>(p, w, w.tile * 16 * RT, w.slot * 16 * RT, lds);
+  few_rows<D, F8, RT, 4, true, OUT_F32>(p, w, w.tile * 16 * RT, w.slot * 16 * RT, lds);
 }
 
 // ---- Row tiles whose keys were cut: out = sum of exp(lse_i - lse) out_i over their live parts, in their order.

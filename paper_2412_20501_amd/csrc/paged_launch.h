@@ -1,5 +1,6 @@
 // Launches of one head dim and type of the pages (one .hip each, so that they compile side by side).
 #pragma once
+#include <algorithm>
 #include <atomic>
 
 #include "paged_tile.h"
@@ -28,20 +29,21 @@ hipError_t launch_out(PagedParams& p, const PagedLaunch& l, float* workspace, hi
   for (int i = 0; i < l.n; i++) {
     const PagedLaunch::Part& c = l.part[i];
     p.rows = c.rows;
-    p.share = workspace ? c.share : Share{0, 0, 0, 0};
+    p.share = workspace ? c.share : Share{0, 0, 0, 0, 0};
     p.slots = p.share.slots(c.tiles);
     p.part_out = workspace;
     p.part_lse = workspace ? workspace + (int64_t)p.slots * c.rows.tile * D : nullptr;
     if (workspace) workspace += c.floats(D);
-    const int64_t most = (int64_t)p.share.at_once * p.share.rounds;   // items that cutting adds
-    const dim3 items((unsigned)((c.tiles + most + 7) / 8 * 8));       // an eighth of the items for every XCD, rounded up
+    // Workgroups beyond those that have an item cost a microsecond for every four hundred.  (An eighth of the items for every XCD, rounded up.)
+    const int64_t most = std::min(c.tiles + p.share.most(), c.tiles * (p.share.most() > 0 ? c.parts : 1));
+    const dim3 items((unsigned)((most + 7) / 8 * 8));
     hipError_t e;
     if (c.rows.tile == kManyRows) e = launch_lds(paged_many_kernel<D, F8, OUT_F32>, raised[0], items, dim3(512), Tile<D>::LDS, stream, p);
     else if (c.rows.tile == 32) e = launch_lds(paged_few_kernel<D, F8, 2, OUT_F32>, raised[1], items, dim3(256), Few<D, F8, 2, 4>::LDS, stream, p);
     else e = launch_lds(paged_few_kernel<D, F8, 1, OUT_F32>, raised[2], items, dim3(256), Few<D, F8, 1, 4>::LDS, stream, p);
     if (e != hipSuccess) return e;
-    if (most == 0) continue;
-    const unsigned cut = (unsigned)(c.tiles < most ? c.tiles : most);   // tiles that are cut, at most
+    if (p.share.most() == 0) continue;
+    const unsigned cut = (unsigned)std::min<int64_t>(c.tiles, p.share.most());   // tiles that are cut, at most
     e = launch_kernel(paged_fold_kernel<D, OUT_F32>, dim3(cut, c.rows.tile == kManyRows ? 8 : c.rows.tile * D / 1024), dim3(256), 0, stream, p);
     if (e != hipSuccess) return e;
   }

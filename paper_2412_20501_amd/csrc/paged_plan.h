@@ -50,33 +50,46 @@ constexpr int tiles_of(int rows, RowClass c) { return rows > c.over && rows <= c
 // Keys of a part, a multiple of kPartStep, so that parts begin on whole steps of a workgroup.
 //   work     sum over (sequence, K/V head) of row tiles x steps_of(keys); tiles: of row tiles; longest: largest steps_of(keys)
 //   share    how the keys may be shared out
-// Uncut, the row tiles take as long as rounds of the longest or, where they are of different lengths, an even share and the longest behind it.  Cut for r rounds of
-// `at_once` workgroups a tile's last part is half a part on average, so that parts are work / (r at_once - tiles / 2).  What is estimated to end first is
-// taken, costs beside the keys' being those of an item and of the fold, in sixteenths of a step.
+// What is estimated to end first is taken, in sixteenths of the time that a step takes a workgroup which has its compute unit to itself:
+//   - uncut: rounds of the longest row tile or, where they are of different lengths, an even share and the longest behind it;
+//   - cut for one round of 1 .. most_per_unit workgroups a unit, or for more of them, which then share the work evenly but for the last.  A tile's last part is half a
+//     part on average, so that parts are work / (workgroups - tiles / 2).
+// (Few rows, K and V at HBM's rate: 1, 2, 3 a unit take 253, 224, 218 us for 64 sequences of up to 16K keys in 8 bits, but each part costs the fold: 1 x 32K keys in
+// 8 bits 24.5, 25.4, 32.4.)
 // Tiles that are cut have fewer than steps / part + 1 parts: all of them together at most share.slots(tiles).
-constexpr int kPartStep = 128, kMostRounds = 4;
+constexpr int kPartStep = 128, kUnits = 256, kMaxPerUnit = 4;
 constexpr int steps_of(int keys) { return (keys + kPartStep - 1) / kPartStep; }
 struct Share {
-  int at_once;      // workgroups that run at once, 0: keys are not shared out
-  int rounds;       // at most
-  int item, fold;   // costs
-  constexpr int slots(int64_t tiles) const { return at_once * rounds + (int)(tiles < at_once * rounds ? tiles : at_once * rounds); }
+  int most_per_unit;   // workgroups that a compute unit holds, 0: keys are not shared out
+  int rounds;          // at most
+  int item, fold, part;   // costs of an item beside its steps, of the fold, and of a part there, in sixteenths of a step
+  constexpr int most() const { return kUnits * most_per_unit * rounds; }   // items that cutting adds
+  constexpr int slots(int64_t tiles) const { return most() + (int)(tiles < most() ? tiles : most()); }
 };
-constexpr int part_keys(int64_t work, int64_t tiles, int longest, Share share) {
-  if (share.at_once <= 0 || work <= 0 || work > 0x3ffffff) return kPosLimit;   // (as many keys as a sequence has at most)
-  const unsigned w = (unsigned)work, at_once = (unsigned)share.at_once, n_tiles = (unsigned)(tiles < 0x3ffffff ? tiles : 0x3ffffff);
-  const unsigned full = (n_tiles + at_once - 1) / at_once;
-  const unsigned even = 16 * w / at_once + 16 * (unsigned)longest, rounds = full < 0x3ff && longest < 0x3fff ? 16 * full * (unsigned)longest : even;
-  unsigned best = (even < rounds ? even : rounds) + (unsigned)share.item * (full < 64 ? full : 64);
+constexpr int step_time(int per_unit) { return per_unit <= 1 ? 16 : per_unit == 2 ? 28 : per_unit == 3 ? 41 : 54; }
+constexpr int ceil_div(int n, int d) {   // of n < 2^24: the float quotient is at least the whole one
+  const int q = (int)((float)n / (float)d);
+  return q * d < n ? q + 1 : q;
+}
+constexpr int part_keys(int64_t work, int64_t tiles, int longest, const Share& share) {
+  if (share.most_per_unit <= 0 || work <= 0 || work >= (1 << 24) || tiles >= (1 << 24) || longest >= (1 << 14)) return kPosLimit;   // (as many keys as a sequence has at most)
+  const int w = (int)work, n_tiles = (int)tiles, most = share.most_per_unit, at_once = kUnits * most, all_busy = step_time(most);
+  const int full = n_tiles / at_once, rest = n_tiles - full * at_once;
+  const float each = (float)longest, rounds = (float)full * (each * (float)all_busy + (float)share.item) + (rest > 0 ? each * (float)step_time((rest + kUnits - 1) / kUnits) + (float)share.item : 0.f);
+  const float even = (float)w * (float)all_busy / (float)at_once + 16.f * each + (float)share.item;
+  float best = rounds < even ? rounds : even;
   int part = kPosLimit;
-  for (int r = 1; r <= share.rounds; r++) {
-    const unsigned all = (unsigned)r * at_once;
-    if (all <= n_tiles / 2) continue;
-    const unsigned n = all - n_tiles / 2, steps = (w + n - 1) / n < 2 ? 2 : (w + n - 1) / n;
-    const unsigned time = (unsigned)r * (16 * steps + (unsigned)share.item) + (unsigned)share.fold;
-    if (steps < (unsigned)longest && time < best) {
+  for (int c = 1; c < most + share.rounds; c++) {   // (more rounds than one where every unit is full)
+    const int per_unit = c < most ? c : most, r = c < most ? 1 : c - most + 1, n = kUnits * per_unit * r - n_tiles / 2;
+    if (n <= 0) continue;
+    const int least = ceil_div(w, n), steps = least < 2 ? 2 : least;
+    if (steps >= longest) continue;
+    const float shared = r == 1 ? (float)(steps * step_time(per_unit) + share.item)
+                                : ((float)w * (float)all_busy + ((float)w / (float)steps + (float)(n_tiles / 2)) * (float)share.item) / (float)at_once + 8.f * (float)steps;
+    const float time = shared + (float)(share.fold + share.part * ceil_div(longest, steps));
+    if (time < best) {
       best = time;
-      part = (int)steps * kPartStep;
+      part = steps * kPartStep;
     }
   }
   return part;

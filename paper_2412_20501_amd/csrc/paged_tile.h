@@ -133,9 +133,9 @@ __device__ __forceinline__ bool tile_rows(const PagedParams& p, const Item& w, i
   // Tiles go out in pairs, K of tile a and V of tile a - 1 (one that is not there is left out): the place of V's tile is the one that K's had.
   const int edge_tile = min(limit_first >= end ? n_tiles : max(0, limit_first - w.k0) / BN, n_keys % BN ? last_tile : n_tiles);   // from here on tiles hold keys that some rows do not see
   unsigned bad = 0;
-  auto look = [&](u32x4 x) __attribute__((always_inline)) {   // a half's top bit: its exponent is all ones
+  auto look = [&](u32x4 x) __attribute__((always_inline)) {
 #pragma unroll
-    for (int i = 0; i < 4; i++) bad |= ((x[i] & 0x7f807f80u) + 0x00800080u) & 0x80008000u;
+    for (int i = 0; i < 4; i++) bad |= not_finite(x[i]);
   };
   struct Raw { u32x4 x; unsigned scale; };   // e4m3: 16 values of a row
   auto load8 = [&](const char* base, const unsigned char* scales, Place at, bool last, int l, Raw& r) __attribute__((always_inline)) {
@@ -494,7 +494,7 @@ __global__ void __launch_bounds__(512, 2) paged_many_kernel(const PagedParams p)
   if (tile_rows<D, F8, OUT_F32>(p, w, slot_row, lds)) return;
   for (int r = 0; r < n; r += 16) {
     __syncthreads();
-    few_rows<D, F8, 1, 8, OUT_F32>(p, w, row0 + r, slot_row + r, lds);
+    few_rows<D, F8, 1, 8, false, OUT_F32>(p, w, row0 + r, slot_row + r, lds);
   }
 }
 

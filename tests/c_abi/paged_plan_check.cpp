@@ -32,8 +32,8 @@ int main() {
     s.table_stride = max_pages; s.n = n; s.max_pages = max_pages; s.tokens = tokens; s.n_pages = n_pages; s.page_size = page_size;
     s.by_page = tr::make_divisor((unsigned)page_size);
     for (tr::RowClass tile : {tr::RowClass{16, 0, 1 << 30}, tr::RowClass{32, 0, 1 << 30}, tr::RowClass{32, 0, 32}, tr::RowClass{256, 32, 1 << 30}})
-      for (int at_once : {0, 8, 512}) {
-        const tr::Share share = {at_once, 1 + round % 4, 5 * (round % 7), 10 * (round % 5)};
+      for (int per_unit : {0, 1, 3}) {
+        const tr::Share share = {per_unit, 1 + round % 4, 5 * (round % 7), 10 * (round % 5), round % 3};
         int64_t work = 0, tiles = 0;
         int longest = 0;
         for (int b = 0; b < n; b++) {
@@ -57,7 +57,7 @@ int main() {
         }
         if (!wild) EXPECT(tiles <= tr::most_tiles(tokens, n, gq, tile));
         const int part = tr::part_keys(work * Hkv, tiles * Hkv, longest, share);
-        EXPECT(part > 0 && (part == tr::kPosLimit || part % tr::kPartStep == 0) && (at_once > 0 || part == tr::kPosLimit));
+        EXPECT(part > 0 && (part == tr::kPosLimit || part % tr::kPartStep == 0) && (per_unit > 0 || part == tr::kPosLimit));
         int64_t items = 0, slots = 0;
         for (int b = 0; b < n; b++) {
           const tr::Sequence q = tr::sequence(s, b);
@@ -67,7 +67,7 @@ int main() {
           if (parts > 1) slots += mine;
         }
         EXPECT(slots <= share.slots(tiles * Hkv));
-        EXPECT(items <= tiles * Hkv + at_once * share.rounds);
+        EXPECT(items <= tiles * Hkv + share.most());
       }
   }
   printf("paged plan ok\n");
