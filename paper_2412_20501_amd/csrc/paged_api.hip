@@ -124,7 +124,8 @@ tr_status take_sequences(const tr_sequences* seqs, const tr_tensor* pages, int64
   }
   s.table = seqs->page_table; s.kv_len = seqs->kv_len; s.q_start = seqs->q_start; s.q_pos = seqs->q_pos;
   s.table_stride = seqs->table_stride;
-  s.n = (int)seqs->n_seqs; s.max_pages = (int)seqs->max_pages; s.tokens = (int)(tokens < 0 ? 0 : tokens);
+  s.n = (int)seqs->n_seqs; s.max_pages = pages->B > 0 ? (int)seqs->max_pages : 0;   // (no pages: no keys)
+  s.tokens = (int)(tokens < 0 ? 0 : tokens);
   s.n_pages = (int)pages->B; s.page_size = (int)pages->S;
   s.by_page = tr::make_divisor((unsigned)pages->S);
   views.add(seqs->page_table, seqs->max_pages > 0 && seqs->n_seqs > 0 ? (seqs->n_seqs - 1) * seqs->table_stride + seqs->max_pages : 0);

@@ -22,11 +22,12 @@ PagedLaunch paged_launch(int64_t tokens, int64_t n_seqs, int64_t max_keys, int H
   for (int i = 0; i < l.n; i++) {
     PagedLaunch::Part& c = l.part[i];
     c.tiles = most_tiles(tokens, n_seqs, gq, c.rows) * Hkv;
-    // Workgroups that the registers of each kernel allow a compute unit; what an item, the fold and its parts cost, measured.  More rounds than one only
-    // for launches that may have more row tiles than a part of one round.
+    // Workgroups that the registers of each kernel allow a compute unit; what an item, the fold and its parts cost, measured.  A second round only
+    // for launches of few rows that may have more row tiles than a part of the first: the launch has workgroups for all that its plan may choose, and
+    // those without an item cost 2 us a round of theirs (a mixture of 527 tokens of 16 sequences 99 us with 1300 of them, 108 with 3800).
     const int per_unit = c.rows.tile == kManyRows ? 1 : paged_few_waves(D, f8, c.rows.tile / 16);
-    const int rounds = 2 * c.tiles <= kUnits * per_unit ? 1 : c.rows.tile == kManyRows ? 2 : 4;
-    const Share cut = c.rows.tile == kManyRows ? Share{1, rounds, 20, 32, 2} : Share{per_unit, rounds, 36, 64, 2};
+    const int rounds = c.rows.tile == kManyRows || 2 * c.tiles <= kUnits * per_unit ? 1 : 2;
+    const Share cut = c.rows.tile == kManyRows ? Share{1, 1, 20, 32, 2} : Share{per_unit, rounds, 36, 64, 2};
     c.parts = std::max<int64_t>(1, (max_keys + 2 * kPartStep - 1) / (2 * kPartStep));
     c.share = c.parts == 1 ? Share{0, 0, 0, 0, 0} : cut;
   }

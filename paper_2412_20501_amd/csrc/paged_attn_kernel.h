@@ -11,7 +11,7 @@ typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
 typedef unsigned u32x2 __attribute__((ext_vector_type(2)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 
-constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kLog2e = 1.4426950408889634f, kSumCap = 0x1p80f;
 
 // ---- Which work a workgroup has.
 //
@@ -125,10 +125,9 @@ __device__ __forceinline__ Sequence uniform_sequence(const PagedParams& p, int b
   return Sequence{uniform(q.start), uniform(q.n), uniform(q.len), uniform(q.pos)};
 }
 
-// The item of workgroup `id` of `ids`; false: none.  The items of a K/V head and part lie next to each other, and each XCD has a contiguous
-// eighth of all, so that row tiles which read the same keys mostly share an L2.
-__device__ __forceinline__ bool find_item(const PagedParams& p, int id, Item& w) {
-  const Plan plan = make_plan(p);
+// Item `id` of the launch; false: none (it lies behind the last one, or its part has no live keys).  The items of a K/V head and part lie next to each
+// other, and each XCD has a contiguous eighth of all, so that row tiles which read the same keys mostly share an L2.
+__device__ __forceinline__ bool find_item(const PagedParams& p, const Plan& plan, int id, Item& w) {
   const int part = plan.part;
   auto items = [&](const Sequence& q) { return tiles_of(q.n * p.gq, p.rows) * parts_of(q.len, part) * p.Hkv; };
   int before, b = 0;
@@ -292,13 +291,12 @@ __device__ __forceinline__ void few_rows(const PagedParams& p, const Item& w, in
   };
 
   f32x4 acc[RT][DL];
-  float m_ref[RT], mc[RT], l_run[RT], cap[RT];
+  float m_ref[RT], mc[RT], l_run[RT];
   const float c2 = p.scale * kLog2e;
 #pragma unroll
   for (int rt = 0; rt < RT; rt++) {
-    m_ref[rt] = -INFINITY;
-    mc[rt] = l_run[rt] = 0.f;
-    cap[rt] = -1.f;
+    m_ref[rt] = mc[rt] = -INFINITY;
+    l_run[rt] = 0.f;
 #pragma unroll
     for (int j = 0; j < DL; j++) acc[rt][j] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
@@ -344,7 +342,8 @@ __device__ __forceinline__ void few_rows(const PagedParams& p, const Item& w, in
             if (key0 + 16 * h + 4 * g + r >= limit[rt] || !there[h]) s[rt][h][r] = -INFINITY;
     }
     // Weights relative to a reference that is not the running maximum: any gives the same result, and one that the
-    // first scores set is replaced only where a sum of weights passes 2^80 (fp32 and bf16 hold them as well as small ones).
+    // first scores set is replaced only where a sum of weights passes 2^80 (fp32 and bf16 hold them as well as small ones).  A row without one has -inf there: its
+    // weights are infinite or NaN.
     bf16x8 pf[RT];
 #pragma unroll
     for (int rt = 0; rt < RT; rt++) {
@@ -354,7 +353,7 @@ __device__ __forceinline__ void few_rows(const PagedParams& p, const Item& w, in
         e[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[rt][i >> 2][i & 3], c2, -mc[rt]));
         sum += e[i];
       }
-      if (__any(!(sum <= cap[rt]))) {
+      if (__any(!(sum <= kSumCap))) {
         float top = s[rt][0][0];
 #pragma unroll
         for (int i = 1; i < 8; i++) top = fmaxf(top, s[rt][i >> 2][i & 3]);
@@ -369,12 +368,12 @@ __device__ __forceinline__ void few_rows(const PagedParams& p, const Item& w, in
 #pragma unroll
           for (int r = 0; r < 4; r++) acc[rt][j][r] *= a;
         m_ref[rt] = m_new;
-        mc[rt] = m_new == -INFINITY ? 0.f : m_new * c2;
-        cap[rt] = m_new == -INFINITY ? -1.f : 0x1p80f;
+        mc[rt] = m_new * c2;
+        const float by = m_new == -INFINITY ? 0.f : mc[rt];
         sum = 0.f;
 #pragma unroll
         for (int i = 0; i < 8; i++) {
-          e[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[rt][i >> 2][i & 3], c2, -mc[rt]));
+          e[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[rt][i >> 2][i & 3], c2, -by));
           sum += e[i];
         }
       }
@@ -519,34 +518,36 @@ template <int D, bool F8, int RT, bool OUT_F32>
 __global__ void __launch_bounds__(256, paged_few_waves(D, F8, RT)) paged_few_kernel(const PagedParams p) {
   extern __shared__ __attribute__((aligned(1024))) char lds[];
   Item w;
-  if (!find_item(p, (int)blockIdx.x, w)) return;
+  if (!find_item(p, make_plan(p), (int)blockIdx.x, w)) return;
   few_rows<D, F8, RT, 4, true, OUT_F32>(p, w, w.tile * 16 * RT, w.slot * 16 * RT, lds);
 }
 
 // ---- Row tiles whose keys were cut: out = sum of exp(lse_i - lse) out_i over their live parts, in their order.
-// A workgroup has a tile and, in turns of gridDim.y, 1024 / D of its rows, D / 4 lanes a row.  What bounds it is latency: the lanes of a row
+// A workgroup has pieces of 1024 / D rows of a tile, D / 4 lanes a row.  What bounds it is latency: the lanes of a row
 // fetch the lse of one part each, and pieces of eight parts are on their way at a time.
 template <int D, bool OUT_F32>
 __global__ void __launch_bounds__(256) paged_fold_kernel(const PagedParams p) {
   constexpr int LANES = D / 4, ROWS = 256 / LANES, AHEAD = 8;
   const Plan plan = make_plan(p);
-  const int part = plan.part, size = p.rows.tile;
+  const int part = plan.part, size = p.rows.tile, pieces = max(1, size / ROWS);
   auto cut_tiles = [&](const Sequence& q) { return parts_of(q.len, part) > 1 ? tiles_of(q.n * p.gq, p.rows) * p.Hkv : 0; };
+  for (int at = (int)blockIdx.x;; at += (int)gridDim.x) {
   int b, before;
-  if (!locate(p, plan, (int)blockIdx.x, cut_tiles, b, before)) return;
+  if (!locate(p, plan, at / pieces, cut_tiles, b, before)) return;
   Item w;
   w.q = uniform_sequence(p, uniform(b));
   w.rows = uniform(w.q.n * p.gq);
   const int base = sum_before(p, plan, uniform(b), [&](const Sequence& q) { return cut_tiles(q) * parts_of(q.len, part); });
-  const int parts = uniform(parts_of(w.q.len, part)), tiles = uniform(tiles_of(w.rows, p.rows)), i = uniform((int)blockIdx.x - before);
+  const int parts = uniform(parts_of(w.q.len, part)), tiles = uniform(tiles_of(w.rows, p.rows)), i = uniform(at / pieces - before);
   w.hk = uniform(i / tiles);
   const int row0 = (i - w.hk * tiles) * size, rows = min(size, w.rows - row0);
   const int n_live = uniform(parts_of(row_limit(p, w.q, row0 + rows - 1), part));
-  if (n_live == 1) return;   // one part: written already
-  if (base < 0 || base + (i + 1) * parts > p.slots) return;   // (only where sequences overlap)
+  if (n_live == 1) continue;   // one part: written already
+  if (base < 0 || base + (i + 1) * parts > p.slots) continue;   // (only where sequences overlap)
   w.n_parts = 1;   // what follows is stored for good
   const int c = (int)threadIdx.x % LANES;
-  for (int r = (int)blockIdx.y * ROWS + (int)threadIdx.x / LANES; r < rows; r += (int)gridDim.y * ROWS) {
+  const int r = at % pieces * ROWS + (int)threadIdx.x / LANES;
+  if (r < rows) {
     const int64_t slot_row = ((int64_t)base + (int64_t)i * parts) * size + r;
     const float* const ls = p.part_lse + slot_row;
     const float* const out = p.part_out + slot_row * D + 4 * c;
@@ -585,6 +586,7 @@ __global__ void __launch_bounds__(256) paged_fold_kernel(const PagedParams p) {
 #pragma unroll
     for (int e = 0; e < 4; e++) o[e] *= inv;
     store_piece<D, OUT_F32>(p, w, row0, 0, r, c, o, nan ? __builtin_nanf("") : total > 0.f ? top + logf(total) : -INFINITY);
+  }
   }
 }
 

@@ -51,7 +51,7 @@ constexpr int tiles_of(int rows, RowClass c) { return rows > c.over && rows <= c
 //   work     sum over (sequence, K/V head) of row tiles x steps_of(keys); tiles: of row tiles; longest: largest steps_of(keys)
 //   share    how the keys may be shared out
 // What is estimated to end first is taken, in sixteenths of the time that a step takes a workgroup which has its compute unit to itself:
-//   - uncut: rounds of the longest row tile or, where they are of different lengths, an even share and the longest behind it;
+//   - uncut: rounds of the longest row tile or, where they are of different lengths, an even share and the longest behind it, which then has its unit to itself;
 //   - cut for one round of 1 .. most_per_unit workgroups a unit, or for more of them, which then share the work evenly but for the last.  A tile's last part is half a
 //     part on average, so that parts are work / (workgroups - tiles / 2).
 // (Few rows, K and V at HBM's rate: 1, 2, 3 a unit take 253, 224, 218 us for 64 sequences of up to 16K keys in 8 bits, but each part costs the fold: 1 x 32K keys in
@@ -76,8 +76,9 @@ constexpr int part_keys(int64_t work, int64_t tiles, int longest, const Share& s
   const int w = (int)work, n_tiles = (int)tiles, most = share.most_per_unit, at_once = kUnits * most, all_busy = step_time(most);
   const int full = n_tiles / at_once, rest = n_tiles - full * at_once;
   const float each = (float)longest, rounds = (float)full * (each * (float)all_busy + (float)share.item) + (rest > 0 ? each * (float)step_time((rest + kUnits - 1) / kUnits) + (float)share.item : 0.f);
-  const float even = (float)w * (float)all_busy / (float)at_once + 16.f * each + (float)share.item;
-  float best = rounds < even ? rounds : even;
+  const float even = ((float)w * (float)all_busy + (float)n_tiles * (float)share.item) / (float)at_once + 8.f * each;
+  const float alone = 16.f * each + (float)share.item, at_least = even > alone ? even : alone;
+  float best = rounds < at_least ? rounds : at_least;
   int part = kPosLimit;
   for (int c = 1; c < most + share.rounds; c++) {   // (more rounds than one where every unit is full)
     const int per_unit = c < most ? c : most, r = c < most ? 1 : c - most + 1, n = kUnits * per_unit * r - n_tiles / 2;
@@ -96,10 +97,11 @@ constexpr int part_keys(int64_t work, int64_t tiles, int longest, const Share& s
 }
 constexpr int parts_of(int keys, int part) { return keys <= part ? 1 : (keys - 1) / part + 1; }
 
-// Row tiles that the sequences of `tokens` tokens have at most, `group` rows a token: each has at most one that is not full.
+// Row tiles that the sequences of `tokens` tokens have at most, `group` rows a token: each has at most one that is not full, and over + 1 rows at least for
+// a tile (a class that leaves rows out leaves out half a tile at most); where the most rows are one tile's, no sequence has two.
 constexpr int64_t most_tiles(int64_t tokens, int64_t n_seqs, int64_t group, RowClass c) {
-  const int64_t some = tokens * group / (c.over + 1);
-  return tokens * group / c.tile + (some < n_seqs ? some : n_seqs);
+  const int64_t rows = tokens * group, some = rows / (c.over + 1), full = c.most <= c.tile ? n_seqs : rows / c.tile + n_seqs;
+  return some < full ? some : full;
 }
 
 }  // namespace tr

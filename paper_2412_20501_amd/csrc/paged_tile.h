@@ -72,16 +72,7 @@ __device__ __forceinline__ bool tile_rows(const PagedParams& p, const Item& w, i
   const int limit_first = row_limit(p, w.q, row0), end = min(w.k1, row_limit(p, w.q, row0 + n_rows - 1));
   const int n_keys = end - w.k0, n_tiles = uniform((max(n_keys, 0) + BN - 1) / BN), last_tile = n_tiles - 1;
 
-  // a page that is none: looked for in all of the item's keys at once
   if (tid == 0) *reinterpret_cast<int*>(lds + T::FLAG) = 0;
-  __syncthreads();
-  {
-    bool none = false;
-    for (int key = w.k0 + tid * 16; key < end; key += 512 * 16) none |= slot_of(p.seq, w.b, key).page < 0;
-    if (__any(none) && lane == 0) *reinterpret_cast<int*>(lds + T::FLAG) = 1;
-  }
-  __syncthreads();
-  if (*reinterpret_cast<volatile int*>(lds + T::FLAG)) return false;
 
   // ---- tiles on their way: page and slot of this wave's share of a tile, in scalar registers
   const char* const kb = p.k_pages + (int64_t)w.hk * p.head_b;
@@ -90,11 +81,14 @@ __device__ __forceinline__ bool tile_rows(const PagedParams& p, const Item& w, i
   const const_ptr table = (const_ptr)(uintptr_t)(p.seq.table + (int64_t)w.b * p.seq.table_stride);
   const int share0 = w.k0 + wave * SHARE;   // first key of this wave's share of tile 0
   struct Place { int page, slot; };
-  auto place_of = [&](int t) __attribute__((always_inline)) -> Place {   // tiles up to the last one; there a share behind the end takes the last keys' place
+  // Tiles up to the last one; there a share behind the end takes the last keys' place.  In the place of a page that is none the last one is read, and the
+  // result is not kept (below).
+  const unsigned last_page = p.seq.n_pages - 1;
+  auto place_of = [&](int t) __attribute__((always_inline)) -> Place {
     int key = (share0 + t * BN) & ~15;
     key = min(key, (end - 1) & ~15);
     const int i = divide(p.seq.by_page, uniform(key));
-    return Place{table[i], key - i * p.seq.page_size};
+    return Place{(int)min((unsigned)table[i], last_page), key - i * p.seq.page_size};
   };
   auto last_slot = [&](int row) __attribute__((always_inline)) -> int {   // of a row of the last tile in its group
     const int first = (share0 + last_tile * BN) & ~15, group = min(first, (end - 1) & ~15);
@@ -212,10 +206,16 @@ __device__ __forceinline__ bool tile_rows(const PagedParams& p, const Item& w, i
       pl_v = p3;
       if (n > 4) pl_k = place_of(4);
     } else {
-      pl_k = place_of(0);
-      pair(0, 0, IC<0>{});
-      pair(1, 0, IC<0>{});
-      pair(2, 1, IC<0>{});
+      // (all places at once: each is a load that the next would wait behind)
+      const Place p0 = place_of(0), p1 = place_of(min(1, last_tile)), p2 = place_of(min(2, last_tile)), p3 = place_of(min(3, last_tile));
+      send(kb, p0, last_tile == 0, k_off, false, 0);
+      send(vb, p0, last_tile == 0, v_off, true, NS * TILE_BYTES);
+      if (last_tile >= 1) send(kb, p1, last_tile == 1, k_off, false, TILE_BYTES);
+      if (last_tile >= 2) send(kb, p2, last_tile == 2, k_off, false, 2 * TILE_BYTES);
+      if (last_tile >= 1) send(vb, p1, last_tile == 1, v_off, true, (NS + 1) * TILE_BYTES);
+      a = 3;
+      pl_k = p3;
+      pl_v = p2;
     }
   }
   const int qrow = row0 + min(qw0 + ql, n_rows - 1), q_tok = divide(p.by_gq, qrow);
@@ -225,6 +225,8 @@ __device__ __forceinline__ bool tile_rows(const PagedParams& p, const Item& w, i
 #pragma unroll
     for (int ks = 0; ks < KS; ks++) qf[ks] = *reinterpret_cast<const bf16x8*>(qp + 16 * ks);
   }
+  // pages that are none, among all of the item's keys
+  for (int key = w.k0 + tid * 16; key < end; key += 512 * 16) bad |= slot_of(p.seq, w.b, key).page < 0 ? 1u : 0u;
   // keys that the lane's row, and the first and the last row of the wave, see (in keys from k0 on)
   const int lane_end = min(w.k1, visible(w.q, q_tok, p.causal)) - w.k0;
   const bool rows_here = qw0 < n_rows;
@@ -247,7 +249,7 @@ __device__ __forceinline__ bool tile_rows(const PagedParams& p, const Item& w, i
   for (int db = 0; db < DB; db++)
 #pragma unroll
     for (int i = 0; i < 16; i++) o_acc[db][i] = 0.f;
-  float m_ref = -INFINITY, mc = 0.f, l_run = 0.f, cap = -1.f;   // as in few_rows
+  float m_ref = -INFINITY, mc = -INFINITY, l_run = 0.f;   // as in few_rows
   const float c2 = p.scale * kLog2e;
 
   // One step, as in the block attention kernel: S_{j+1} = K_{j+1} Q^T and O += V_{j-1}^T P_{j-1}^T beside the weights of sub-tile j, in the order
@@ -325,7 +327,7 @@ __device__ __forceinline__ bool tile_rows(const PagedParams& p, const Item& w, i
 #pragma unroll
     for (int h = 0; h < 2; h++) p_out[h] = __builtin_bit_cast(bf16x8, u32x4{pw[4 * h], pw[4 * h + 1], pw[4 * h + 2], pw[4 * h + 3]});
     float psum = ps0 + ps1;
-    if (__builtin_expect(__any(!(psum <= cap)), 0)) {
+    if (__builtin_expect(__any(!(psum <= kSumCap)), 0)) {
       float top = s_in[0];
 #pragma unroll
       for (int i = 1; i < 16; i++) top = fmaxf(top, s_in[i]);
@@ -338,9 +340,8 @@ __device__ __forceinline__ bool tile_rows(const PagedParams& p, const Item& w, i
 #pragma unroll
         for (int i = 0; i < 16; i++) o_acc[db][i] *= f;
       m_ref = m_new;
-      mc = m_ref == -INFINITY ? 0.f : m_ref * c2;
-      cap = m_ref == -INFINITY ? -1.f : 0x1p80f;
-      const float mc2 = mc;
+      mc = m_ref * c2;
+      const float mc2 = m_ref == -INFINITY ? 0.f : mc;
       float q0s = 0.f, q1s = 0.f;
 #pragma unroll
       for (int i = 0; i < 16; i += 2) {
@@ -457,7 +458,7 @@ __device__ __forceinline__ bool tile_rows(const PagedParams& p, const Item& w, i
 
   // ---- epilogue: each wave turns its 32 x D results over in LDS and stores whole rows
   {
-  const int lane = __builtin_amdgcn_mbcnt_hi(~0u, __builtin_amdgcn_mbcnt_lo(~0u, 0u)), ql = lane & 31, hf = lane >> 5;   // (counted anew: not held over the loop)
+  const int lane = lane_anew(), ql = lane & 31, hf = lane >> 5;   // (not held over the loop)
   const float l_tot = halves_sum(l_run), inv = l_tot == 0.f ? 0.f : 1.f / l_tot;
   const float lse = l_tot > 0.f ? m_ref * p.scale + logf(l_tot) : l_tot == 0.f ? -INFINITY : __builtin_nanf("");
   char* const my = lds + wave * (32 * 4 * D);
@@ -489,9 +490,10 @@ template <int D, bool F8, bool OUT_F32>
 __global__ void __launch_bounds__(512, 2) paged_many_kernel(const PagedParams p) {
   extern __shared__ __attribute__((aligned(1024))) char lds[];
   Item w;
-  if (!find_item(p, (int)blockIdx.x, w)) return;
+  if (!find_item(p, make_plan(p), (int)blockIdx.x, w)) return;
   const int row0 = w.tile * kManyRows, slot_row = w.slot * kManyRows, n = min(kManyRows, w.rows - row0);
   if (tile_rows<D, F8, OUT_F32>(p, w, slot_row, lds)) return;
+#pragma unroll 1
   for (int r = 0; r < n; r += 16) {
     __syncthreads();
     few_rows<D, F8, 1, 8, false, OUT_F32>(p, w, row0 + r, slot_row + r, lds);
