@@ -14,7 +14,9 @@ PagedLaunch paged_launch(int64_t tokens, int64_t n_seqs, int64_t max_keys, int H
   PagedLaunch l;
   const int64_t rows = tokens * gq;
   constexpr int any = 0x7fffffff;
-  const RowClass few16 = {16, 0, any}, few32 = {32, 0, any}, many = {kManyRows, 0, any}, only_few = {32, 0, 32}, only_many = {kManyRows, 32, any};
+  const RowClass few16 = {16, 0, any}, few32 = {32, 0, any}, many = {kManyRows, 0, any};
+  const int few = gq <= 4 ? 16 : 32;   // in a mixture: four tokens
+  const RowClass only_few = {few, 0, few}, only_many = {kManyRows, few, any};
   const bool mixed = rows > 32 * n_seqs && n_seqs > 1;
   l.n = mixed ? 2 : 1;
   l.part[0].rows = mixed ? only_few : rows <= 16 * n_seqs ? few16 : rows <= 32 * n_seqs ? few32 : many;
