@@ -354,7 +354,7 @@ size_t tr_paged_attn_workspace_bytes(const tr_tensor* q, const tr_tensor* k_page
  * from this thread carries them in its dispatch: start_event then holds the time the kernel
  * began executing and stop_event the time it finished, so hipEventElapsedTime(start, stop)
  * is the kernel's own duration without queueing gaps.  Only that one launch is timed
- * (tr_ring_attn: its first kernel; a block step whose keys are cut, tr_paged_attn: its attention, not the fold); the events stay owned by the caller.  Always TR_OK.
+ * (tr_ring_attn, tr_paged_attn: its first kernel; a block step whose keys are cut: its attention, not the fold); the events stay owned by the caller.  Always TR_OK.
  */
 tr_status tr_time_next_kernel(void* start_event, void* stop_event);
 

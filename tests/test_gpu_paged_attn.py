@@ -160,3 +160,98 @@ def test_arrays_with_wrong_entries(lib):
     out.fill_(3.5)
     lib.tr_paged_attn(q, *c.args(), backwards, True, 0.1, out, lse)
     assert (out == 3.5).all()
+
+
+@pytest.mark.parametrize("f8", [False, True])
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("shape", [([12001], [300], 1, 4, 64), ([9000, 20, 300], [700, 1, 31], 2, 2, 16), ([40000, 1], [1, 1], 1, 8, 16), ([6000] * 5, [7] * 5, 1, 4, 32)])
+def test_long_caches(lib, shape, D, f8):
+    """Keys that are shared out among workgroups, and the same without a workspace."""
+    kv, q, Hkv, gq, page = shape
+    c = Cache(kv, q, Hkv, D, page, f8, "head", seed=15)
+    for workspace in (True, False):
+        _, out, lse, found = _run(lib, c, Hkv * gq, workspace=workspace, behind=1)
+        print(check(found, out, lse))
+
+
+@pytest.mark.parametrize("form", ["pages", "rows", "heads"])
+def test_k_and_v_in_one_array(lib, form):
+    """K and V as the two halves of each page, of each row and of each token's heads; results and queries head by head."""
+    H, page, D = 2, 32, 64
+    c = Cache([500, 77, 300], [3, 40, 100], H, D, page, False, "head", seed=16)
+    P = c.n_pages
+    if form == "pages":
+        both = torch.empty(P, 2, H, page, D, dtype=torch.bfloat16, device="cuda")
+        k, v = both[:, 0], both[:, 1]
+    elif form == "rows":
+        both = torch.empty(P, page, H, 2 * D, dtype=torch.bfloat16, device="cuda").transpose(1, 2)
+        k, v = both[..., :D], both[..., D:]
+    else:
+        both = torch.empty(P, page, 2 * H, D, dtype=torch.bfloat16, device="cuda").transpose(1, 2)
+        k, v = both[:, :H], both[:, H:]
+    k.copy_(c.pages["k"])
+    v.copy_(c.pages["v"])
+    c.pages = {"k": k, "v": v}
+    q = torch.randn(1, 8, c.tokens, D, device="cuda").bfloat16()
+    out = torch.zeros(1, 8, c.tokens, D + 24, dtype=torch.bfloat16, device="cuda")[..., :D]
+    lse = torch.zeros(c.tokens, 8, device="cuda").t().unsqueeze(0)
+    lib.tr_paged_attn(q, *c.args(), c.q_start, True, 0.1, out, lse)
+    check(attention(c, q, 0.1, True), out, lse)
+    new = torch.randn(1, c.tokens, H, D, device="cuda").bfloat16().transpose(1, 2)
+    lib.tr_cache_write(new, new + 1, *c.args(), c.q_start)
+    assert torch.equal(c.rows("k", 1)[0][37:].transpose(0, 1), new[0, :, 3:43].double())
+    assert torch.equal(c.rows("v", 2)[0][200:].transpose(0, 1), (new + 1)[0, :, 43:].double())
+    back = [torch.empty(3, H, 500, D, dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+    lib.tr_cache_read(*c.args(), *back)
+    assert torch.equal(back[0][0].double(), c.rows("k", 0)[0].transpose(0, 1)) and torch.equal(back[1][1, :, :77].double(), c.rows("v", 1)[0].transpose(0, 1))
+
+
+def test_what_the_gpu_refuses(lib):
+    """Operands on the CPU, index arrays of other types and sizes."""
+    c = Cache([20], [2], 1, 64, 16, False, "head", seed=17)
+    q, out, lse = (torch.zeros(1, 2, 2, 64, dtype=torch.bfloat16, device="cuda") for _ in range(2)), None, torch.zeros(1, 2, 2, device="cuda")
+    q, out = q
+    call = lambda **o: lib.tr_paged_attn(o.get("q", q), *c.args()[:2], o.get("table", c.table), o.get("n", c.kv_len), o.get("start", c.q_start), True, 0.1,   # noqa: E731
+                                         o.get("out", out), lse, q_pos=o.get("pos"), workspace=o.get("ws"))
+    call()
+    with pytest.raises(ValueError, match="different devices"):
+        call(out=out.cpu())
+    with pytest.raises(ValueError, match="different devices"):
+        call(start=c.q_start.cpu())
+    with pytest.raises(TypeError, match="page_table must be int32"):
+        call(table=c.table.long())
+    with pytest.raises(TypeError, match="unsupported dtype"):
+        call(q=q.half())
+    with pytest.raises(ValueError, match="kv_len must have 1 elements"):
+        call(n=torch.zeros(2, dtype=torch.int32, device="cuda"))
+    with pytest.raises(ValueError, match="q_start must have 2 elements"):
+        call(start=c.kv_len)
+    with pytest.raises(ValueError, match="dimension"):
+        call(table=c.table[0])
+    with pytest.raises(ValueError, match="contiguous"):
+        call(ws=torch.zeros(64, 64, dtype=torch.uint8, device="cuda").t()[:, :3])
+    with pytest.raises(lib.TokenRingError, match="TR_ERR_ALIAS"):
+        call(out=q)
+    long = torch.full((1, 64), -1, dtype=torch.int32, device="cuda")
+    with pytest.raises(lib.TokenRingError, match="too small"):
+        call(table=long, ws=torch.zeros(256, dtype=torch.uint8, device="cuda"))
+
+
+def test_a_cache_without_pages(lib):
+    """No page at all: nothing is seen, written or read."""
+    for f8 in (False, True):
+        t = torch.float8_e4m3fn if f8 else torch.bfloat16
+        pages = torch.empty(0, 2, 16, 64, dtype=t, device="cuda")
+        s = torch.empty(0, 2, 16, dtype=torch.float8_e8m0fnu, device="cuda") if f8 else None
+        ints = lambda *v: torch.tensor(v, dtype=torch.int32, device="cuda")   # noqa: E731
+        table, kv, start = ints(*range(64)).view(1, 64), ints(1000), ints(0, 300)
+        q = torch.randn(1, 2, 300, 64, device="cuda").bfloat16()
+        out, lse = torch.full_like(q, 7), torch.zeros(1, 2, 300, device="cuda")
+        lib.tr_paged_attn(q, pages, pages, table, kv, start, True, 0.1, out, lse, s, s)
+        assert (out == 0).all() and torch.isneginf(lse).all()
+        k = torch.full((1, 2, 1000, 64), 7.0, dtype=torch.bfloat16, device="cuda")
+        v = k.clone()
+        lib.tr_cache_read(pages, pages, table, kv, k, v, 0, s, s)
+        lib.tr_cache_write(q, q, pages, pages, table, kv, start, s, s)
+        torch.cuda.synchronize()
+        assert (k == 7).all() and (v == 7).all()
