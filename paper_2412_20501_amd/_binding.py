@@ -276,6 +276,8 @@ def tr_ring_attn_noalloc(q, k, v, n_chunks, causal, out, lse, scale=0.0, stream=
 
 def _shape(t: torch.Tensor) -> TrTensor:
     """Descriptor of type and sizes alone, for questions about them."""
+    if t.dim() != 4:
+        raise ValueError("expected a [B,H,S,D] tensor")
     return TrTensor(None, TR_F8E4M3 if t.dtype == torch.float8_e4m3fn else _DTYPES.get(t.dtype, -1), *t.shape, 0, 0, 0)
 
 
@@ -303,5 +305,7 @@ def tr_paged_attn(q, k_pages, v_pages, page_table, kv_len, q_start, causal, scal
 
 
 def tr_paged_attn_workspace_bytes(q, k_pages, page_table) -> int:
-    """Bytes of a workspace for tr_paged_attn on tensors of these shapes."""
+    """Bytes of a workspace for tr_paged_attn on tensors of these types and shapes."""
+    if page_table.dim() != 2:
+        raise ValueError("page_table must have 2 dimension(s), the last one dense")
     return int(_lib.tr_paged_attn_workspace_bytes(ctypes.byref(_shape(q)), ctypes.byref(_shape(k_pages)), *page_table.shape))

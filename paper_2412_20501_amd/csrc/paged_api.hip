@@ -16,6 +16,7 @@ using tr::overlaps;
 namespace {
 
 constexpr int64_t kMaxKeys = (int64_t)1 << 30;
+constexpr int64_t kMaxGroups = (int64_t)1 << 24;   // workgroups of 256 threads of a grid's dimension, which holds fewer than 2^32 threads
 
 // A descriptor without the strides of dimensions of one element, which say nothing; null stays null.
 struct View {
@@ -182,7 +183,7 @@ tr_status tr_cache_write(const tr_tensor* k_, const tr_tensor* v_, const tr_tens
   if (k->H != k_pages->H || k->D != k_pages->D) return fail(TR_ERR_SHAPE, "k does not match the pages' heads or head dim");
   if (v->H != k->H || v->S != k->S || v->D != k->D) return fail(TR_ERR_SHAPE, "k and v shapes differ");
   if (k->stride_h != v->stride_h || k->stride_s != v->stride_s) return fail(TR_ERR_STRIDE, "k and v must share their strides");
-  if (k->S * k->H * 2 >= ((int64_t)1 << 31)) return fail(TR_ERR_SHAPE, "too many rows for one call (2 * S * Hkv must stay below 2^31)");
+  if ((k->S + 63) / 64 * k->H * 2 >= kMaxGroups) return fail(TR_ERR_SHAPE, "too many rows for one call (2 * ceil(S / 64) * Hkv must stay below 2^24)");
   tr::CacheCopyParams p;
   memset(&p, 0, sizeof(p));
   SeqViews views;
@@ -222,7 +223,7 @@ tr_status tr_cache_read(const tr_tensor* k_pages_, const tr_tensor* v_pages_, co
   SeqViews views;
   if ((st = take_sequences(seqs, k_pages, -1, p.seq, views)) != TR_OK) return st;
   if (k->B != seqs->n_seqs) return fail(TR_ERR_SHAPE, "k has %lld batch entries for %lld sequences", (long long)k->B, (long long)seqs->n_seqs);
-  if (k->S * k->H * 2 >= ((int64_t)1 << 31)) return fail(TR_ERR_SHAPE, "too many rows for one call (2 * S * Hkv must stay below 2^31)");
+  if ((k->S + 63) / 64 * k->H * 2 >= kMaxGroups) return fail(TR_ERR_SHAPE, "too many rows for one call (2 * ceil(S / 64) * Hkv must stay below 2^24)");
   const tr_tensor* const written[] = {k, v};
   const tr_tensor* const read[] = {k_pages, v_pages, k_scales, v_scales};
   if ((st = check_apart(written, 2, read, 4, views)) != TR_OK) return st;
@@ -285,7 +286,7 @@ tr_status tr_paged_attn(const tr_tensor* q_, const tr_tensor* k_pages_, const tr
   const int gq = (int)(q->H / k_pages->H), D = (int)q->D;
   const tr::PagedLaunch l = tr::paged_launch(q->S, p.seq.n, (int64_t)p.seq.max_pages * p.seq.page_size, (int)k_pages->H, gq, D, k_scales != nullptr);
   for (int i = 0; i < l.n; i++)
-    if (l.part[i].tiles + l.part[i].share.most() >= ((int64_t)1 << 23)) return fail(TR_ERR_SHAPE, "too many workgroups for one launch");   // (of 512 threads, fewer than 2^32 in all)
+    if (l.part[i].tiles + l.part[i].share.most() >= ((int64_t)1 << 23) - 8) return fail(TR_ERR_SHAPE, "too many workgroups for one launch");   // (of 512 threads, fewer than 2^32 in all)
   const size_t need = tr_paged_attn_workspace_bytes(q, k_pages, seqs->n_seqs, seqs->max_pages);
   if (workspace && need > 0) {
     if ((uintptr_t)workspace % 256) return fail(TR_ERR_WORKSPACE, "workspace must be 256-byte aligned");

@@ -371,9 +371,12 @@ __device__ __forceinline__ bool tile_rows(const PagedParams& p, const Item& w, i
 #pragma unroll
   for (int ks = 0; ks < KS; ks++) asm volatile("" ::"v"(qf[ks]));
   __builtin_amdgcn_s_waitcnt(0);
+  asm volatile("" ::: "memory");
   look_at(0, 0);
   __builtin_amdgcn_s_waitcnt(0);
+  asm volatile("" ::: "memory");
   __builtin_amdgcn_s_barrier();   // B_0
+  asm volatile("" ::: "memory");
 
   f32x16 sA, sB;
   bf16x8 pA[2], pB[2];
@@ -418,6 +421,7 @@ __device__ __forceinline__ bool tile_rows(const PagedParams& p, const Item& w, i
       constexpr int none = 0x0F70;
       if (INNER || u + 2 <= last_tile) __builtin_amdgcn_s_waitcnt(none | 2 * IPW);
       else __builtin_amdgcn_s_waitcnt(none);
+      asm volatile("" ::: "memory");
       if (!INNER) look_at(u, su);
     }
     asm volatile("" ::: "memory");

@@ -143,6 +143,20 @@ def test_k_and_v_in_one_array(tr):
     assert write(128, 2 * half + 128, 256, 2 * 256) == ALIAS             # steps of the pages that are no multiple of the rows'
 
 
+def test_more_than_a_launch_holds(tr):
+    c = Call(tr)
+    def call(name, fields, S, H=2):   # noqa: E306
+        return c(name, **{f: c.like(f, H=H, S=S, stride_h=128 * S, stride_b=128 * S * H) for f in fields})
+    st, msg = call("write", ("k", "v"), 1 << 28)
+    assert st == SHAPE and "2^24" in msg
+    st, msg = call("read", ("k_out", "v_out"), 1 << 30)
+    assert st == SHAPE and "2^24" in msg
+
+
+def test_layout_of_the_sequences(tr):
+    assert ctypes.sizeof(tr.TrSequences) == 4 * 8 + 3 * 8 and tr.TrSequences.n_seqs.offset == 32
+
+
 def test_read_rejects(tr):
     c = Call(tr)
     assert c("read", first=-1)[0] == SHAPE
@@ -210,6 +224,10 @@ def test_python_operands(tr):
         tr.tr_cache_read(pages, pages, table, n, q, q)
     # 8192 keys: keys are shared out; what the workspace holds for that grows with the head dim only
     many = torch.zeros(1, 512, dtype=torch.int32)
+    with pytest.raises(ValueError, match=r"\[B,H,S,D\]"):
+        tr.tr_paged_attn_workspace_bytes(q[0], pages, many)
+    with pytest.raises(ValueError, match="page_table"):
+        tr.tr_paged_attn_workspace_bytes(q, pages, many[0])
     assert tr.tr_paged_attn_workspace_bytes(q, pages, many) > 0 and tr.tr_paged_attn_workspace_bytes(q[:, :, :0], pages, many) == 0
 
 
