@@ -45,7 +45,7 @@ __device__ __forceinline__ float halves_sum(float x) {
 template <int D>
 struct Tile {
   static constexpr int RB = 2 * D, BN = D == 64 ? 128 : 64, NS = 4, TILE_BYTES = BN * RB, ROWS = kManyRows;
-  static constexpr int RINGS = 2 * NS * TILE_BYTES, FLAG = RINGS, LSE = RINGS + 64, LDS = LSE + ROWS * 4;
+  static constexpr int RINGS = 2 * NS * TILE_BYTES, FLAG = RINGS, OFF = RINGS + 64, LDS = OFF + ROWS * 8;
   static_assert(TILE_BYTES == 16384 && 8 * 32 * 4 * D <= RINGS, "the waves' results lie where the rings were");
 };
 
@@ -466,8 +466,17 @@ __device__ __forceinline__ bool tile_rows(const PagedParams& p, const Item& w, i
   const float l_tot = halves_sum(l_run), inv = l_tot == 0.f ? 0.f : 1.f / l_tot;
   const float lse = l_tot > 0.f ? m_ref * p.scale + logf(l_tot) : l_tot == 0.f ? -INFINITY : __builtin_nanf("");
   char* const my = lds + wave * (32 * 4 * D);
-  float* const my_lse = reinterpret_cast<float*>(lds + T::LSE) + wave * 32;
-  if (hf == 0) my_lse[ql] = lse;
+  int64_t* const my_off = reinterpret_cast<int64_t*>(lds + T::OFF) + wave * 32;   // where the wave's rows go, counted once a row
+  if (hf == 0 && qw0 + ql < n_rows) {
+    if (w.n_parts > 1) {
+      my_off[ql] = (int64_t)(slot_row + qw0 + ql) * D;
+      p.part_lse[slot_row + qw0 + ql] = lse;
+    } else {
+      const int r = row0 + qw0 + ql, t = divide(p.by_gq, r), head = w.hk * p.gq + r - t * p.gq;
+      my_off[ql] = (int64_t)head * p.o_sh + (int64_t)(w.q.start + t) * p.o_ss;
+      p.lse[(int64_t)head * p.l_sh + (int64_t)(w.q.start + t) * p.l_ss] = lse != lse ? -INFINITY : lse;
+    }
+  }
 #pragma unroll
   for (int db = 0; db < DB; db++)
 #pragma unroll
@@ -480,11 +489,22 @@ __device__ __forceinline__ bool tile_rows(const PagedParams& p, const Item& w, i
     }
   __builtin_amdgcn_s_waitcnt(0xC07F);
   constexpr int CPRF = D / 4, RPO = 64 / CPRF;
+  const bool whole = w.n_parts == 1;
+  float* const to_f32 = whole ? reinterpret_cast<float*>(p.out) : p.part_out;
 #pragma unroll
   for (int it = 0; it < 32 / RPO; it++) {
     const int r = it * RPO + lane / CPRF, c = lane % CPRF;
-    if (qw0 + r < n_rows)
-      store_piece<D, OUT_F32>(p, w, row0, slot_row, qw0 + r, c, *reinterpret_cast<const f32x4*>(my + r * (4 * D) + ((c ^ (r & 15)) << 4)), my_lse[r]);
+    if (qw0 + r >= n_rows) continue;
+    const f32x4 o = *reinterpret_cast<const f32x4*>(my + r * (4 * D) + ((c ^ (r & 15)) << 4));
+    const int64_t to = my_off[r] + 4 * c;
+    if (OUT_F32 || !whole) {
+      *reinterpret_cast<f32x4*>(to_f32 + to) = o;
+    } else {
+      bf16x4 ob;
+#pragma unroll
+      for (int k = 0; k < 4; k++) ob[k] = (__bf16)o[k];
+      *reinterpret_cast<bf16x4*>(reinterpret_cast<__bf16*>(p.out) + to) = ob;
+    }
   }
   }
   return true;
