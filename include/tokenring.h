@@ -320,7 +320,8 @@ tr_status tr_cache_write(const tr_tensor* k, const tr_tensor* v, const tr_tensor
 /*
  * Reads the cache back as dense tensors, what tr_block_attn takes or another device is sent: row s of sequence b is key first + s.
  *   k, v [n_seqs,Hkv,S,D] bf16 (written), strides multiples of 8 elements; first >= 0
- * Exact: bf16 holds every e4m3 value times a power of two (down to its own smallest values, 2^-133, below which it rounds).
+ * Exact: bf16 holds every e4m3 value times a power of two (down to its own smallest values, 2^-133, below which it rounds, and
+ * below 2^128, from where on they are infinities).
  * Rows of keys that are not there (first + s >= kv_len[b], no page) are left as they were.  q_start and q_pos are not used.
  */
 tr_status tr_cache_read(const tr_tensor* k_pages, const tr_tensor* v_pages, const tr_tensor* k_scales, const tr_tensor* v_scales,

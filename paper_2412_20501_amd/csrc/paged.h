@@ -71,8 +71,8 @@ PagedLaunch paged_launch(int64_t tokens, int64_t n_seqs, int64_t max_keys, int H
 hipError_t launch_paged_attn(PagedParams& p, const PagedLaunch& l, int D, bool f8, float* workspace, hipStream_t stream);
 
 #if defined(__HIPCC__)
-// Two e4m3 values (the upper ones of x, if upper) times 2^(scale - 127), as two bf16: the conversion takes the scale as the exponent of a float.
-// That float is 2^(scale - 127) for 1 .. 254; 0, whose 2^-127 no normal float has, goes through half of 2^-126, and 255 is a NaN.
+// Two e4m3 values (the upper ones of x, if upper) times 2^(scale - 127), as two bf16: the conversion takes the scale as the exponent of a float.  It reads 0 as
+// 2^-127 and 255 as NaN, like the type (all 65536 pairs of a code and a scale are tested).
 __device__ __forceinline__ unsigned f8_pair(unsigned x, bool upper, unsigned scale) {
   const float s = __builtin_bit_cast(float, scale << 23);
   return __builtin_bit_cast(unsigned, upper ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x, s, true) : __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x, s, false));

@@ -193,7 +193,9 @@ __device__ __forceinline__ void store_piece(const PagedParams& p, const Item& w,
 // transposed, S^T = K Q^T, with 16x16x32 products: A is K as it lies in memory, lane (i = lane % 16, g = lane / 16) then holds
 // scores of row i for keys 4g .. 4g + 3 of each 16.  In this order the exponentials are the B operand of O^T = V^T P^T (a contraction index may
 // be permuted if both operands agree): its A operand needs 8 keys of one d in a lane, and a lane that loads D / 16 adjacent d's of those 8 keys has them after
-// one exchange of 16-bit halves.  No LDS, no barrier inside the loop.  Bound: HBM.
+// one exchange of 16-bit halves.  No LDS, no barrier inside the loop.  Bound: HBM, and where few keys are left to a workgroup the latency of its set-up and
+// loads.  64 sequences of 0.8K to 16K keys on 8 K/V heads of 128: in 8 bits 215 us, 5.2 TB/s; 4 of 8K in bf16 27 us, 4.7 TB/s; a step of 128 keys takes a workgroup that
+// has its unit to itself 1.1 us at D 128, 0.73 at D 64, the rest of it 5 (32 rows: 1.16 and 0.75).
 template <int D, bool F8, int RT, int W>
 struct Few {
   static constexpr int TILE = 16 * RT, DL = D / 16;              // rows of a tile; d's of a lane in V
@@ -522,7 +524,7 @@ __global__ void __launch_bounds__(256, paged_few_waves(D, F8, RT)) paged_few_ker
   few_rows<D, F8, RT, 4, true, OUT_F32>(p, w, w.tile * 16 * RT, w.slot * 16 * RT, lds);
 }
 
-// ---- Row tiles whose keys were cut: out = sum of exp(lse_i - lse) out_i over their live parts, in their order.
+// ---- Row tiles whose keys were cut (6 us for 32 tiles of 16 rows in 17 parts, 13 for 64 of 256 rows in four, 38 MB): out = sum of exp(lse_i - lse) out_i over their live parts, in their order.
 // A workgroup has pieces of 1024 / D rows of a tile, D / 4 lanes a row.  What bounds it is latency: the lanes of a row
 // fetch the lse of one part each, and pieces of eight parts are on their way at a time.
 template <int D, bool OUT_F32>

@@ -57,7 +57,7 @@ constexpr int tiles_of(int rows, RowClass c) { return rows > c.over && rows <= c
 // (Few rows, K and V at HBM's rate: 1, 2, 3 a unit take 253, 224, 218 us for 64 sequences of up to 16K keys in 8 bits, but each part costs the fold: 1 x 32K keys in
 // 8 bits 24.5, 25.4, 32.4.)
 // Tiles that are cut have fewer than steps / part + 1 parts: all of them together at most share.slots(tiles).
-constexpr int kPartStep = 128, kUnits = 256, kMaxPerUnit = 4;
+constexpr int kPartStep = 128, kUnits = 256;   // keys; compute units
 constexpr int steps_of(int keys) { return (keys + kPartStep - 1) / kPartStep; }
 struct Share {
   int most_per_unit;   // workgroups that a compute unit holds, 0: keys are not shared out

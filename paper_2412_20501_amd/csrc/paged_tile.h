@@ -38,7 +38,8 @@ __device__ __forceinline__ float halves_sum(float x) {
 // V read from LDS with the transposing read, one softmax sub-tile behind the products in one instruction stream, rings of four 16 KiB tiles of K
 // and of V), on rows that are (token, query head of a K/V head) pairs and with tiles that are gathered from pages: a wave's share of a tile, 8 keys
 // at D 128 and 16 at D 64, lies on one page, whose address is found with scalar loads a tile ahead.  bf16 goes straight from memory into LDS, e4m3 through
-// registers, where each value is converted once for all 256 rows.  Bound: MFMA and power, as there.
+// registers, where each value is converted once for all 256 rows.  Bound: MFMA and power, as there.  An item takes 1.1 us for 64 keys at D 128 on an idle chip (1.7 on a
+// full one), 1.55 for 128 at D 64, and 11 and 8 for its set-up and epilogue; 2048 tokens of 32 heads behind 30K keys in 8 bits 1.13 to 1.19 PFLOP/s.
 //
 // What is rare takes another way: an item with a page that is none, or with an infinity or NaN in V at a key that only some of its rows see, is computed
 // by few_rows, 16 rows at a time, which holds nothing of either against it.

@@ -146,6 +146,16 @@ def test_many_sequences(lib):
     check(found, out, lse)
 
 
+@pytest.mark.parametrize("f8", [False, True])
+def test_a_prompt_among_many_tokens(lib, f8):
+    """A chunk of a prompt and drafts in a call whose sequences have few rows on average."""
+    q = [1] * 70
+    q[33], q[50], q[60] = 330, 6, 9
+    c = Cache([n + 13 * (i % 7) for i, n in enumerate(q)], q, 1, 128, 16, f8, "head", seed=18)
+    _, out, lse, found = _run(lib, c, 4, behind=1)
+    check(found, out, lse)
+
+
 def test_arrays_with_wrong_entries(lib):
     """Lengths and starts out of range are taken as the nearest that is: nothing else is touched."""
     c = Cache([48, 48, 48], [2, 2, 2], 1, 128, 16, False, "head", seed=14, poison=False)
