@@ -336,7 +336,8 @@ tr_status tr_cache_read(const tr_tensor* k_pages, const tr_tensor* v_pages, cons
  *   q [1,Hq,S,D] bf16      out [1,Hq,S,D] bf16 or fp32 (written)      lse [1,Hq,S] fp32 (written)
  * A block result like tr_block_attn's: results on the parts of a cache that several devices hold are folded by tr_merge or
  * tr_merge_n.  A token that sees no key gets out = 0, lse = -inf.  What lies at masked keys (infinities, NaN, slots never written) reaches no result.
- * Arithmetic as tr_block_attn's; e4m3 values enter it exactly.
+ * Arithmetic as tr_block_attn's; e4m3 values enter it exactly.  Weights of up to 2^20 times V are summed up in fp32, so results are finite where
+ * the largest |V| times the number of keys is at most 2^107.
  *   workspace: device memory through which long key ranges are shared out among workgroups, 256-byte aligned, at least
  *   tr_paged_attn_workspace_bytes() bytes; its contents on return are unspecified, and it need not be initialised.  It serves one call at a
  *   time: calls (replayed graphs too) that may run at once need one each.  NULL: a row's keys are one workgroup's work, the same
