@@ -71,13 +71,24 @@ constexpr int ceil_div(int n, int d) {   // of n < 2^24: the float quotient is a
   const int q = (int)((float)n / (float)d);
   return q * d < n ? q + 1 : q;
 }
+// work plus that of `tiles` row tiles of steps_of(keys) = steps, kMostWork for that and more: no call whose sequences do not overlap reaches it before its rows
+// fill the chip many times over, so that nothing is cut there.  (tiles below 2^27, steps up to 2^23.)
+constexpr int64_t kMostWork = (int64_t)1 << 39;
+constexpr int64_t add_work(int64_t work, int64_t tiles, int steps) { return work + tiles * steps < kMostWork ? work + tiles * steps : kMostWork; }
 constexpr int part_keys(int64_t work, int64_t tiles, int longest, const Share& share) {
-  if (share.most_per_unit <= 0 || work <= 0 || work >= (1 << 24) || tiles >= (1 << 24) || longest >= (1 << 14)) return kPosLimit;   // (as many keys as a sequence has at most)
+  if (share.most_per_unit <= 0 || work <= 0 || tiles >= (1 << 24)) return kPosLimit;   // (as many keys as a sequence has at most)
+  int unit = 0;   // work is counted in 2^unit steps, rounded up, which 24 bits hold (one token of 32 heads on 2^21 keys 1.2 ms; left uncut 22.5)
+  while (work >= (1 << 24)) {
+    work = (work + 1) >> 1;
+    longest = (longest + 1) >> 1;
+    unit++;
+  }
+  const int cost_item = share.item >> unit, cost_fold = share.fold >> unit, cost_part = share.part >> unit;
   const int w = (int)work, n_tiles = (int)tiles, most = share.most_per_unit, at_once = kUnits * most, all_busy = step_time(most);
   const int full = n_tiles / at_once, rest = n_tiles - full * at_once;
-  const float each = (float)longest, rounds = (float)full * (each * (float)all_busy + (float)share.item) + (rest > 0 ? each * (float)step_time((rest + kUnits - 1) / kUnits) + (float)share.item : 0.f);
-  const float even = ((float)w * (float)all_busy + (float)n_tiles * (float)share.item) / (float)at_once + 8.f * each;
-  const float alone = 16.f * each + (float)share.item, at_least = even > alone ? even : alone;
+  const float each = (float)longest, rounds = (float)full * (each * (float)all_busy + (float)cost_item) + (rest > 0 ? each * (float)step_time((rest + kUnits - 1) / kUnits) + (float)cost_item : 0.f);
+  const float even = ((float)w * (float)all_busy + (float)n_tiles * (float)cost_item) / (float)at_once + 8.f * each;
+  const float alone = 16.f * each + (float)cost_item, at_least = even > alone ? even : alone;
   float best = rounds < at_least ? rounds : at_least;
   int part = kPosLimit;
   for (int c = 1; c < most + share.rounds; c++) {   // (more rounds than one where every unit is full)
@@ -85,12 +96,12 @@ constexpr int part_keys(int64_t work, int64_t tiles, int longest, const Share& s
     if (n <= 0) continue;
     const int least = ceil_div(w, n), steps = least < 2 ? 2 : least;
     if (steps >= longest) continue;
-    const float shared = r == 1 ? (float)(steps * step_time(per_unit) + share.item)
-                                : ((float)w * (float)all_busy + ((float)w / (float)steps + (float)(n_tiles / 2)) * (float)share.item) / (float)at_once + 8.f * (float)steps;
-    const float time = shared + (float)(share.fold + share.part * ceil_div(longest, steps));
+    const float shared = r == 1 ? (float)(steps * step_time(per_unit) + cost_item)
+                                : ((float)w * (float)all_busy + ((float)w / (float)steps + (float)(n_tiles / 2)) * (float)cost_item) / (float)at_once + 8.f * (float)steps;
+    const float time = shared + (float)(cost_fold + cost_part * ceil_div(longest, steps));
     if (time < best) {
       best = time;
-      part = steps * kPartStep;
+      part = (steps << unit) * kPartStep;
     }
   }
   return part;
