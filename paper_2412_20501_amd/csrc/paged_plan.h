@@ -56,6 +56,8 @@ constexpr int tiles_of(int rows, RowClass c) { return rows > c.over && rows <= c
 //     part on average, so that parts are work / (workgroups - tiles / 2).
 // (Few rows, K and V at HBM's rate: 1, 2, 3 a unit take 253, 224, 218 us for 64 sequences of up to 16K keys in 8 bits, but each part costs the fold: 1 x 32K keys in
 // 8 bits 24.5, 25.4, 32.4.)
+// The kernels of a call each make the plan for themselves and have to agree, or the fold reads parts that nobody wrote: floating-point operations are rounded one by one, as they are
+// written, not fused where a kernel's code happens to suggest it.  (In whole numbers a step of 16 sequences of five tokens takes 38.3 us for 37.7.)
 // Tiles that are cut have fewer than steps / part + 1 parts: all of them together at most share.slots(tiles).
 constexpr int kPartStep = 128, kUnits = 256;   // keys; compute units
 constexpr int steps_of(int keys) { return (keys + kPartStep - 1) / kPartStep; }
@@ -76,6 +78,9 @@ constexpr int ceil_div(int n, int d) {   // of n < 2^24: the float quotient is a
 constexpr int64_t kMostWork = (int64_t)1 << 39;
 constexpr int64_t add_work(int64_t work, int64_t tiles, int steps) { return work + tiles * steps < kMostWork ? work + tiles * steps : kMostWork; }
 constexpr int part_keys(int64_t work, int64_t tiles, int longest, const Share& share) {
+#if defined(__clang__)
+#pragma clang fp contract(off)
+#endif
   if (share.most_per_unit <= 0 || work <= 0 || tiles >= (1 << 24)) return kPosLimit;   // (as many keys as a sequence has at most)
   int unit = 0;   // work is counted in 2^unit steps, rounded up, which 24 bits hold (one token of 32 heads on 2^21 keys 1.2 ms; left uncut 22.5)
   while (work >= (1 << 24)) {
