@@ -224,6 +224,7 @@ tr_status tr_cache_read(const tr_tensor* k_pages_, const tr_tensor* v_pages_, co
   if ((st = take_sequences(seqs, k_pages, -1, p.seq, views)) != TR_OK) return st;
   if (k->B != seqs->n_seqs) return fail(TR_ERR_SHAPE, "k has %lld batch entries for %lld sequences", (long long)k->B, (long long)seqs->n_seqs);
   if ((k->S + 63) / 64 * k->H * 2 >= kMaxGroups) return fail(TR_ERR_SHAPE, "too many rows for one call (2 * ceil(S / 64) * Hkv must stay below 2^24)");
+  if (2 * k->B * k->H >= ((int64_t)1 << 31)) return fail(TR_ERR_SHAPE, "too many heads for one call (2 * sequences * Hkv must stay below 2^31)");
   const tr_tensor* const written[] = {k, v};
   const tr_tensor* const read[] = {k_pages, v_pages, k_scales, v_scales};
   if ((st = check_apart(written, 2, read, 4, views)) != TR_OK) return st;

@@ -1,0 +1,44 @@
+"""Sizes that the operators on a paged cache refuse, on a machine without a GPU: addresses that nothing is behind, refused before anything is launched."""
+import ctypes
+
+import pytest
+
+SHAPE = 3
+BASE = 1 << 44
+
+
+@pytest.fixture(scope="module")
+def tr():
+    from paper_2412_20501_amd.build import ensure_built
+    ensure_built()
+    import paper_2412_20501_amd as m
+    m.raw_lib()
+    return m
+
+
+def _t(tr, dtype, B, H, S, D, at):
+    return tr.TrTensor(BASE + (at << 40), dtype, B, H, S, D, H * S * D, S * D, D)
+
+
+def _seqs(tr, n, max_pages=4):
+    return tr.TrSequences(BASE + (20 << 40), BASE + (21 << 40), BASE + (22 << 40), None, n, max_pages, max_pages)
+
+
+def _refs(*x):
+    return [None if y is None else ctypes.byref(y) for y in x]
+
+
+def test_more_rows_of_heads_than_a_read_counts(tr):
+    """2^24 sequences of 64 heads, K and V: their number passes 2^31, in which the kernel counts."""
+    lib, n = tr.raw_lib(), 1 << 24
+
+    def read(n, H, S=1):   # (S = 0: nothing to read)
+        pages = [_t(tr, tr.TR_BF16, 10, H, 16, 64, i) for i in (1, 2)]
+        out = [_t(tr, tr.TR_BF16, n, H, S, 64, i) for i in (3, 4)]
+        s = _seqs(tr, n)
+        st = lib.tr_cache_read(*_refs(*pages, None, None, s), 0, *_refs(*out), None)
+        return st, lib.tr_last_error().decode()
+    for n, H in ((1 << 24, 64), (1 << 24, 100), (1 << 20, 1024)):
+        st, msg = read(n, H)
+        assert st == SHAPE and "2^31" in msg, (n, H, st, msg)
+    assert read((1 << 24) - 1, 64, 0)[0] == 0
