@@ -42,3 +42,22 @@ def test_more_rows_of_heads_than_a_read_counts(tr):
         st, msg = read(n, H)
         assert st == SHAPE and "2^31" in msg, (n, H, st, msg)
     assert read((1 << 24) - 1, 64, 0)[0] == 0
+
+
+def test_more_sequences_than_an_attention_call_takes(tr):
+    """Every workgroup of the attention goes through the sequences: beyond 2^16 of them a call would hold the GPU for seconds to hours."""
+    lib = tr.raw_lib()
+    pages = [_t(tr, tr.TR_BF16, 10, 2, 16, 64, i) for i in (1, 2)]
+
+    def attend(n, S):
+        q, out, lse = _t(tr, tr.TR_BF16, 1, 4, S, 64, 3), _t(tr, tr.TR_BF16, 1, 4, S, 64, 4), _t(tr, tr.TR_F32, 1, 4, S, 1, 5)
+        s = _seqs(tr, n, 64)
+        st = lib.tr_paged_attn(*_refs(q, *pages, None, None, s), 1, 0.1, *_refs(out, lse), None, 0, None)
+        return st, lib.tr_last_error().decode(), lib.tr_paged_attn_workspace_bytes(*_refs(q, pages[0]), n, 64)
+    for n in ((1 << 16) + 1, 1 << 24):
+        st, msg, need = attend(n, 100)
+        assert st == SHAPE and "2^16" in msg and need == 0
+    st, msg, need = attend(1 << 16, 0)
+    assert st == 0 and need == 0
+    q = _t(tr, tr.TR_BF16, 1, 4, 100, 64, 3)
+    assert lib.tr_paged_attn_workspace_bytes(*_refs(q, pages[0]), 1 << 16, 64) > 0
