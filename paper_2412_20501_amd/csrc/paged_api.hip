@@ -244,8 +244,9 @@ tr_status tr_cache_read(const tr_tensor* k_pages_, const tr_tensor* v_pages_, co
 }
 
 size_t tr_paged_attn_workspace_bytes(const tr_tensor* q, const tr_tensor* k_pages, int64_t n_seqs, int64_t max_pages) {
-  if (!q || !k_pages || q->S < 0 || q->S > kMaxKeys || q->H < 0 || q->H > INT32_MAX || k_pages->H < 1 || q->H % k_pages->H || (q->D != 64 && q->D != 128)) return 0;
-  if (k_pages->S < 16 || n_seqs < 0 || max_pages < 0 || max_pages > kMaxKeys / k_pages->S || n_seqs > kMaxAttended || q->S * q->H >= ((int64_t)1 << 31)) return 0;
+  if (!q || !k_pages || q->dtype != TR_BF16 || q->B != 1 || q->S < 0 || q->S > kMaxKeys || q->H < 0 || q->H > INT32_MAX || (q->D != 64 && q->D != 128)) return 0;
+  if ((k_pages->dtype != TR_BF16 && k_pages->dtype != TR_F8E4M3) || k_pages->B < 0 || k_pages->H < 1 || q->H % k_pages->H || k_pages->D != q->D || k_pages->S < 16 || k_pages->S % 16) return 0;
+  if (n_seqs < 0 || n_seqs > kMaxAttended || max_pages < 0 || max_pages > kMaxKeys / k_pages->S || q->S * q->H >= ((int64_t)1 << 31)) return 0;
   if (q->S == 0 || q->H == 0 || n_seqs == 0) return 0;
   const tr::PagedLaunch l = tr::paged_launch(q->S, n_seqs, max_pages * k_pages->S, (int)k_pages->H, (int)(q->H / k_pages->H), (int)q->D, k_pages->dtype == TR_F8E4M3);
   int64_t floats = 0;

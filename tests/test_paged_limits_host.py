@@ -61,3 +61,21 @@ def test_more_sequences_than_an_attention_call_takes(tr):
     assert st == 0 and need == 0
     q = _t(tr, tr.TR_BF16, 1, 4, 100, 64, 3)
     assert lib.tr_paged_attn_workspace_bytes(*_refs(q, pages[0]), 1 << 16, 64) > 0
+
+
+def test_workspace_bytes_of_calls_that_are_none(tr):
+    """0 for types and shapes that tr_paged_attn refuses."""
+    lib = tr.raw_lib()
+
+    def need(q=None, pages=None, n=3, max_pages=64):
+        a = dict(dtype=tr.TR_BF16, B=1, H=4, S=100, D=64)
+        b = dict(dtype=tr.TR_F8E4M3, B=10, H=2, S=16, D=64)
+        a.update(q or {})
+        b.update(pages or {})
+        return lib.tr_paged_attn_workspace_bytes(*_refs(*(_t(tr, x["dtype"], x["B"], x["H"], x["S"], x["D"], i) for i, x in enumerate((a, b)))), n, max_pages)
+    assert need() > 0 and need(pages=dict(dtype=tr.TR_BF16)) > 0
+    for q in (dict(dtype=tr.TR_F32), dict(dtype=tr.TR_F8E4M3), dict(B=2), dict(B=0), dict(D=96), dict(D=128), dict(H=3)):
+        assert need(q=q) == 0, q
+    for pages in (dict(dtype=tr.TR_F32), dict(dtype=tr.TR_F8E8M0), dict(dtype=7), dict(D=128), dict(S=24), dict(S=8), dict(B=-1), dict(H=0)):
+        assert need(pages=pages) == 0, pages
+    assert need(n=-1) == 0 and need(max_pages=-1) == 0
