@@ -52,21 +52,6 @@ struct PagedParams {
   float* part_lse; // [slots][rows of a tile]
 };
 
-// How a call is launched: one launch for each class of sequences.
-// Waves a SIMD of the kernel for tiles of 16 * rt rows, which are workgroups (of four waves) a compute unit.
-constexpr int paged_few_waves(int D, bool f8, int rt) { return D == 128 ? (rt == 1 && f8 ? 3 : 2) : rt == 1 ? 4 : 3; }
-constexpr int kManyRows = 256;   // rows of the tiles of sequences with many
-struct PagedLaunch {
-  int n;
-  struct Part {
-    RowClass rows;
-    Share share;     // where a workspace is there
-    int64_t tiles;   // of all sequences and K/V heads, at most
-    int64_t parts;   // of a tile, at most
-    int64_t floats(int D) const { return (int64_t)share.slots(tiles) * rows.tile * (D + 1); }   // of the workspace
-  } part[2];
-};
-PagedLaunch paged_launch(int64_t tokens, int64_t n_seqs, int64_t max_keys, int Hkv, int gq, int D, bool f8);
 // p without what belongs to a launch (rows, share, scratch); workspace: null or the floats of all parts
 hipError_t launch_paged_attn(PagedParams& p, const PagedLaunch& l, int D, bool f8, float* workspace, hipStream_t stream);
 

@@ -35,8 +35,7 @@ hipError_t launch_out(PagedParams& p, const PagedLaunch& l, float* workspace, hi
     p.part_lse = workspace ? workspace + (int64_t)p.slots * c.rows.tile * D : nullptr;
     if (workspace) workspace += c.floats(D);
     // Workgroups beyond those that have an item cost a microsecond for every four hundred.  (An eighth of the items for every XCD, rounded up.)
-    const int64_t most = std::min(c.tiles + p.share.most(), c.tiles * (p.share.most() > 0 ? c.parts : 1));
-    const dim3 items((unsigned)((most + 7) / 8 * 8));
+    const dim3 items((unsigned)((c.items(p.share) + 7) / 8 * 8));
     hipError_t e;
     if (c.rows.tile == kManyRows) e = launch_lds(paged_many_kernel<D, F8, OUT_F32>, raised[0], items, dim3(512), Tile<D>::LDS, stream, p);
     else if (c.rows.tile == 32) e = launch_lds(paged_few_kernel<D, F8, 2, OUT_F32>, raised[1], items, dim3(256), Few<D, F8, 2, 4>::LDS, stream, p);

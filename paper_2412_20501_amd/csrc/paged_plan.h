@@ -1,4 +1,4 @@
-// What the kernels on a paged cache read from the arrays of a tr_sequences, and how a launch's keys are shared out.  Plain C++: constexpr
+// What the kernels on a paged cache read from the arrays of a tr_sequences, how a launch's keys are shared out, and the launches of a call.  Plain C++: constexpr
 // functions are both the host's and the device's, so the bounds that keep every access inside the caller's arrays are tested on the host.
 #pragma once
 #include <stdint.h>
@@ -118,6 +118,55 @@ constexpr int parts_of(int keys, int part) { return keys <= part ? 1 : (keys - 1
 constexpr int64_t most_tiles(int64_t tokens, int64_t n_seqs, int64_t group, RowClass c) {
   const int64_t rows = tokens * group, some = rows / (c.over + 1), full = c.most <= c.tile ? n_seqs : rows / c.tile + n_seqs;
   return some < full ? some : full;
+}
+
+// How a call is launched: one launch for each class of sequences.
+// Waves a SIMD of the kernel for tiles of 16 * rt rows, which are workgroups (of four waves) a compute unit.
+constexpr int paged_few_waves(int D, bool f8, int rt) { return D == 128 ? (rt == 1 && f8 ? 3 : 2) : rt == 1 ? 4 : 3; }
+constexpr int kManyRows = 256;   // rows of the tiles of sequences with many
+struct PagedLaunch {
+  int n;
+  struct Part {
+    RowClass rows;
+    Share share;     // where a workspace is there
+    int64_t tiles;   // of all sequences and K/V heads, at most
+    int64_t parts;   // of a tile, at most
+    // Workgroups with an item, at most, where the keys are shared out by `with` (the share above, or none).
+    int64_t items(const Share& with) const {
+      const int64_t cut = tiles + with.most(), whole = tiles * (with.most() > 0 ? parts : 1);
+      return cut < whole ? cut : whole;
+    }
+    int64_t floats(int D) const { return (int64_t)share.slots(tiles) * rows.tile * (D + 1); }   // of the workspace
+  } part[2];
+};
+// The launches of a call.  The lengths are not known here, so it goes by the average rows of a sequence and K/V head: up to 32, sequences are taken to be
+// of single tokens and drafts, and workgroups of 16 or 32 rows serve them all; a lone sequence of more is one of many rows; several are a mixture,
+// a launch for either kind.
+inline PagedLaunch paged_launch(int64_t tokens, int64_t n_seqs, int64_t max_keys, int Hkv, int gq, int D, bool f8) {
+  PagedLaunch l;
+  const int64_t rows = tokens * gq;
+  constexpr int any = 0x7fffffff;
+  const RowClass few16 = {16, 0, any}, few32 = {32, 0, any}, many = {kManyRows, 0, any};
+  const int few = gq <= 4 ? 16 : 32;   // rows of few tokens in a mixture: 16 / gq tokens (4 at groups of 4), 32 / gq beyond (4 at 8, 2 at 16, none above 32)
+  const RowClass only_few = {few, 0, few}, only_many = {kManyRows, few, any};
+  const bool mixed = rows > 32 * n_seqs && n_seqs > 1;
+  l.n = mixed ? 2 : 1;
+  l.part[0].rows = mixed ? only_few : rows <= 16 * n_seqs ? few16 : rows <= 32 * n_seqs ? few32 : many;
+  l.part[1].rows = only_many;
+  for (int i = 0; i < l.n; i++) {
+    PagedLaunch::Part& c = l.part[i];
+    c.tiles = most_tiles(tokens, n_seqs, gq, c.rows) * Hkv;
+    // Workgroups that the registers of each kernel allow a compute unit; what an item, the fold and its parts cost, measured.  A second round only
+    // for launches of few rows that may have more row tiles than a part of the first: the launch has workgroups for all that its plan may choose, and
+    // those without an item cost 2 us a round of theirs (a mixture of 527 tokens of 16 sequences 99 us with 1300 of them, 108 with 3800).
+    const int per_unit = c.rows.tile == kManyRows ? 1 : paged_few_waves(D, f8, c.rows.tile / 16);
+    const int rounds = c.rows.tile == kManyRows || 2 * c.tiles <= kUnits * per_unit ? 1 : 2;
+    const Share cut = c.rows.tile == kManyRows ? Share{1, 1, 20, 32, 2} : Share{per_unit, rounds, 36, 64, 2};
+    const int64_t two_steps = (max_keys + 2 * kPartStep - 1) / (2 * kPartStep);
+    c.parts = two_steps < 1 ? 1 : two_steps;
+    c.share = c.parts == 1 ? Share{0, 0, 0, 0, 0} : cut;
+  }
+  return l;
 }
 
 }  // namespace tr

@@ -7,7 +7,7 @@ import pytest
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 
 
-@pytest.mark.parametrize("name,ok", [("paged_long_check", "long keys ok")])
+@pytest.mark.parametrize("name,ok", [("paged_long_check", "long keys ok"), ("paged_launch_check", "launches ok")])
 def test_host_checks(tmp_path, name, ok):
     exe = str(tmp_path / name)
     subprocess.run(["g++", "-O1", "-std=c++17", "-Wall", "-Wextra", "-Werror", "-fsanitize=address,undefined", "-I",
