@@ -75,12 +75,11 @@ __device__ __forceinline__ Plan make_plan(const PagedParams& p) {
     for (int b0 = 0; b0 < plan.n; b0 += 64) {
       const Sequence q = lane_sequence(p, plan, b0);
       const int n = tiles_of(q.n * p.gq, p.rows);
-      work = add_work(work, n, steps_of(q.len));
+      work += (int64_t)n * steps_of(q.len);
       tiles += n;
       if (n > 0) longest = max(longest, steps_of(q.len));
     }
-    work = wave_sum(work);
-    work = work < kMostWork ? work * p.Hkv : 0;   // (0: nothing is cut)
+    work = wave_sum(work) * p.Hkv;
     tiles = wave_sum(tiles) * p.Hkv;
     longest = wave_max(longest);
   }

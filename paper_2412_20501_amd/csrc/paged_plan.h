@@ -73,15 +73,12 @@ constexpr int ceil_div(int n, int d) {   // of n < 2^24: the float quotient is a
   const int q = (int)((float)n / (float)d);
   return q * d < n ? q + 1 : q;
 }
-// work plus that of `tiles` row tiles of steps_of(keys) = steps, kMostWork for that and more: no call whose sequences do not overlap reaches it before its rows
-// fill the chip many times over, so that nothing is cut there.  (tiles below 2^27, steps up to 2^23.)
-constexpr int64_t kMostWork = (int64_t)1 << 39;
-constexpr int64_t add_work(int64_t work, int64_t tiles, int steps) { return work + tiles * steps < kMostWork ? work + tiles * steps : kMostWork; }
 constexpr int part_keys(int64_t work, int64_t tiles, int longest, const Share& share) {
 #if defined(__clang__)
 #pragma clang fp contract(off)
 #endif
-  if (share.most_per_unit <= 0 || work <= 0 || tiles >= (1 << 24)) return kPosLimit;   // (as many keys as a sequence has at most)
+  // (As many keys as a sequence has at most.  No grid has 2^24 tiles: only sequences that overlap do, and for fewer work is below 2^47.)
+  if (share.most_per_unit <= 0 || work <= 0 || tiles >= (1 << 24)) return kPosLimit;
   int unit = 0;   // work is counted in 2^unit steps, rounded up, which 24 bits hold (one token of 32 heads on 2^21 keys 1.2 ms; left uncut 22.5)
   while (work >= (1 << 24)) {
     work = (work + 1) >> 1;

@@ -57,7 +57,7 @@ int main() {
         for (int b = 0; b < n; b++) {
           const tr::Sequence q = tr::sequence(s, b);
           const int t = tr::tiles_of(q.n * gq, c.rows);
-          work = tr::add_work(work, t, tr::steps_of(q.len));
+          work += (int64_t)t * tr::steps_of(q.len);
           tiles += t;
           if (t > 0 && tr::steps_of(q.len) > longest) longest = tr::steps_of(q.len);
         }

@@ -34,13 +34,10 @@ int main() {
     if (tiles / 2 >= share.most()) EXPECT(part == tr::kPosLimit);   // 800 / 2 >= 256: there is no room for parts beside the tiles' halves
     else EXPECT(part < keys / 8);
   }
-  // work that only sequences which overlap can have
+  // more tiles than a grid has: only sequences that overlap have them
   const tr::Share share = shares[0];
-  const int tiles = 1, keys = 1 << 30;
-  int64_t sum = 0;
-  for (int i = 0; i < 100000; i++) sum = tr::add_work(sum, 1 << 27, 1 << 23);
-  EXPECT(sum == tr::kMostWork && tr::add_work(0, 3, 5) == 15);
-  EXPECT(tr::part_keys(tr::kMostWork, (int64_t)1 << 40, 1 << 23, share) == tr::kPosLimit);
+  const int tiles = 1 << 24, keys = 1 << 30;
+  for (int64_t work : {(int64_t)1, (int64_t)1 << 40, (int64_t)1 << 62, (int64_t)-5}) EXPECT(tr::part_keys(work, tiles, tr::steps_of(keys), share) == tr::kPosLimit);
   printf("long keys ok\n");
   return 0;
 }
