@@ -6,7 +6,6 @@ namespace {
 
 typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
 typedef unsigned u32x2 __attribute__((ext_vector_type(2)));
-typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 
 constexpr int kThreads = 256;
 
@@ -31,12 +30,8 @@ struct Rows {
 __device__ __forceinline__ int64_t from(int64_t x, int lane) {
   return (int64_t)(((uint64_t)(unsigned)__shfl((int)(x >> 32), lane) << 32) | (unsigned)__shfl((int)x, lane));
 }
-// (head, K or V), which lie next to each other, and the 16 rows of this wave.
+// The first of the 16 rows of this wave, its head, and whether it has V's.
 struct WaveRows { int rows, head, is_v; };
-__device__ __forceinline__ WaveRows wave_rows(const CacheCopyParams& p, int64_t wave) {
-  const int group = divide(p.by_heads, (int)wave), other = (int)wave - group * 2 * p.heads;
-  return WaveRows{group * 16, other < p.heads ? other : other - p.heads, other >= p.heads};
-}
 
 template <int D, bool F8>
 __global__ void __launch_bounds__(kThreads) cache_write_kernel(const CacheCopyParams p) {

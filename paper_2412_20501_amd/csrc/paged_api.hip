@@ -9,7 +9,6 @@ using tr::check_tensor;
 using tr::check_typed;
 using tr::check_written;
 using tr::elem_bytes;
-using tr::extent_elems;
 using tr::fail;
 using tr::overlaps;
 
