@@ -286,6 +286,7 @@ size_t tr_ring_attn_workspace_bytes(const tr_tensor* q, int n_chunks);
  *                       token by token, K and V may lie side by side in one array).
  *   k_scales, v_scales  [n_pages, Hkv, page_size] e8m0, with e4m3 pages only (else NULL): one scale for a key's row of D values.  Same
  *                       strides for both, stride_s 1, pointer and other strides multiples of 16.  A value is e4m3 * 2^(scale - 127).
+ *                       What is written must be apart from first to last element: scales do not lie between the pages.
  * Key c of sequence b lies on page page_table[b][c / page_size], in slot c mod page_size.  Several sequences may share pages
  * that are read.  An entry that is no page (< 0 or >= n_pages) stands for keys that are not there: they are read as masked and
  * written nowhere, and nothing outside the arrays is touched.
@@ -308,7 +309,7 @@ typedef struct {
 
 /*
  * Writes K and V of the new tokens into the cache: token i of sequence b as key q_pos[b] + i, if 0 <= q_pos[b] + i < kv_len[b].
- *   k, v [1,Hkv,S,D] bf16, strides multiples of 8 elements
+ *   k, v [1,Hkv,S,D] bf16, of the same strides, multiples of 8 elements
  * bf16 pages take the rows as they are.  e4m3 pages: the scale of a row is the smallest power of two, 2^-126 at least, that brings its largest
  * finite magnitude down to 448 or less (1 for a row of zeros); the values are divided by it, which is exact, and rounded to
  * nearest even.  An infinity or NaN is stored as NaN.  Each new token needs a slot of its own: two rows of one call in the same slot of a page
@@ -319,7 +320,7 @@ tr_status tr_cache_write(const tr_tensor* k, const tr_tensor* v, const tr_tensor
 
 /*
  * Reads the cache back as dense tensors, what tr_block_attn takes or another device is sent: row s of sequence b is key first + s.
- *   k, v [n_seqs,Hkv,S,D] bf16 (written), strides multiples of 8 elements; first >= 0
+ *   k, v [n_seqs,Hkv,S,D] bf16 (written), of the same strides, multiples of 8 elements; first >= 0
  * Exact: bf16 holds every e4m3 value times a power of two (down to its own smallest values, 2^-133, below which it rounds, and
  * below 2^128, from where on they are infinities).
  * Rows of keys that are not there (first + s >= kv_len[b], no page) are left as they were.  q_start and q_pos are not used.
@@ -335,7 +336,7 @@ tr_status tr_cache_read(const tr_tensor* k_pages, const tr_tensor* v_pages, cons
  *   lse[0,h,q_start[b]+i]   = ln sum_c exp(scale * <q[0,h,q_start[b]+i,:], K_c>)
  *   q [1,Hq,S,D] bf16      out [1,Hq,S,D] bf16 or fp32 (written)      lse [1,Hq,S] fp32 (written)
  * A block result like tr_block_attn's: results on the parts of a cache that several devices hold are folded by tr_merge or
- * tr_merge_n.  A token that sees no key gets out = 0, lse = -inf.  What lies at masked keys (infinities, NaN, slots never written) reaches no result.
+ * tr_merge_n.  As there, a row that sees a NaN or +infinity among its scores has out = NaN and lse = -inf.  A token that sees no key gets out = 0, lse = -inf.  What lies at masked keys (infinities, NaN, slots never written) reaches no result.
  * Arithmetic as tr_block_attn's; e4m3 values enter it exactly.  Weights of up to 2^20 times V are summed up in fp32, so results are finite where
  * the largest |V| times the number of keys is at most 2^107.
  * At most 2^16 sequences.  The work is found on the device in time that grows with their square: next to nothing for a few hundred, as much as the attention on

@@ -16,7 +16,7 @@ namespace {
 
 constexpr int64_t kMaxKeys = (int64_t)1 << 30;
 // Sequences of an attention call.  Its workgroups each go through all of them, 64 at a time in about half a microsecond, so that the time for it grows with their square: tokens of as many sequences with
-// 200 keys, on 8 K/V heads, 51 us for 256, 0.36 ms for 1024 (twice what the keys take), 3.5 for 4096, 52 for 16384.
+// 200 keys, on 8 K/V heads, 50 us for 256, 0.37 ms for 1024 (twice what the keys take), 3.6 for 4096, 53 for 16384.
 constexpr int64_t kMaxAttended = (int64_t)1 << 16;
 constexpr int64_t kMaxGroups = (int64_t)1 << 24;   // workgroups of 256 threads of a grid's dimension, which holds fewer than 2^32 threads
 

@@ -38,10 +38,10 @@ __device__ __forceinline__ float halves_sum(float x) {
 // and of V), on rows that are (token, query head of a K/V head) pairs and with tiles that are gathered from pages: a wave's share of a tile, 8 keys
 // at D 128 and 16 at D 64, lies on one page, whose address is found with scalar loads a tile ahead.  bf16 goes straight from memory into LDS, e4m3 through
 // registers, where each value is converted once for all 256 rows.  Bound: MFMA and power, as there.  An item takes 1.1 us for 64 keys at D 128 on an idle chip (1.7 on a
-// full one), 1.55 for 128 at D 64, and 11 and 8 for its set-up and epilogue; 2048 tokens of 32 heads behind 30K keys in 8 bits 1.13 to 1.19 PFLOP/s.
+// full one), 1.55 for 128 at D 64, and 11 and 8 for its set-up and epilogue; 2048 tokens of 32 heads behind 30K keys in 8 bits 1.06 to 1.19 PFLOP/s (cards differ).
 //
 // What is rare takes another way: an item with a page that is none, or with an infinity or NaN in V at a key that only some of its rows see, is computed
-// by few_rows, 16 rows at a time, which holds nothing of either against it.
+// by few_rows, 16 rows at a time, which holds nothing of either against it and takes five times as long (500 tokens on 12500 keys 114 us, with one entry that is no page 619).
 template <int D>
 struct Tile {
   static constexpr int RB = 2 * D, BN = D == 64 ? 128 : 64, NS = 4, TILE_BYTES = BN * RB, ROWS = kManyRows;
@@ -295,6 +295,7 @@ __device__ __forceinline__ bool tile_rows(const PagedParams& p, const Item& w, i
         const int e = g * EPM + k;
         if (e & 1) {
           ps1 += ex[e];
+          // (bf16 is what the second product takes: a weight is off by up to 2^-8 of itself, its sum and the results are held in 32 bits)
           asm volatile("v_cvt_pk_bf16_f32 %0, %1, %2" : "=v"(pw[e >> 1]) : "v"(ex[e - 1]), "v"(ex[e]));
         } else {
           ps0 += ex[e];
