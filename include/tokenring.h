@@ -354,6 +354,70 @@ tr_status tr_paged_attn(const tr_tensor* q, const tr_tensor* k_pages, const tr_t
 size_t tr_paged_attn_workspace_bytes(const tr_tensor* q, const tr_tensor* k_pages, int64_t n_seqs, int64_t max_pages);
 
 /*
+ * Attention of drafted tokens that form a tree (or several branches behind one text), each on the keys in front of the drafts and on its own branch:
+ * tr_paged_attn, but token i of sequence b sees the keys c < q_pos[b], and of the keys q_pos[b] + j, which its n drafted tokens stand at, those whose
+ * bit j is set in row q_start[b] + i of the tree, for j < n (its own bit among them: bits say all).  Keys from q_pos[b] + n on are seen by none.
+ * Bits beyond the words of a row count as not set.  Everything else (arguments, rows that see no key, what is masked, workspace) as in tr_paged_attn, with
+ * the workspace's size from tr_paged_attn_tree_workspace_bytes().
+ */
+typedef struct {
+  const int32_t* bits;   /* [tokens][words], rows stride elements apart: bit j of a row is bit j mod 32 of word j / 32.  Read by the kernels */
+  int64_t tokens, words; /* tokens: S of q; 1 <= words <= 2^15 */
+  int64_t stride;        /* >= words; 0 if all rows are one */
+} tr_tree;
+tr_status tr_paged_attn_tree(const tr_tensor* q, const tr_tensor* k_pages, const tr_tensor* v_pages, const tr_tensor* k_scales,
+                             const tr_tensor* v_scales, const tr_sequences* seqs, const tr_tree* tree, float scale, const tr_tensor* out,
+                             const tr_tensor* lse, void* workspace, size_t workspace_bytes, void* hip_stream);
+/* (0 on invalid arguments, and where no keys would be shared out.) */
+size_t tr_paged_attn_tree_workspace_bytes(const tr_tensor* q, const tr_tensor* k_pages, int64_t n_seqs, int64_t max_pages);
+
+/*
+ * The attention weight that every cached key gets from the new tokens, added up for an eviction: for key c of sequence b and K/V head g, over the
+ * tokens i of sequence b that see it (c <= q_pos[b] + i with causal != 0) and the query heads h of g,
+ *   weights[page][g][slot] += sum exp(scale * <q[0,h,q_start[b]+i,:], K_c> - lse[0,h,q_start[b]+i])
+ *   q [1,Hq,S,D] bf16      lse [1,Hq,S] fp32: what tr_paged_attn gave, or, where several devices hold parts of a cache, what tr_merge made of it
+ *   k_pages, k_scales as in tr_paged_attn      weights [n_pages,Hkv,page_size] fp32 (read + written), strides as the scales': stride_s 1, pointer and other
+ *   strides multiples of 16 bytes
+ * fresh != 0: the keys of the new tokens themselves (c = q_pos[b] + i, those that tr_cache_write has just written) start from 0 instead of what their slots hold.
+ * A token whose lse is not finite (it saw nothing, or a NaN) adds nothing; what its row of q or a masked key holds reaches no weight.  Keys that no token sees keep their weight, slots
+ * that hold no key of a sequence with new tokens are not touched.  Scores and sums are in fp32.  A page that several sequences of the call share gets the sum of
+ * one of them (or a mixture): weigh such sequences in calls of their own.  The result is bitwise reproducible.  At most 2^16 sequences.  Nothing is allocated; may be captured.
+ */
+tr_status tr_cache_weigh(const tr_tensor* q, const tr_tensor* lse, const tr_tensor* k_pages, const tr_tensor* k_scales, const tr_sequences* seqs,
+                         int causal, float scale, int fresh, const tr_tensor* weights, void* hip_stream);
+
+/* Keys of every sequence, device arrays. */
+typedef struct {
+  int32_t* keys;             /* [n_seqs][heads][max_keys]: numbers of keys, rising, the last dimension dense */
+  int32_t* count;            /* [n_seqs]: of each sequence's keys in a list */
+  int64_t heads;             /* Hkv, or (tr_cache_keep only) 1: the same keys for every head */
+  int64_t max_keys;          /* 0 .. 2^30 */
+  int64_t stride_b, stride_h;
+} tr_kept;
+
+/*
+ * Chooses the keys that stay: of each sequence and K/V head the first `first` keys, the last `last`, and of those between them the ones with the largest
+ * weights, kept->max_keys in all or, if the sequence has fewer, all of its keys.  Of equal weights (0 and -0 among them) the lower key number stays.  A NaN counts as more
+ * than any number, a key that is on no page as less than any.
+ *   first, last >= 0, first + last <= max_keys (TR_ERR_SHAPE)
+ *   kept: keys (written; entries from count on are left as they were) and count[b] = min(kv_len[b], max_keys) (written); heads = Hkv
+ * weights as in tr_cache_weigh (read).  q_start and q_pos are not used.  Nothing is allocated; may be captured.
+ */
+tr_status tr_cache_select(const tr_tensor* weights, const tr_sequences* seqs, int64_t first, int64_t last, const tr_kept* kept, void* hip_stream);
+
+/*
+ * Moves kept keys together: key kept->keys[b][h][i] of sequence b becomes key start[b] + i, for i < count[b] (taken as 0 .. max_keys), with K, V, their scales and, if given, their
+ * weights, in place.  start: [n_seqs] int32 or NULL for zeros.  An eviction moves what tr_cache_select chose; an accepted path of a tree is moved behind the
+ * text with start = number of the first drafted token's key and one list for all heads.  The sequence then has start[b] + count[b] keys: kv_len is the caller's to change.
+ *   A list must rise, and no key may move up: keys[b][h][i] >= start[b] + i.  An entry that moves up, a key or a place that is not 0 <= .. < kv_len[b], or that is on no
+ *   page, is skipped: its place is left as it was.  Of a list that does not rise, places hold what any of the entries in question had, nothing else is touched.
+ *   No page may belong to two sequences of the call that move keys.
+ * weights as in tr_cache_weigh, or NULL.  q_start and q_pos are not used.  Nothing is allocated; may be captured.
+ */
+tr_status tr_cache_keep(const tr_tensor* k_pages, const tr_tensor* v_pages, const tr_tensor* k_scales, const tr_tensor* v_scales, const tr_tensor* weights,
+                        const tr_sequences* seqs, const tr_kept* kept, const int32_t* start, void* hip_stream);
+
+/*
  * Measurement aid (no operation of the paper): arms two hipEvent_t handles (either may be
  * NULL; both NULL disarms) for the calling thread.  The next kernel any entry point launches
  * from this thread carries them in its dispatch: start_event then holds the time the kernel

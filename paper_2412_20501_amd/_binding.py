@@ -42,6 +42,19 @@ class TrSequences(ctypes.Structure):
     ]
 
 
+class TrTree(ctypes.Structure):
+    """Mirror of `tr_tree` in include/tokenring.h."""
+    _fields_ = [("bits", ctypes.c_void_p), ("tokens", ctypes.c_int64), ("words", ctypes.c_int64), ("stride", ctypes.c_int64)]
+
+
+class TrKept(ctypes.Structure):
+    """Mirror of `tr_kept` in include/tokenring.h."""
+    _fields_ = [
+        ("keys", ctypes.c_void_p), ("count", ctypes.c_void_p),
+        ("heads", ctypes.c_int64), ("max_keys", ctypes.c_int64), ("stride_b", ctypes.c_int64), ("stride_h", ctypes.c_int64),
+    ]
+
+
 class TokenRingError(RuntimeError):
     def __init__(self, status: int, message: str):
         super().__init__(f"{STATUS_NAMES.get(status, status)}: {message}")
@@ -100,6 +113,17 @@ def _load():
     lib.tr_paged_attn.restype = ctypes.c_int
     lib.tr_paged_attn_workspace_bytes.argtypes = [P, P, ctypes.c_int64, ctypes.c_int64]
     lib.tr_paged_attn_workspace_bytes.restype = ctypes.c_size_t
+    T, K = ctypes.POINTER(TrTree), ctypes.POINTER(TrKept)
+    lib.tr_paged_attn_tree.argtypes = [P, P, P, P, P, G, T, ctypes.c_float, P, P, ctypes.c_void_p, ctypes.c_size_t, ctypes.c_void_p]
+    lib.tr_paged_attn_tree.restype = ctypes.c_int
+    lib.tr_paged_attn_tree_workspace_bytes.argtypes = [P, P, ctypes.c_int64, ctypes.c_int64]
+    lib.tr_paged_attn_tree_workspace_bytes.restype = ctypes.c_size_t
+    lib.tr_cache_weigh.argtypes = [P, P, P, P, G, ctypes.c_int, ctypes.c_float, ctypes.c_int, P, ctypes.c_void_p]
+    lib.tr_cache_weigh.restype = ctypes.c_int
+    lib.tr_cache_select.argtypes = [P, G, ctypes.c_int64, ctypes.c_int64, K, ctypes.c_void_p]
+    lib.tr_cache_select.restype = ctypes.c_int
+    lib.tr_cache_keep.argtypes = [P, P, P, P, P, G, K, ctypes.c_void_p, ctypes.c_void_p]
+    lib.tr_cache_keep.restype = ctypes.c_int
     lib.tr_last_error.argtypes = []
     lib.tr_last_error.restype = ctypes.c_char_p
     lib.tr_version.argtypes = []
@@ -304,8 +328,48 @@ def tr_paged_attn(q, k_pages, v_pages, page_table, kv_len, q_start, causal, scal
     _check(_native.paged_attn(q, k_pages, v_pages, page_table, kv_len, q_start, causal, scale, out, lse, k_scales, v_scales, q_pos, workspace, stream))
 
 
-def tr_paged_attn_workspace_bytes(q, k_pages, page_table) -> int:
-    """Bytes of a workspace for tr_paged_attn on tensors of these types and shapes."""
+def _workspace_bytes(entry, q, k_pages, page_table) -> int:
     if page_table.dim() != 2:
         raise ValueError("page_table must have 2 dimension(s), the last one dense")
-    return int(_lib.tr_paged_attn_workspace_bytes(ctypes.byref(_shape(q)), ctypes.byref(_shape(k_pages)), *page_table.shape))
+    return int(entry(ctypes.byref(_shape(q)), ctypes.byref(_shape(k_pages)), *page_table.shape))
+
+
+def tr_paged_attn_workspace_bytes(q, k_pages, page_table) -> int:
+    """Bytes of a workspace for tr_paged_attn on tensors of these types and shapes."""
+    return _workspace_bytes(_lib.tr_paged_attn_workspace_bytes, q, k_pages, page_table)
+
+
+def tr_paged_attn_tree(q, k_pages, v_pages, page_table, kv_len, q_start, tree, scale, out, lse, k_scales=None, v_scales=None, q_pos=None,
+                       workspace=None, stream=None):
+    """tr_paged_attn for drafted tokens that form a tree: each sees the keys in front of the drafts and the drafts whose bits are set (see tokenring.h).
+
+    `tree`: int32 [S, words], bit j of a token's row (bit j % 32 of word j // 32): it sees the j-th new token of its sequence.
+    `workspace`: None, or a caller-owned device tensor of at least tr_paged_attn_tree_workspace_bytes(q, k_pages, page_table) bytes.
+    """
+    _check(_native.paged_attn_tree(q, k_pages, v_pages, page_table, kv_len, q_start, tree, scale, out, lse, k_scales, v_scales, q_pos, workspace, stream))
+
+
+def tr_paged_attn_tree_workspace_bytes(q, k_pages, page_table) -> int:
+    """Bytes of a workspace for tr_paged_attn_tree on tensors of these types and shapes."""
+    return _workspace_bytes(_lib.tr_paged_attn_tree_workspace_bytes, q, k_pages, page_table)
+
+
+def tr_cache_weigh(q, lse, k_pages, page_table, kv_len, q_start, causal, scale, weights, fresh=True, k_scales=None, q_pos=None, stream=None):
+    """weights [n_pages,Hkv,page_size] fp32 += the attention weight that each key gets from the new tokens q [1,Hq,S,D], by their lse [1,Hq,S] (see tokenring.h).
+
+    `fresh`: the new tokens' own keys start from 0 instead of what their slots hold.
+    """
+    _check(_native.cache_weigh(q, lse, k_pages, page_table, kv_len, q_start, causal, scale, weights, fresh, k_scales, q_pos, stream))
+
+
+def tr_cache_select(weights, page_table, kv_len, first, last, keys, count, stream=None):
+    """keys [n_seqs,Hkv,N], count [n_seqs] (int32) <- of each sequence and K/V head the first, the last and between them the heaviest keys, N in all (see tokenring.h)."""
+    _check(_native.cache_select(weights, page_table, kv_len, first, last, keys, count, stream))
+
+
+def tr_cache_keep(k_pages, v_pages, page_table, kv_len, keys, count, start=None, k_scales=None, v_scales=None, weights=None, stream=None):
+    """Key keys[b,h,i] of sequence b becomes key start[b] + i, i < count[b], in place, with its scales and weight (see tokenring.h).
+
+    keys: int32 [n_seqs,Hkv,N], or [n_seqs,1,N] for all heads alike, rising and moving nothing to a larger number; start: int32 [n_seqs] or None for zeros.
+    """
+    _check(_native.cache_keep(k_pages, v_pages, page_table, kv_len, keys, count, start, k_scales, v_scales, weights, stream))

@@ -22,8 +22,8 @@ CSRC = os.path.join(PKG_DIR, "csrc")
 INCLUDE = os.path.join(ROOT, "include")
 LIB_PATH = os.path.join(PKG_DIR, "libtokenring.so")
 BINDING_PATH = os.path.join(PKG_DIR, "_native.so")   # Python module over it
-SOURCES = ["api.hip", "merge.hip", "block_attn.hip", "paged_api.hip", "cache.hip", "paged_attn.hip"] + [f"block_attn_d{d}_{r}rows.hip" for d in (128, 64) for r in (256, 128, 64)] + \
-    [f"paged_attn_d{d}_{t}.hip" for d in (128, 64) for t in ("bf16", "e4m3")]
+SOURCES = ["api.hip", "merge.hip", "block_attn.hip", "paged_api.hip", "cache.hip", "paged_attn.hip", "evict_api.hip", "weigh.hip", "evict.hip"] + [f"block_attn_d{d}_{r}rows.hip" for d in (128, 64) for r in (256, 128, 64)] + \
+    [f"paged_{kind}_d{d}_{t}.hip" for kind in ("attn", "tree") for d in (128, 64) for t in ("bf16", "e4m3")]
 
 HIPCC_FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",

@@ -369,6 +369,61 @@ PyObject* cache_read(PyObject*, PyObject* const* a, Py_ssize_t n) {   // k_pages
     return nullptr;
   return call([&] { return tr_cache_read(kp.at, vp.at, ks.at, vs.at, &s, first, k.at, v.at, stream); });
 }
+// A workspace: None, or a contiguous tensor.
+bool take_workspace(PyObject* obj, Place& place, void*& ws, size_t& bytes) {
+  ws = nullptr;
+  bytes = 0;
+  if (obj == Py_None) return true;
+  try {
+    const at::Tensor* t = strided(obj, place);
+    if (!t) return false;
+    if (!t->is_contiguous()) {
+      PyErr_SetString(PyExc_ValueError, "the workspace must be contiguous");
+      return false;
+    }
+    ws = t->data_ptr();
+    bytes = (size_t)t->nbytes();
+    return true;
+  } catch (const std::exception& e) {
+    PyErr_SetString(PyExc_RuntimeError, e.what());
+    return false;
+  }
+}
+bool take_tree(PyObject* obj, Place& place, tr_tree& tree) {
+  try {
+    const at::Tensor* t;
+    if (!indices(obj, "tree", 2, -1, place, t)) return false;
+    tree.bits = (const int32_t*)t->data_ptr();
+    tree.tokens = t->size(0);
+    tree.words = t->size(1);
+    tree.stride = t->stride(0);
+    return true;
+  } catch (const std::exception& e) {
+    PyErr_SetString(PyExc_RuntimeError, e.what());
+    return false;
+  }
+}
+bool take_kept(PyObject* keys, PyObject* count, Place& place, int64_t n_seqs, tr_kept& kept) {
+  try {
+    const at::Tensor* t;
+    if (!indices(keys, "keys", 3, -1, place, t)) return false;
+    if (t->size(0) != n_seqs) {
+      PyErr_Format(PyExc_ValueError, "keys must have a list for each of the %lld sequences, not %lld", (long long)n_seqs, (long long)t->size(0));
+      return false;
+    }
+    kept.keys = (int32_t*)t->data_ptr();
+    kept.heads = t->size(1);
+    kept.max_keys = t->size(2);
+    kept.stride_b = t->stride(0);
+    kept.stride_h = t->stride(1);
+    if (!indices(count, "count", 1, n_seqs, place, t)) return false;
+    kept.count = (int32_t*)t->data_ptr();
+    return true;
+  } catch (const std::exception& e) {
+    PyErr_SetString(PyExc_RuntimeError, e.what());
+    return false;
+  }
+}
 // q, k_pages, v_pages, page_table, kv_len, q_start, causal, scale, out, lse, k_scales, v_scales, q_pos, workspace, stream
 PyObject* paged_attn(PyObject*, PyObject* const* a, Py_ssize_t n) {
   Place place;
@@ -376,29 +431,75 @@ PyObject* paged_attn(PyObject*, PyObject* const* a, Py_ssize_t n) {
   tr_sequences s;
   int64_t causal;
   float scale;
-  void *stream, *ws = nullptr;
-  size_t bytes = 0;
+  void *stream, *ws;
+  size_t bytes;
   if (!argc_is(n, 15) || !q.take(a[0], place) || !kp.take(a[1], place) || !vp.take(a[2], place) || !take_sequences(a[3], a[4], a[5], a[12], place, s) ||
       !to_bool(a[6], causal) || !to_float(a[7], scale) || !out.take(a[8], place) || !lse.take(a[9], place) || !ks.take(a[10], place, true) ||
-      !vs.take(a[11], place, true))
+      !vs.take(a[11], place, true) || !take_workspace(a[13], place, ws, bytes) || !to_stream(a[14], stream))
     return nullptr;
-  if (a[13] != Py_None) {
+  return call([&] { return tr_paged_attn(q.at, kp.at, vp.at, ks.at, vs.at, &s, (int)causal, scale, out.at, lse.at, ws, bytes, stream); });
+}
+// the same with a tree in the place of causal
+PyObject* paged_attn_tree(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  Place place;
+  Operand q, kp, vp, out, lse, ks, vs;
+  tr_sequences s;
+  tr_tree tree;
+  float scale;
+  void *stream, *ws;
+  size_t bytes;
+  if (!argc_is(n, 15) || !q.take(a[0], place) || !kp.take(a[1], place) || !vp.take(a[2], place) || !take_sequences(a[3], a[4], a[5], a[12], place, s) ||
+      !take_tree(a[6], place, tree) || !to_float(a[7], scale) || !out.take(a[8], place) || !lse.take(a[9], place) || !ks.take(a[10], place, true) ||
+      !vs.take(a[11], place, true) || !take_workspace(a[13], place, ws, bytes) || !to_stream(a[14], stream))
+    return nullptr;
+  return call([&] { return tr_paged_attn_tree(q.at, kp.at, vp.at, ks.at, vs.at, &s, &tree, scale, out.at, lse.at, ws, bytes, stream); });
+}
+PyObject* cache_weigh(PyObject*, PyObject* const* a, Py_ssize_t n) {   // q, lse, k_pages, page_table, kv_len, q_start, causal, scale, weights, fresh, k_scales, q_pos, stream
+  Place place;
+  Operand q, lse, kp, ks, w;
+  tr_sequences s;
+  int64_t causal, fresh;
+  float scale;
+  void* stream;
+  if (!argc_is(n, 13) || !q.take(a[0], place) || !lse.take(a[1], place) || !kp.take(a[2], place) || !take_sequences(a[3], a[4], a[5], a[11], place, s) ||
+      !to_bool(a[6], causal) || !to_float(a[7], scale) || !w.take(a[8], place) || !to_bool(a[9], fresh) || !ks.take(a[10], place, true) || !to_stream(a[12], stream))
+    return nullptr;
+  return call([&] { return tr_cache_weigh(q.at, lse.at, kp.at, ks.at, &s, (int)causal, scale, (int)fresh, w.at, stream); });
+}
+PyObject* cache_select(PyObject*, PyObject* const* a, Py_ssize_t n) {   // weights, page_table, kv_len, first, last, keys, count, stream
+  Place place;
+  Operand w;
+  tr_sequences s;
+  tr_kept kept;
+  int64_t first, last;
+  void* stream;
+  if (!argc_is(n, 8) || !w.take(a[0], place) || !take_sequences(a[1], a[2], nullptr, nullptr, place, s) || !to_int(a[3], first) || !to_int(a[4], last) ||
+      !take_kept(a[5], a[6], place, s.n_seqs, kept) || !to_stream(a[7], stream))
+    return nullptr;
+  return call([&] { return tr_cache_select(w.at, &s, first, last, &kept, stream); });
+}
+PyObject* cache_keep(PyObject*, PyObject* const* a, Py_ssize_t n) {   // k_pages, v_pages, page_table, kv_len, keys, count, start, k_scales, v_scales, weights, stream
+  Place place;
+  Operand kp, vp, ks, vs, w;
+  tr_sequences s;
+  tr_kept kept;
+  const int32_t* start = nullptr;
+  void* stream;
+  if (!argc_is(n, 11) || !kp.take(a[0], place) || !vp.take(a[1], place) || !take_sequences(a[2], a[3], nullptr, nullptr, place, s) ||
+      !take_kept(a[4], a[5], place, s.n_seqs, kept))
+    return nullptr;
+  if (a[6] != Py_None) {
     try {
-      const at::Tensor* t = strided(a[13], place);
-      if (!t) return nullptr;
-      if (!t->is_contiguous()) {
-        PyErr_SetString(PyExc_ValueError, "the workspace must be contiguous");
-        return nullptr;
-      }
-      ws = t->data_ptr();
-      bytes = (size_t)t->nbytes();
+      const at::Tensor* t;
+      if (!indices(a[6], "start", 1, s.n_seqs, place, t)) return nullptr;
+      start = (const int32_t*)t->data_ptr();
     } catch (const std::exception& e) {
       PyErr_SetString(PyExc_RuntimeError, e.what());
       return nullptr;
     }
   }
-  if (!to_stream(a[14], stream)) return nullptr;
-  return call([&] { return tr_paged_attn(q.at, kp.at, vp.at, ks.at, vs.at, &s, (int)causal, scale, out.at, lse.at, ws, bytes, stream); });
+  if (!ks.take(a[7], place, true) || !vs.take(a[8], place, true) || !w.take(a[9], place, true) || !to_stream(a[10], stream)) return nullptr;
+  return call([&] { return tr_cache_keep(kp.at, vp.at, ks.at, vs.at, w.at, &s, &kept, start, stream); });
 }
 PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t n) {
   if (!argc_is(n, 5)) return nullptr;
@@ -415,7 +516,8 @@ PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t n) {
 #define TR_METHOD(name) {#name, (PyCFunction)(void (*)(void))name, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {TR_METHOD(bind), TR_METHOD(block_attn), TR_METHOD(block_attn_merge), TR_METHOD(block_attn_causal_at), TR_METHOD(merge),
                          TR_METHOD(merge_n), TR_METHOD(ring_attn), TR_METHOD(ring_attn_noalloc), TR_METHOD(ring_attn_sched),
-                         TR_METHOD(ring_attn_blocks), TR_METHOD(cache_write), TR_METHOD(cache_read), TR_METHOD(paged_attn), {nullptr, nullptr, 0, nullptr}};
+                         TR_METHOD(ring_attn_blocks), TR_METHOD(cache_write), TR_METHOD(cache_read), TR_METHOD(paged_attn), TR_METHOD(paged_attn_tree),
+                         TR_METHOD(cache_weigh), TR_METHOD(cache_select), TR_METHOD(cache_keep), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_native", "Calls into libtokenring with torch tensors; status codes come back.", -1, methods,
                       nullptr, nullptr, nullptr, nullptr};
 

@@ -52,8 +52,16 @@ struct PagedParams {
   float* part_lse; // [slots][rows of a tile]
 };
 
+// The same where new tokens see those of the others that their bits say.
+struct TreeParams : PagedParams {
+  const unsigned* tree;    // [tokens][words], rows tree_stride apart
+  int64_t tree_stride;
+  int words;
+};
+
 // p without what belongs to a launch (rows, share, scratch); workspace: null or the floats of all parts
 hipError_t launch_paged_attn(PagedParams& p, const PagedLaunch& l, int D, bool f8, float* workspace, hipStream_t stream);
+hipError_t launch_paged_attn(TreeParams& p, const PagedLaunch& l, int D, bool f8, float* workspace, hipStream_t stream);
 
 #if defined(__HIPCC__)
 // Two e4m3 values (the upper ones of x, if upper) times 2^(scale - 127), as two bf16: the conversion takes the scale as the exponent of a float.  It reads 0 as

@@ -1,6 +1,8 @@
 // Attention of new tokens on a paged cache (tr_paged_attn) for gfx950.
 #pragma once
-#include "paged.h"
+#include <type_traits>
+
+#include "paged_sums.h"
 
 namespace tr {
 namespace {
@@ -23,46 +25,6 @@ constexpr float kSumCap = 0x1p20f;
 // The lengths lie in device memory, so the launch does not know them: it has as many workgroups as the shapes allow work items, and every
 // workgroup finds its own item, by sums over the sequences that each of its waves takes for itself (64 sequences a load).  An item
 // is a row tile of a K/V head of a sequence on one part of the keys (part_keys).
-template <int CONTROL, int ROWS>
-__device__ __forceinline__ int from_lane(int x) { return __builtin_amdgcn_update_dpp(0, x, CONTROL, ROWS, 0xf, false); }   // 0 where no lane is
-__device__ __forceinline__ int wave_scan(int x) {   // sum over the lanes up to and including this one
-  x += from_lane<0x111, 0xf>(x);   // rows of 16 lanes: from 1, 2, 4, 8 below,
-  x += from_lane<0x112, 0xf>(x);
-  x += from_lane<0x114, 0xf>(x);
-  x += from_lane<0x118, 0xf>(x);
-  x += from_lane<0x142, 0xa>(x);   // then a row's last lane to the next row,
-  x += from_lane<0x143, 0xc>(x);   // and the lower half's to the upper
-  return x;
-}
-template <int CONTROL, int ROWS>
-__device__ __forceinline__ int64_t add_from(int64_t x) {
-  return x + (int64_t)(((uint64_t)(unsigned)from_lane<CONTROL, ROWS>((int)(x >> 32)) << 32) | (unsigned)from_lane<CONTROL, ROWS>((int)x));
-}
-__device__ __forceinline__ int64_t wave_sum(int64_t x) {
-  x = add_from<0x118, 0xf>(add_from<0x114, 0xf>(add_from<0x112, 0xf>(add_from<0x111, 0xf>(x))));
-  x = add_from<0x143, 0xc>(add_from<0x142, 0xa>(x));
-  return (int64_t)(((uint64_t)(unsigned)__builtin_amdgcn_readlane((int)(x >> 32), 63) << 32) | (unsigned)__builtin_amdgcn_readlane((int)x, 63));
-}
-__device__ __forceinline__ int wave_max(int x) {   // of numbers that are not negative
-  x = max(x, from_lane<0x111, 0xf>(x));
-  x = max(x, from_lane<0x112, 0xf>(x));
-  x = max(x, from_lane<0x114, 0xf>(x));
-  x = max(x, from_lane<0x118, 0xf>(x));
-  x = max(x, from_lane<0x142, 0xa>(x));
-  return __builtin_amdgcn_readlane(max(x, from_lane<0x143, 0xc>(x)), 63);
-}
-__device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
-
-// What the sums are over.  Lane i has sequence i in registers; further ones are loaded when their 64 come up.
-struct Plan {
-  int n;            // sequences
-  int part;         // keys of a part
-  Sequence first;   // sequence `lane` (empty if there is none)
-};
-__device__ __forceinline__ Sequence lane_sequence(const PagedParams& p, const Plan& plan, int b0) {
-  const int b = b0 + (int)(threadIdx.x & 63);
-  return b0 == 0 ? plan.first : b < plan.n ? sequence(p.seq, b) : Sequence{0, 0, 0, 0};
-}
 __device__ __forceinline__ Plan make_plan(const PagedParams& p) {
   Plan plan;
   const int lane = threadIdx.x & 63;
@@ -87,34 +49,6 @@ __device__ __forceinline__ Plan make_plan(const PagedParams& p) {
   return plan;
 }
 
-// Sums count(sequence) over the sequences up to the one that holds element `at`: true, and its number and the sum before it; false, and the sum of all.
-template <typename Count>
-__device__ __forceinline__ bool locate(const PagedParams& p, const Plan& plan, int at, Count count, int& b, int& before) {
-  before = 0;
-  for (int b0 = 0; b0 < plan.n; b0 += 64) {
-    const int c = count(lane_sequence(p, plan, b0)), upto = wave_scan(c);
-    const unsigned long long over = __ballot(at < before + upto);
-    if (over) {
-      const int i = __builtin_ctzll(over);
-      b = b0 + i;
-      before += __builtin_amdgcn_readlane(upto - c, i);
-      return true;
-    }
-    before += __builtin_amdgcn_readlane(upto, 63);
-  }
-  return false;
-}
-// The sum of count over the sequences in front of b.
-template <typename Count>
-__device__ __forceinline__ int sum_before(const PagedParams& p, const Plan& plan, int end, Count count) {
-  int sum = 0;
-  for (int b0 = 0; b0 < end; b0 += 64) {
-    const int c = b0 + (int)(threadIdx.x & 63) < end ? count(lane_sequence(p, plan, b0)) : 0;
-    sum += __builtin_amdgcn_readlane(wave_scan(c), 63);
-  }
-  return sum;
-}
-
 struct Item {
   int rows;                         // of the sequence and a K/V head
   int b, hk, tile, part, n_parts;   // n_parts: live ones, those whose keys some row of the tile sees, and the first one
@@ -125,6 +59,13 @@ struct Item {
 
 // Rows of a tile see keys 0 .. limit(row) - 1; row r of a sequence and K/V head is query head r mod gq of token r / gq.
 __device__ __forceinline__ int row_limit(const PagedParams& p, const Sequence& q, int r) { return visible(q, divide(p.by_gq, r), p.causal); }
+// What all rows of a tile see whose first row is r, and what some row of one sees whose last row is r.  In a tree rows see the keys in front of the drafts, and what their bits say.
+__device__ __forceinline__ int first_limit(const PagedParams& p, const Sequence& q, int r) { return row_limit(p, q, r); }
+__device__ __forceinline__ int first_limit(const TreeParams& p, const Sequence& q, int r) { return visible_to_all(q); }
+__device__ __forceinline__ int last_limit(const PagedParams& p, const Sequence& q, int r) { return row_limit(p, q, r); }
+__device__ __forceinline__ int last_limit(const TreeParams& p, const Sequence& q, int r) { return visible_to_any(q); }
+template <typename P>
+constexpr bool is_tree = std::is_same<P, TreeParams>::value;
 __device__ __forceinline__ Sequence uniform_sequence(const PagedParams& p, int b) {   // (loaded by vectors, in scalar registers from here on)
   const Sequence q = sequence(p.seq, b);
   return Sequence{uniform(q.start), uniform(q.n), uniform(q.len), uniform(q.pos)};
@@ -132,7 +73,8 @@ __device__ __forceinline__ Sequence uniform_sequence(const PagedParams& p, int b
 
 // Item `id` of the launch; false: none (it lies behind the last one, or its part has no live keys).  The items of a K/V head and part lie next to each
 // other, and each XCD has a contiguous eighth of all, so that row tiles which read the same keys mostly share an L2.
-__device__ __forceinline__ bool find_item(const PagedParams& p, const Plan& plan, int id, Item& w) {
+template <typename P>
+__device__ __forceinline__ bool find_item(const P& p, const Plan& plan, int id, Item& w) {
   const int part = plan.part;
   auto items = [&](const Sequence& q) { return tiles_of(q.n * p.gq, p.rows) * parts_of(q.len, part) * p.Hkv; };
   int before, b = 0;
@@ -149,7 +91,7 @@ __device__ __forceinline__ bool find_item(const PagedParams& p, const Plan& plan
   w.hk = uniform(unit / parts);
   w.part = unit - w.hk * parts;
   const int last = min((w.tile + 1) * p.rows.tile, w.rows) - 1;
-  const int seen = uniform(row_limit(p, w.q, last));
+  const int seen = uniform(last_limit(p, w.q, last));
   w.n_parts = parts_of(seen, part);
   w.k0 = w.part * part;
   w.k1 = w.part + 1 < w.n_parts ? w.k0 + part : seen;
@@ -208,21 +150,23 @@ struct Few {
   static constexpr int LDS = W * TILE * (D + 2) * 4;
 };
 
-template <int D, bool F8, int RT, int W, bool AHEAD, bool OUT_F32>   // AHEAD: the next stretch is on its way beside the products (it takes registers)
-__device__ __forceinline__ void few_rows(const PagedParams& p, const Item& w, int row0, int slot_row, char* lds) {
+template <int D, bool F8, int RT, int W, bool AHEAD, bool OUT_F32, typename P>   // AHEAD: the next stretch is on its way beside the products (it takes registers)
+__device__ __forceinline__ void few_rows(const P& p, const Item& w, int row0, int slot_row, char* lds) {
   typedef Few<D, F8, RT, W> F;
   constexpr int STEP = 32 * W;   // keys of a step of the workgroup
   constexpr int TILE = F::TILE, DL = F::DL, KL = F::KL, VW = F::VW, QS = D / 32;
   const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), i16 = lane & 15, g = lane >> 4;
   const int rows = min(TILE, w.q.n * p.gq - row0);
-  const int limit_lo = row_limit(p, w.q, row0), limit_hi = min(w.k1, row_limit(p, w.q, row0 + rows - 1));
+  const int limit_lo = first_limit(p, w.q, row0), limit_hi = min(w.k1, last_limit(p, w.q, row0 + rows - 1));
 
   bf16x8 qf[RT][QS];
   int limit[RT];
+  const unsigned* branch[RT];   // tree: the row's bits
 #pragma unroll
   for (int rt = 0; rt < RT; rt++) {
     const int r = row0 + min(rt * 16 + i16, rows - 1), t = divide(p.by_gq, r);
-    limit[rt] = min(w.k1, visible(w.q, t, p.causal));
+    if constexpr (is_tree<P>) branch[rt] = p.tree + (int64_t)(w.q.start + t) * p.tree_stride;
+    else limit[rt] = min(w.k1, visible(w.q, t, p.causal));
     const __bf16* const src = p.q + (int64_t)(w.hk * p.gq + r - t * p.gq) * p.q_sh + (int64_t)(w.q.start + t) * p.q_ss;
 #pragma unroll
     for (int s = 0; s < QS; s++)   // d's in the order of the K loads
@@ -340,13 +284,25 @@ __device__ __forceinline__ void few_rows(const PagedParams& p, const Item& w, in
       }
     if (AHEAD && step + 1 < steps) load_k(step + 1);
     if (edge) {
+      if constexpr (is_tree<P>) {
 #pragma unroll
-      for (int h = 0; h < 2; h++)
+        for (int rt = 0; rt < RT; rt++) {
+          const unsigned seen = tree_bits(branch[rt], p.words, w.q, key0, limit_hi) >> 4 * g;
 #pragma unroll
-        for (int r = 0; r < 4; r++)
+          for (int h = 0; h < 2; h++)
 #pragma unroll
-          for (int rt = 0; rt < RT; rt++)
-            if (key0 + 16 * h + 4 * g + r >= limit[rt] || !there[h]) s[rt][h][r] = -INFINITY;
+            for (int r = 0; r < 4; r++)
+              if (!(seen >> (16 * h + r) & 1) || !there[h]) s[rt][h][r] = -INFINITY;
+        }
+      } else {
+#pragma unroll
+        for (int h = 0; h < 2; h++)
+#pragma unroll
+          for (int r = 0; r < 4; r++)
+#pragma unroll
+            for (int rt = 0; rt < RT; rt++)
+              if (key0 + 16 * h + 4 * g + r >= limit[rt] || !there[h]) s[rt][h][r] = -INFINITY;
+      }
     }
     // Weights relative to a reference that is not the running maximum: any gives the same result, and one that the
     // first scores set is replaced only where a sum of weights passes kSumCap (fp32 and bf16 hold them as well as small ones).  A row without one has -inf there: its
@@ -456,6 +412,12 @@ __device__ __forceinline__ void few_rows(const PagedParams& p, const Item& w, in
       if (one.page < 0) continue;
       const char* const vp = vb + (int64_t)one.page * p.page_b + (int64_t)one.slot * p.slot_b + g * 16 * VW;
       const unsigned scale = F8 ? vsb[(int64_t)one.page * p.scale_sp + one.slot] : 0;
+      bool sees[RT];
+#pragma unroll
+      for (int rt = 0; rt < RT; rt++) {
+        if constexpr (is_tree<P>) sees[rt] = tree_bits(branch[rt], p.words, w.q, key, limit_hi) & 1;
+        else sees[rt] = key < limit[rt];
+      }
 #pragma unroll
       for (int i = 0; i < 4 * VW; i++) {   // the lane's 4 * DL values, d = 4 g DL + ...
         const unsigned x = reinterpret_cast<const unsigned*>(vp)[i];
@@ -465,8 +427,8 @@ __device__ __forceinline__ void few_rows(const PagedParams& p, const Item& w, in
           const int e = F8 ? 4 * i + 2 * n : 2 * i;
 #pragma unroll
           for (int rt = 0; rt < RT; rt++) {
-            if (key < limit[rt] && (pair & 0x7f80u) == 0x7f80u) acc[rt][e % DL][e / DL] += __builtin_bit_cast(float, pair << 16);
-            if (key < limit[rt] && (pair & 0x7f800000u) == 0x7f800000u) acc[rt][e % DL + 1][e / DL] += __builtin_bit_cast(float, pair & 0xffff0000u);
+            if (sees[rt] && (pair & 0x7f80u) == 0x7f80u) acc[rt][e % DL][e / DL] += __builtin_bit_cast(float, pair << 16);
+            if (sees[rt] && (pair & 0x7f800000u) == 0x7f800000u) acc[rt][e % DL + 1][e / DL] += __builtin_bit_cast(float, pair & 0xffff0000u);
           }
         }
       }
@@ -522,8 +484,8 @@ __device__ __forceinline__ void few_rows(const PagedParams& p, const Item& w, in
   }
 }
 
-template <int D, bool F8, int RT, bool OUT_F32>
-__global__ void __launch_bounds__(256, paged_few_waves(D, F8, RT)) paged_few_kernel(const PagedParams p) {
+template <int D, bool F8, int RT, bool OUT_F32, typename P>
+__global__ void __launch_bounds__(256, paged_few_waves(D, F8, RT)) paged_few_kernel(const P p) {
   extern __shared__ __attribute__((aligned(1024))) char lds[];
   Item w;
   if (!find_item(p, make_plan(p), (int)blockIdx.x, w)) return;
@@ -533,8 +495,8 @@ __global__ void __launch_bounds__(256, paged_few_waves(D, F8, RT)) paged_few_ker
 // ---- Row tiles whose keys were cut (6 us for 32 tiles of 16 rows in 16 parts, 13 for 64 of 256 rows in four, 34 MB): out = sum of exp(lse_i - lse) out_i over their live parts, in their order.
 // A workgroup has pieces of 1024 / D rows of a tile, D / 4 lanes a row.  What bounds it is latency: the lanes of a row
 // fetch the lse of one part each, and pieces of eight parts are on their way at a time.
-template <int D, bool OUT_F32>
-__global__ void __launch_bounds__(256) paged_fold_kernel(const PagedParams p) {
+template <int D, bool OUT_F32, typename P>
+__global__ void __launch_bounds__(256) paged_fold_kernel(const P p) {
   constexpr int LANES = D / 4, ROWS = 256 / LANES, AHEAD = 8;
   const Plan plan = make_plan(p);
   const int part = plan.part, size = p.rows.tile, pieces = max(1, size / ROWS);
@@ -549,7 +511,7 @@ __global__ void __launch_bounds__(256) paged_fold_kernel(const PagedParams p) {
   const int parts = uniform(parts_of(w.q.len, part)), tiles = uniform(tiles_of(w.rows, p.rows)), i = uniform(at / pieces - before);
   w.hk = uniform(i / tiles);
   const int row0 = (i - w.hk * tiles) * size, rows = min(size, w.rows - row0);
-  const int n_live = uniform(parts_of(row_limit(p, w.q, row0 + rows - 1), part));
+  const int n_live = uniform(parts_of(last_limit(p, w.q, row0 + rows - 1), part));
   if (n_live == 1) continue;   // one part: written already
   if (base < 0 || base + (i + 1) * parts > p.slots) continue;   // (only where sequences overlap)
   w.n_parts = 1;   // what follows is stored for good

@@ -36,6 +36,21 @@ constexpr Sequence sequence(const Sequences& s, int b) {
 // Keys 0 .. visible(...) - 1 are those that token t of a sequence sees.
 constexpr int visible(const Sequence& q, int t, bool causal) { return causal ? clamped(q.pos + t + 1, 0, q.len) : q.len; }
 
+// Of a tree: keys 0 .. visible_to_all() - 1 are seen by every token of the sequence, those from visible_to_any() on by none.
+constexpr int visible_to_all(const Sequence& q) { return clamped(q.pos, 0, q.len); }
+constexpr int visible_to_any(const Sequence& q) { return clamped(q.pos + q.n, 0, q.len); }
+// Which of the keys key0 .. key0 + 31 a token sees by its row of the tree (bit i: key0 + i); `seen`: visible_to_any(), or an earlier end of the keys.
+constexpr unsigned tree_word(const unsigned* row, int words, int n, int i) {   // of drafted tokens 32 i .. 32 i + 31; those in front of the first are keys that all see
+  return i < 0 ? ~0u : i >= words || 32 * i >= n ? 0u : n - 32 * i >= 32 ? row[i] : row[i] & ((1u << (n - 32 * i)) - 1);
+}
+constexpr unsigned tree_bits(const unsigned* row, int words, const Sequence& q, int key0, int seen) {
+  const int from = key0 - q.pos, i = from >> 5, left = seen - key0;   // (from is below 2^31: 0 <= key0 < 2^30, pos >= -2^30)
+  if (left <= 0) return 0;
+  const uint64_t both = (uint64_t)tree_word(row, words, q.n, i + 1) << 32 | tree_word(row, words, q.n, i);
+  const unsigned bits = (unsigned)(both >> (from & 31));
+  return left >= 32 ? bits : bits & ((1u << left) - 1);
+}
+
 // Page (-1: none) and slot of key c, 0 <= c < max_pages * page_size.
 struct Slot { int page, slot; };
 constexpr Slot slot_of(const Sequences& s, int b, int c) {

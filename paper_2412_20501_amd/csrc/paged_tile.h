@@ -1,7 +1,5 @@
 // Attention on a paged cache: items of many rows (a chunk of a prompt).
 #pragma once
-#include <type_traits>
-
 #include "paged_attn_kernel.h"
 
 namespace tr {
@@ -61,15 +59,15 @@ __device__ __forceinline__ int v_tile_off(int row, int c) {   // the same of a V
 }
 
 // true: done; false: the item needs the other way (nothing has been written)
-template <int D, bool F8, bool OUT_F32>
-__device__ __forceinline__ bool tile_rows(const PagedParams& p, const Item& w, int slot_row, char* lds) {
+template <int D, bool F8, bool OUT_F32, typename P>
+__device__ __forceinline__ bool tile_rows(const P& p, const Item& w, int slot_row, char* lds) {
   typedef Tile<D> T;
   constexpr int RB = T::RB, BN = T::BN, NS = T::NS, TILE_BYTES = T::TILE_BYTES, KS = D / 16, DB = D / 32, CPR = D / 8, SUB = 32, NSW = BN / SUB;
   constexpr int RPI = 1024 / RB, IPW = 2, SHARE = IPW * RPI;   // rows of a wave-wide 16-byte load; loads of a wave, tile and tensor; its rows
   static_assert(BN / SHARE == 8, "eight waves load a tile");
   const int tid = threadIdx.x, wave = uniform(tid >> 6), lane = tid & 63, ql = lane & 31, hf = lane >> 5;
   const int row0 = w.tile * T::ROWS, n_rows = min(T::ROWS, w.q.n * p.gq - row0), qw0 = wave * 32;   // (rows counted within the item)
-  const int limit_first = row_limit(p, w.q, row0), end = min(w.k1, row_limit(p, w.q, row0 + n_rows - 1));
+  const int limit_first = first_limit(p, w.q, row0), end = min(w.k1, last_limit(p, w.q, row0 + n_rows - 1));
   const int n_keys = end - w.k0, n_tiles = uniform((max(n_keys, 0) + BN - 1) / BN), last_tile = n_tiles - 1;
 
   if (tid == 0) *reinterpret_cast<int*>(lds + T::FLAG) = 0;
@@ -228,10 +226,12 @@ __device__ __forceinline__ bool tile_rows(const PagedParams& p, const Item& w, i
   // pages that are none, among all of the item's keys
   for (int key = w.k0 + tid * 16; key < end; key += 512 * 16) bad |= slot_of(p.seq, w.b, key).page < 0 ? 1u : 0u;
   // keys that the lane's row, and the first and the last row of the wave, see (in keys from k0 on)
-  const int lane_end = min(w.k1, visible(w.q, q_tok, p.causal)) - w.k0;
+  int lane_end = 0;
+  if constexpr (is_tree<P>) *reinterpret_cast<int64_t*>(lds + T::OFF + (qw0 + ql) * 8) = (int64_t)(w.q.start + q_tok) * p.tree_stride;   // (the row's bits; both halves write it)
+  else lane_end = min(w.k1, visible(w.q, q_tok, p.causal)) - w.k0;
   const bool rows_here = qw0 < n_rows;
-  const int wave_lo = uniform(min(w.k1, row_limit(p, w.q, row0 + min(qw0, n_rows - 1))) - w.k0);
-  const int wave_hi = uniform(rows_here ? min(w.k1, row_limit(p, w.q, row0 + min(qw0 + 31, n_rows - 1))) - w.k0 : 0);
+  const int wave_lo = uniform(min(w.k1, first_limit(p, w.q, row0 + min(qw0, n_rows - 1))) - w.k0);
+  const int wave_hi = uniform(rows_here ? min(w.k1, last_limit(p, w.q, row0 + min(qw0 + 31, n_rows - 1))) - w.k0 : 0);
   const int jw = (max(wave_hi, 0) + SUB - 1) / SUB;      // sub-tiles this wave has visible keys in
   const int kmask_from = wave_lo - SUB;                  // a sub-tile from kstart on needs a mask iff kstart > kmask_from
   const int jw_first = jw, jw_in = min(jw, NSW * n_tiles - 1);
@@ -271,9 +271,17 @@ __device__ __forceinline__ bool tile_rows(const PagedParams& p, const Item& w, i
     constexpr int n_mfma = FIRST ? NQK : NQK + NPV, EPM = 16 / n_mfma;
     constexpr unsigned v_imm = decltype(v_imm_c)::value, k_imm_next = decltype(k_imm_next_c)::value;
     if (!INNER && kstart > kmask_from) {
+      if constexpr (is_tree<P>) {
+        const int64_t row = *reinterpret_cast<const int64_t*>(lds + T::OFF + (qw0 + ql) * 8);
+        const unsigned seen = tree_bits(p.tree + row, p.words, w.q, w.k0 + kstart, end) >> 4 * hf;
 #pragma unroll
-      for (int i = 0; i < 16; i++)
-        if (kstart + 8 * (i >> 2) + 4 * hf + (i & 3) >= lane_end) s_in[i] = -INFINITY;
+        for (int i = 0; i < 16; i++)
+          if (!(seen >> (8 * (i >> 2) + (i & 3)) & 1)) s_in[i] = -INFINITY;
+      } else {
+#pragma unroll
+        for (int i = 0; i < 16; i++)
+          if (kstart + 8 * (i >> 2) + 4 * hf + (i & 3) >= lane_end) s_in[i] = -INFINITY;
+      }
     }
     f32x16 acc;
 #pragma unroll
@@ -511,8 +519,8 @@ __device__ __forceinline__ bool tile_rows(const PagedParams& p, const Item& w, i
   return true;
 }
 
-template <int D, bool F8, bool OUT_F32>
-__global__ void __launch_bounds__(512, 2) paged_many_kernel(const PagedParams p) {
+template <int D, bool F8, bool OUT_F32, typename P>
+__global__ void __launch_bounds__(512, 2) paged_many_kernel(const P p) {
   extern __shared__ __attribute__((aligned(1024))) char lds[];
   Item w;
   if (!find_item(p, make_plan(p), (int)blockIdx.x, w)) return;
