@@ -1,27 +1,12 @@
 // Launches of one head dim and type of the pages (one .hip each, so that they compile side by side).
 #pragma once
 #include <algorithm>
-#include <atomic>
 
+#include "launch_lds.h"
 #include "paged_tile.h"
 
 namespace tr {
 namespace {
-
-// A launch that asks for more LDS than the default limit: raised once for each device and kernel.
-template <typename Kernel, typename... Args>
-hipError_t launch_lds(Kernel kernel, std::atomic<uint64_t>& raised, dim3 grid, dim3 block, int lds_bytes, hipStream_t stream, Args... args) {
-  int dev = 0;
-  hipError_t e = hipGetDevice(&dev);
-  if (e != hipSuccess) return e;
-  const uint64_t bit = dev >= 0 && dev < 64 ? (uint64_t)1 << dev : 0;
-  if (!(raised.load(std::memory_order_acquire) & bit)) {
-    e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, lds_bytes);
-    if (e != hipSuccess) return e;
-    raised.fetch_or(bit, std::memory_order_release);
-  }
-  return launch_kernel(kernel, grid, block, lds_bytes, stream, args...);
-}
 
 template <int D, bool F8, bool OUT_F32, typename P>
 hipError_t launch_out(P& p, const PagedLaunch& l, float* workspace, hipStream_t stream) {
