@@ -13,7 +13,7 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 //
 // The k-th largest weight of a row (a sequence's K/V head) by its bits, 11, 11 and 10 at a time: counts of each value of these bits among the keys that have the higher
 // bits found so far, in LDS; then the keys above it, and of those equal to it the first ones, in their order.
-constexpr int kSelectThreads = 1024, kDigits = 2048;
+constexpr int kDigits = 2048;
 
 // Weights in the order of unsigned integers: NaN highest, -0 as 0.  Above them all those keys that stay anyway, below them 0: no key, or on no page.
 constexpr unsigned kStays = 0xffffffffu, kZero = 0x80000000u;
@@ -21,20 +21,31 @@ __device__ __forceinline__ unsigned rank_of(float x) {
   const unsigned b = __builtin_bit_cast(unsigned, x == 0.f ? 0.f : x);
   return x != x ? kStays - 1 : b & 0x80000000u ? ~b : b | 0x80000000u;
 }
-// Sum of x over the workgroup's threads in front of this one; all: over all of them.  `waves`: LDS for 17 numbers, free again behind the next barrier.
-__device__ __forceinline__ int before_in_group(int x, int* waves, int& all) {
-  const int wave = (int)threadIdx.x >> 6, upto = wave_scan(x);
-  if ((threadIdx.x & 63) == 63) waves[wave] = upto;
-  __syncthreads();
-  int before = upto - x;
-  all = 0;
+// One wave: the digit of the take-th largest among counts, from the highest digit (DIGITS - 1) down, and how many of those that have it are still to take; false: there are fewer than `take`
+// in all, which are taken off.
+template <int DIGITS>
+__device__ __forceinline__ bool find_digit(const int* counts, int& take, unsigned& digit) {
+  constexpr int EACH = DIGITS / 64;   // lane i has digits DIGITS - 1 - EACH i and the EACH - 1 below
+  const int lane = threadIdx.x & 63;
+  const u32x4* const mine = reinterpret_cast<const u32x4*>(counts) + (63 - lane) * (EACH / 4);
+  int sum = 0;
 #pragma unroll
-  for (int i = 0; i < kSelectThreads / 64; i++) {
-    const int n = waves[i];
-    before += i < wave ? n : 0;
-    all += n;
+  for (int i = 0; i < EACH / 4; i++) {
+    const u32x4 x = mine[(i + lane) % (EACH / 4)];   // (lanes begin on different banks)
+    sum += (int)(x[0] + x[1] + x[2] + x[3]);
   }
-  return before;
+  const int upto = wave_scan(sum), all = __builtin_amdgcn_readlane(upto, 63);
+  if (all < take) {
+    take -= all;
+    return false;
+  }
+  const int first = __builtin_ctzll(__ballot(upto >= take));   // the lane that has it
+  take -= __builtin_amdgcn_readlane(upto - sum, first);
+  const int top = DIGITS - 1 - EACH * first, one = lane < EACH ? counts[top - lane] : 0, below = wave_scan(one);
+  const int at = __builtin_ctzll(__ballot(below >= take));
+  take -= __builtin_amdgcn_readlane(below - one, at);
+  digit = top - at;
+  return true;
 }
 
 // The last key that stays: its rank, and how many of those that are equal to it stay, the first ones.
@@ -59,14 +70,16 @@ __device__ __forceinline__ void write_four(int* out, const Border& border, int k
   }
 }
 
-// A row's ranks are held in LDS, where they fit (`room` of them, a multiple of a turn's), and are read again from memory in every pass where they do not.
-constexpr int kTurn = 4 * kSelectThreads, kTurns = 9;   // keys of a turn of the workgroup; turns that LDS has room for beside the counts
-__global__ void __launch_bounds__(kSelectThreads, 8) select_kernel(const SelectParams p, const int room) {
+// A wave has a stretch of the row's keys, 256 at a time.  Ranks are held in LDS where they fit (`room` of them), and are read from memory again where they do not; those that
+// share the first digit with the border, mostly a few hundredths of them, are held once more as a list, unless it is too long.  Bound: the instructions of one compute unit.
+constexpr int kRoom = 32768, kList = 2048;   // ranks that LDS has room for; entries of the list
+template <int THREADS>
+__global__ void __launch_bounds__(THREADS, 8) select_kernel(const SelectParams p, const int room) {
   extern __shared__ __attribute__((aligned(16))) char lds[];
-  __shared__ int counts[kDigits];
-  __shared__ int waves[2][16];
-  __shared__ int totals[kTurns * 16];
-  __shared__ int found[2];   // digit, keys still to take among those that have it
+  __shared__ __attribute__((aligned(16))) int counts[2 * kDigits + kDigits / 2];   // of the three passes
+  __shared__ unsigned list[kList];
+  __shared__ int sums[2][THREADS / 64];
+  __shared__ int n_list, n_zeros, found[2];   // found: digit, keys still to take among those that have it
   u32x4* const ranks = reinterpret_cast<u32x4*>(lds);
   const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
   for (int64_t row = blockIdx.x; row < (int64_t)p.seq.n * p.heads; row += gridDim.x) {
@@ -75,7 +88,7 @@ __global__ void __launch_bounds__(kSelectThreads, 8) select_kernel(const SelectP
     int* const out = p.keys + (int64_t)b * p.k_sb + (int64_t)h * p.k_sh;
     if (h == 0 && tid == 0) p.count[b] = n;
     if (len <= p.most) {
-      for (int i = tid; i < len; i += kSelectThreads) out[i] = i;
+      for (int i = tid; i < len; i += THREADS) out[i] = i;
       continue;
     }
     if (p.most == 0) continue;
@@ -88,82 +101,114 @@ __global__ void __launch_bounds__(kSelectThreads, 8) select_kernel(const SelectP
 #pragma unroll
         for (int i = 0; i < 4; i++) u[i] = rank_of(x[i]);
       }
+      if (key < p.first || key + 3 >= len - p.last) {
 #pragma unroll
-      for (int i = 0; i < 4; i++) u[i] = key + i >= len ? 0 : key + i < p.first || key + i >= len - p.last ? kStays : u[i];
+        for (int i = 0; i < 4; i++) u[i] = key + i >= len ? 0 : key + i < p.first || key + i >= len - p.last ? kStays : u[i];
+      }
       return u;
     };
     const bool held = len <= room;
-    const int turns = (len + kTurn - 1) / kTurn;
-    if (held) {
-#pragma unroll 4
-      for (int t = 0; t < turns; t++) ranks[t * kSelectThreads + tid] = fetch(t * kTurn + 4 * tid);   // (each thread reads what it wrote)
-    }
-    auto four = [&](int t) __attribute__((always_inline)) -> u32x4 { return held ? ranks[t * kSelectThreads + tid] : fetch(t * kTurn + 4 * tid); };
+    const int steps = (len + 4 * THREADS - 1) / (4 * THREADS), piece0 = wave * steps * 64 + lane;   // of a wave; pieces of four keys are piece0 + 64 i
+    auto four = [&](int i) __attribute__((always_inline)) -> u32x4 { return held ? ranks[piece0 + 64 * i] : fetch(4 * (piece0 + 64 * i)); };
     Border border = {0, p.most};   // (at least one of the keys goes: len > most)
-    unsigned known = 0;            // bits of the rank that are found
-#pragma unroll 1
-    for (int pass = 0; pass < 3; pass++) {
-      const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0;
-      const unsigned digits = pass < 2 ? 2047u : 1023u;
-      for (int i = tid; i < kDigits; i += kSelectThreads) counts[i] = 0;
+    auto find = [&](int pass, int shift) __attribute__((always_inline)) -> bool {
       __syncthreads();
-      int zeros = 0, none = 0;   // (most weights may be 0: they are counted by the wave, 64 additions to one place are 64 turns)
-      for (int t = 0; t < turns; t++) {
-        const u32x4 x = four(t);
-#pragma unroll
-        for (int i = 0; i < 4; i++) {
-          const bool here = (x[i] & known) == border.rank;
-          zeros += __popcll(__ballot(here && x[i] == kZero));
-          none += __popcll(__ballot(here && x[i] == 0));
-          if (here && (x[i] & ~kZero) != 0) atomicAdd(&counts[x[i] >> shift & digits], 1);
+      if (wave == 0) {
+        unsigned digit = 0;
+        int take = border.take;
+        const bool there = pass < 2 ? find_digit<kDigits>(counts + pass * kDigits, take, digit) : find_digit<kDigits / 2>(counts + 2 * kDigits, take, digit);
+        if (lane == 0) {
+          found[0] = there ? (int)digit : -1;
+          found[1] = take;
         }
       }
-      if (lane == 0 && zeros > 0) atomicAdd(&counts[kZero >> shift & digits], zeros);
-      if (lane == 0 && none > 0) atomicAdd(&counts[0], none);
       __syncthreads();
-      // from the highest digit down: thread t has digits 2047 - 2 t and the one below
-      const int hi = counts[kDigits - 1 - 2 * tid], lo = counts[kDigits - 2 - 2 * tid];
-      int all;
-      const int above = before_in_group(hi + lo, waves[0], all);
-      if (above < border.take && above + hi + lo >= border.take) {
-        const bool in_hi = above + hi >= border.take;
-        found[0] = kDigits - 1 - 2 * tid - (in_hi ? 0 : 1);
-        found[1] = border.take - above - (in_hi ? 0 : hi);
-      }
-      __syncthreads();
-      border.rank |= (unsigned)found[0] << shift;
-      known |= digits << shift;
-      border.take = found[1];
-    }
-    if (held) {   // sums within the waves, then one scan over those of all turns and waves
-      for (int t = 0; t < turns; t++) {
-        const int upto = wave_scan(sum_four(border, four(t)));
-        if (lane == 63) totals[t * 16 + wave] = upto;
-      }
-      __syncthreads();
-      int base = 0, scan[(kTurns * 16 + 63) / 64];
+      const int digit = uniform(found[0]);
+      border.take = uniform(found[1]);
+      if (digit < 0) return false;   // there are too few keys on pages: the border is among the others
+      border.rank |= (unsigned)digit << shift;
+      return true;
+    };
+    if (tid == 0) n_list = n_zeros = 0;
+    for (int i = tid; i < (2 * kDigits + kDigits / 2) / 4; i += THREADS) reinterpret_cast<u32x4*>(counts)[i] = u32x4{0, 0, 0, 0};
+    __syncthreads();
+    int zeros = 0;   // (most weights may be 0: they are counted apart, 64 additions to one place are 64 turns)
+#pragma unroll 4
+    for (int i = 0; i < steps; i++) {
+      const u32x4 x = fetch(4 * (piece0 + 64 * i));
+      if (held) ranks[piece0 + 64 * i] = x;   // (each thread reads what it wrote)
 #pragma unroll
-      for (int e = 0; e < (kTurns * 16 + 63) / 64; e++) {
-        const int mine = e * 64 + lane < turns * 16 ? totals[e * 64 + lane] : 0, upto = wave_scan(mine);
-        scan[e] = base + upto - mine;
-        base += __builtin_amdgcn_readlane(upto, 63);
+      for (int k = 0; k < 4; k++) {
+        zeros += x[k] == kZero ? 1 : 0;
+        if ((x[k] & ~kZero) != 0) atomicAdd(&counts[x[k] >> 21], 1);
       }
-      for (int t = 0; t < turns; t++) {
-        const u32x4 x = four(t);
-        const int at = t * 16 + wave, sum = sum_four(border, x), mine = at < 64 ? scan[0] : at < 128 ? scan[1] : scan[2];
-        const int sums = __builtin_amdgcn_readlane(mine, at & 63) + wave_scan(sum) - sum;
-        write_four(out, border, t * kTurn + 4 * tid, x, sums & 0xffff, (int)((unsigned)sums >> 16));
+    }
+    zeros = __builtin_amdgcn_readlane(wave_scan(zeros), 63);
+    if (lane == 0 && zeros > 0) {
+      atomicAdd(&counts[kZero >> 21], zeros);
+      atomicAdd(&n_zeros, zeros);
+    }
+    if (find(0, 21)) {
+      const unsigned digit = border.rank >> 21;
+      for (int i = 0; i < steps; i++) {
+        const u32x4 x = four(i);
+        int mine = 0;
+#pragma unroll
+        for (int k = 0; k < 4; k++) mine += x[k] >> 21 == digit && x[k] != kZero ? 1 : 0;
+        if (!__any(mine != 0)) continue;
+        const int upto = wave_scan(mine);
+        int at = 0;
+        if (lane == 63) at = atomicAdd(&n_list, upto);
+        at = __builtin_amdgcn_readlane(at, 63) + upto - mine;
+#pragma unroll
+        for (int k = 0; k < 4; k++)
+          if (x[k] >> 21 == digit && x[k] != kZero) {
+            atomicAdd(&counts[kDigits + (x[k] >> 10 & 2047)], 1);
+            if (at < kList) list[at] = x[k];
+            at++;
+          }
       }
-    } else {
-      int above = 0, same = 0;
-      for (int t = 0; t < turns; t++) {
-        const u32x4 x = four(t);
-        int all;
-        const int before = before_in_group(sum_four(border, x), waves[t & 1], all);
-        write_four(out, border, t * kTurn + 4 * tid, x, above + (before & 0xffff), same + (before >> 16));
-        above += all & 0xffff;
-        same += all >> 16;
+      if (tid == 0 && digit == kZero >> 21) atomicAdd(&counts[kDigits + (kZero >> 10 & 2047)], n_zeros);
+      find(1, 10);
+      const unsigned high = border.rank >> 10;
+      if (n_list <= kList) {
+        for (int i = tid; i < n_list; i += THREADS)
+          if (list[i] >> 10 == high) atomicAdd(&counts[2 * kDigits + (list[i] & 1023)], 1);
+      } else {
+        for (int i = 0; i < steps; i++) {
+          const u32x4 x = four(i);
+#pragma unroll
+          for (int k = 0; k < 4; k++)
+            if (x[k] >> 10 == high && x[k] != kZero) atomicAdd(&counts[2 * kDigits + (x[k] & 1023)], 1);
+        }
       }
+      if (tid == 0 && high == kZero >> 10) atomicAdd(&counts[2 * kDigits], n_zeros);
+      find(2, 0);
+    }
+    // what the waves in front have: keys above the border, and those equal to it
+    int above = 0, same = 0;
+    for (int i = 0; i < steps; i++) {
+      const int sum = sum_four(border, four(i));
+      above += sum & 0xffff;
+      same += sum >> 16;
+    }
+    above = wave_scan(above);
+    same = wave_scan(same);
+    if (lane == 63) {
+      sums[0][wave] = above;
+      sums[1][wave] = same;
+    }
+    __syncthreads();
+    above = lane < wave ? sums[0][lane] : 0;
+    same = lane < wave ? sums[1][lane] : 0;
+    above = __builtin_amdgcn_readlane(wave_scan(above), 63);
+    same = __builtin_amdgcn_readlane(wave_scan(same), 63);
+    for (int i = 0; i < steps; i++) {
+      const u32x4 x = four(i);
+      const int mine = sum_four(border, x), upto = wave_scan(mine), before = upto - mine, all = __builtin_amdgcn_readlane(upto, 63);
+      write_four(out, border, 4 * (piece0 + 64 * i), x, above + (before & 0xffff), same + (before >> 16));
+      above += all & 0xffff;
+      same += all >> 16;
     }
     __syncthreads();
   }
@@ -279,15 +324,22 @@ __global__ void __launch_bounds__(kKeepThreads) keep_kernel(const KeepParams p, 
 
 }  // namespace
 
+namespace {
+template <int THREADS>
+hipError_t launch_select(const SelectParams& p, int room, dim3 grid, hipStream_t stream) {
+  static std::atomic<uint64_t> raised;
+  const hipError_t e = raise_lds(select_kernel<THREADS>, raised, kRoom * 4);
+  return e != hipSuccess ? e : launch_kernel(select_kernel<THREADS>, grid, dim3(THREADS), room * 4, stream, p, room);
+}
+}  // namespace
+
 hipError_t launch_cache_select(const SelectParams& p, hipStream_t stream) {
   const int64_t rows = (int64_t)p.seq.n * p.heads;
-  const dim3 grid((unsigned)(rows < 65536 ? rows : 65536)), block(kSelectThreads);
-  // LDS for the rows that the table has room for: a compute unit then holds two workgroups on up to 16384 keys, one on more.
-  const int64_t max_keys = (int64_t)p.seq.max_pages * p.seq.page_size, turns = (max_keys + kTurn - 1) / kTurn;
-  const int room = (int)(turns < kTurns ? turns : kTurns) * kTurn;
-  static std::atomic<uint64_t> raised;
-  const hipError_t e = raise_lds(select_kernel, raised, kTurns * kTurn * 4);
-  return e != hipSuccess ? e : launch_kernel(select_kernel, grid, block, room * 4, stream, p, room);
+  const dim3 grid((unsigned)(rows < 65536 ? rows : 65536));
+  const int64_t max_keys = (int64_t)p.seq.max_pages * p.seq.page_size;
+  const int room = (int)(max_keys < kRoom ? (max_keys + 4095) / 4096 * 4096 : kRoom);   // LDS for what the table has room for
+  // With a row for every compute unit, smaller workgroups, two a unit, are less work: 512 rows of 4608 keys 13.2 us, with 1024 threads 14.2, with 256 14.7; 8 rows of 32768 keys 29.6, 22.3 and 50.7.
+  return rows >= 256 ? launch_select<512>(p, room, grid, stream) : launch_select<1024>(p, room, grid, stream);
 }
 
 hipError_t launch_cache_keep(const KeepParams& p, hipStream_t stream) {
