@@ -15,6 +15,7 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 
 constexpr float kLog2e = 1.4426950408889634f;
+constexpr int kFewWaves = 4;     // a SIMD, of few rows
 constexpr int kFewKeys = 256;    // of an item of few rows: 64 a wave
 constexpr int kManyKeys = 256;   // of many rows
 
@@ -47,8 +48,13 @@ __device__ __forceinline__ void item_at(const WeighParams& p, const Plan& plan, 
   int b = 0, before;
   locate(p, plan, at, [&](const Sequence& q) { return tiles_of_keys<WIDTH>(p, q) * p.Hkv; }, b, before);
   w.b = uniform(b);
-  const Sequence q = sequence(p.seq, w.b);
-  w.q = Sequence{uniform(q.start), uniform(q.n), uniform(q.len), uniform(q.pos)};
+  if (w.b < 64) {   // a lane has it
+    const Sequence& q = plan.first;
+    w.q = Sequence{__builtin_amdgcn_readlane(q.start, w.b), __builtin_amdgcn_readlane(q.n, w.b), __builtin_amdgcn_readlane(q.len, w.b), __builtin_amdgcn_readlane(q.pos, w.b)};
+  } else {
+    const Sequence q = sequence(p.seq, w.b);
+    w.q = Sequence{uniform(q.start), uniform(q.n), uniform(q.len), uniform(q.pos)};
+  }
   const int tiles = uniform(tiles_of_keys<WIDTH>(p, w.q)), i = uniform(at - before);
   w.hk = uniform(i / tiles);
   w.k0 = (i - w.hk * tiles) * WIDTH;
@@ -76,32 +82,40 @@ __device__ __forceinline__ void add_weight(const WeighParams& p, const WeighItem
 }
 
 // Few rows (a decode step, drafts): every wave has 64 keys, straight from memory into registers as the B operand of S = Q K^T; lane (i = lane % 16, g = lane / 16) then has
-// scores of key i with rows 4 g .. 4 g + 3 of 16.  Bound: HBM.
+// scores of key i with rows 4 g .. 4 g + 3 of 16.  The pages of the next item's keys are on their way beside this one's.  Bound: HBM.
 template <int D, bool F8>
-__global__ void __launch_bounds__(256) weigh_few_kernel(const WeighParams p) {
+__global__ void __launch_bounds__(256, kFewWaves) weigh_few_kernel(const WeighParams p) {
   constexpr int QS = D / 32, KL = F8 ? D / 64 : D / 32;
   const Plan plan = sums_plan(p);
-  const int total = uniform(all_items<kFewKeys>(p, plan)), each = (total + 7) >> 3, base = ((int)blockIdx.x & 7) * each;
+  const int total = uniform(all_items<kFewKeys>(p, plan)), each = (total + 7) >> 3, base = ((int)blockIdx.x & 7) * each, end = min(each, total - base);
   const int lane = threadIdx.x & 63, wave = uniform((int)threadIdx.x >> 6), i16 = lane & 15, g = lane >> 4;
   const float c2 = p.scale * kLog2e;
-  for (int at = (int)blockIdx.x >> 3; at < each && base + at < total; at += (int)gridDim.x >> 3) {
-    WeighItem w;
-    item_at<kFewKeys>(p, plan, base + at, w);
+  WeighItem w, next;
+  Slot mine = {-1, 0};   // of key key0 + lane
+  auto find = [&](int at, WeighItem& item, Slot& slot) __attribute__((always_inline)) {
+    slot = Slot{-1, 0};
+    if (at >= end) return;
+    item_at<kFewKeys>(p, plan, base + at, item);
+    const int key = item.k0 + wave * 64 + lane;
+    if (key < item.seen) slot = slot_of(p.seq, item.b, key);
+  };
+  find((int)blockIdx.x >> 3, next, mine);
+  for (int at = (int)blockIdx.x >> 3; at < end; at += (int)gridDim.x >> 3) {
+    w = next;
+    const Slot slot_now = mine;
     const int key0 = w.k0 + wave * 64, rows = w.q.n * p.gq;
-    if (key0 >= w.seen) continue;
-    Slot mine = {-1, 0};   // of key key0 + lane
-    if (key0 + lane < w.seen) mine = slot_of(p.seq, w.b, key0 + lane);
     u32x4 kr[4][KL];
     unsigned k_scale[4];
 #pragma unroll
     for (int h = 0; h < 4; h++) {   // 16 keys lie on one page
-      const int page = __builtin_amdgcn_readlane(mine.page, 16 * h), slot = __builtin_amdgcn_readlane(mine.slot, 16 * h);
+      const int page = __builtin_amdgcn_readlane(slot_now.page, 16 * h), slot = __builtin_amdgcn_readlane(slot_now.slot, 16 * h);
       k_scale[h] = 127;
       if (page >= 0) {
-        const char* const kp = p.k_pages + (int64_t)page * p.page_b + (int64_t)w.hk * p.head_b + (int64_t)slot * p.slot_b + (int64_t)i16 * p.slot_b + g * 16;
+        const char* const kp = p.k_pages + (int64_t)page * p.page_b + (int64_t)w.hk * p.head_b + (int64_t)slot * p.slot_b;
+        const unsigned off = (unsigned)(i16 * p.slot_b + g * 16);   // (slot_b is at most 2^25)
 #pragma unroll
-        for (int l = 0; l < KL; l++) kr[h][l] = *reinterpret_cast<const u32x4*>(kp + l * 64);
-        if constexpr (F8) k_scale[h] = p.k_scales[(int64_t)page * p.scale_sp + (int64_t)w.hk * p.scale_sh + slot + i16];
+        for (int l = 0; l < KL; l++) kr[h][l] = *reinterpret_cast<const u32x4*>(kp + off + l * 64);
+        if constexpr (F8) k_scale[h] = (p.k_scales + ((int64_t)page * p.scale_sp + (int64_t)w.hk * p.scale_sh + slot))[(unsigned)i16];
       } else {
 #pragma unroll
         for (int l = 0; l < KL; l++) kr[h][l] = u32x4{0, 0, 0, 0};
@@ -109,29 +123,33 @@ __global__ void __launch_bounds__(256) weigh_few_kernel(const WeighParams p) {
     }
     float old = 0.f;
     float* to = nullptr;
-    if (mine.page >= 0) {
-      to = p.weights + (int64_t)mine.page * p.w_sp + (int64_t)w.hk * p.w_sh + mine.slot;
+    if (slot_now.page >= 0) {
+      to = p.weights + (int64_t)slot_now.page * p.w_sp + (int64_t)w.hk * p.w_sh + slot_now.slot;
       const bool starts = p.fresh && key0 + lane >= w.q.pos && key0 + lane < w.q.pos + w.q.n;
       if (!starts) old = *to;
     }
     float sum = 0.f;   // of key key0 + lane
     for (int r0 = 0; r0 < rows; r0 += 16) {
       bf16x8 qf[QS];
-      const __bf16* const src = row_of(p, w, min(r0 + i16, rows - 1));
+      const int row = r0 + i16, t = divide(p.by_gq, min(row, rows - 1)), head = w.hk * p.gq + min(row, rows - 1) - t * p.gq;
+      const __bf16* const src = p.q + (int64_t)head * p.q_sh + (int64_t)(w.q.start + t) * p.q_ss;
 #pragma unroll
       for (int s = 0; s < QS; s++)   // d's in the order of the K loads
         qf[s] = *reinterpret_cast<const bf16x8*>(src + (F8 ? (s >> 1) * 64 + g * 16 + (s & 1) * 8 : s * 32 + g * 8));
+      const float lse = p.lse[(int64_t)head * p.l_sh + (int64_t)(w.q.start + t) * p.l_ss];
+      if (r0 == 0) find(at + ((int)gridDim.x >> 3), next, mine);   // (in front of what waits for the keys)
+      // the lane's row: what its exponents have taken off, and the keys that it sees, from key0 on
+      const bool live = row < rows && fabsf(lse) < INFINITY;
+      const float my_ref = live ? lse * kLog2e : INFINITY;
+      const int my_limit = live ? visible(w.q, t, p.causal) - key0 : 0;
+      const bool masked = __any(my_limit < 64);
       float ref[4];
-      int limit[4];   // keys that a row sees, from key0 on
-      bool edge = false;
+      int limit[4];
 #pragma unroll
       for (int r = 0; r < 4; r++) {
-        const int row = r0 + 4 * g + r;
-        ref[r] = row_reference(p, w, row, rows);
-        limit[r] = ref[r] == INFINITY ? 0 : visible(w.q, divide(p.by_gq, row), p.causal) - key0;
-        edge |= limit[r] < 64;
+        ref[r] = __shfl(my_ref, 4 * g + r);
+        limit[r] = __shfl(my_limit, 4 * g + r);
       }
-      const bool masked = __any(edge);
 #pragma unroll
       for (int h = 0; h < 4; h++) {
         f32x4 s = {0.f, 0.f, 0.f, 0.f};
@@ -297,7 +315,7 @@ hipError_t launch_form(WeighParams& p, hipStream_t stream) {
     const bool many = mixed ? part == 1 : !few;
     p.rows = mixed ? (many ? RowClass{32, 32, any} : RowClass{32, 0, 32}) : RowClass{32, 0, any};
     const int64_t width = many ? kManyKeys : kFewKeys, seqs = rows / (p.rows.over + 1) < n ? rows / (p.rows.over + 1) : n;
-    const int64_t items = seqs * p.Hkv * ((max_keys + width - 1) / width), most = many ? 512 : 2048;
+    const int64_t items = seqs * p.Hkv * ((max_keys + width - 1) / width), most = many ? 512 : 256 * kFewWaves;
     if (items == 0) continue;
     const dim3 grid((unsigned)((items < most ? items : most) + 7) / 8 * 8);
     const hipError_t e = many ? launch_kernel(weigh_many_kernel<D, F8>, grid, dim3(256), 0, stream, p) : launch_kernel(weigh_few_kernel<D, F8>, grid, dim3(256), 0, stream, p);
