@@ -3,6 +3,8 @@
 // weights[c] += sum over rows r that see c of exp(scale <q_r, K_c> - lse_r), a row being a (token, query head of the K/V head) pair: half of an attention's products, one
 // exponential a score, and sums down the rows instead of along the keys.  A workgroup has some keys and goes through all rows that see them, so that a
 // key's sum is one workgroup's, in one order, and K is read once.
+#include <type_traits>
+
 #include "evict.h"
 #include "paged_sums.h"
 
@@ -59,17 +61,6 @@ __device__ __forceinline__ void item_at(const WeighParams& p, const Plan& plan, 
   w.hk = uniform(i / tiles);
   w.k0 = (i - w.hk * tiles) * WIDTH;
   w.seen = uniform(seen_keys(p, w.q));
-}
-// What a row's exponents have taken off, in powers of two; infinity for rows that add nothing.
-__device__ __forceinline__ float row_reference(const WeighParams& p, const WeighItem& w, int r, int rows) {
-  if (r >= rows) return INFINITY;
-  const int t = divide(p.by_gq, r);
-  const float lse = p.lse[(int64_t)(w.hk * p.gq + r - t * p.gq) * p.l_sh + (int64_t)(w.q.start + t) * p.l_ss];
-  return fabsf(lse) < INFINITY ? lse * kLog2e : INFINITY;
-}
-__device__ __forceinline__ const __bf16* row_of(const WeighParams& p, const WeighItem& w, int r) {
-  const int t = divide(p.by_gq, r);
-  return p.q + (int64_t)(w.hk * p.gq + r - t * p.gq) * p.q_sh + (int64_t)(w.q.start + t) * p.q_ss;
 }
 // Adds to a key's weight, if it has a page.
 __device__ __forceinline__ void add_weight(const WeighParams& p, const WeighItem& w, int key, float sum) {
@@ -180,26 +171,97 @@ __global__ void __launch_bounds__(256, kFewWaves) weigh_few_kernel(const WeighPa
   }
 }
 
-// Many rows (a prompt's chunk): every wave has 64 keys in registers, as the A operand of S^T = K Q^T, and goes through the rows 32 at a time, which the workgroup brings into LDS.
+// Many rows (a prompt's chunk): every wave has 64 keys in registers, as the A operand of S^T = K Q^T, and goes through the rows 32 at a time, which the workgroup brings into LDS.  The
+// products of a tile of rows run beside the exponentials of the one in front, and the operands of the one behind are fetched in the places of those that have been used.
 template <int D>
 struct Many {
   static constexpr int RB = 2 * D, TILE = 32 * RB;             // bytes of a row, of a tile of rows
   static constexpr int SUMS = 4 * 64 * 33 * 4;                 // where the waves add up their lanes' sums
   static constexpr int LDS = 2 * TILE > SUMS ? 2 * TILE : SUMS;
 };
+// Every 32nd row of an item, a (token, query head) pair: where it is, by additions.
+struct RowStep {
+  int t, j;
+  int64_t off, wrap;
+};
+__device__ __forceinline__ RowStep row_step(const WeighParams& p, int64_t sh, int64_t ss) {
+  const int t = uniform(divide(p.by_gq, 32)), j = 32 - t * p.gq;
+  return RowStep{t, j, j * sh + t * ss, ss - p.gq * sh};
+}
+struct Row {
+  int t, j;
+  int64_t off;
+};
+__device__ __forceinline__ Row row_at(const WeighParams& p, int r, int64_t sh, int64_t ss) {
+  const int t = divide(p.by_gq, r), j = r - t * p.gq;
+  return Row{t, j, j * sh + t * ss};
+}
+__device__ __forceinline__ void advance(const WeighParams& p, Row& r, const RowStep& by) {
+  r.t += by.t;
+  r.off += by.off;
+  if (by.j == 0) return;
+  r.j += by.j;
+  if (r.j >= p.gq) {
+    r.j -= p.gq;
+    r.t++;
+    r.off += by.wrap;
+  }
+}
 template <int D, bool F8>
 __global__ void __launch_bounds__(256, 2) weigh_many_kernel(const WeighParams p) {
   typedef Many<D> M;
-  constexpr int KS = D / 16, CPR = D / 8, LOADS = M::TILE / 4096;   // 16-byte loads a thread and tile
+  constexpr int KS = D / 16, CPR = D / 8, LOADS = M::TILE / 4096, EACH = 16 / KS;   // 16-byte loads a thread and tile; exponentials a product
   __shared__ __attribute__((aligned(1024))) char lds[M::LDS];
   const Plan plan = sums_plan(p);
   const int total = uniform(all_items<kManyKeys>(p, plan)), each = (total + 7) >> 3, base = ((int)blockIdx.x & 7) * each;
   const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), l32 = lane & 31, hf = lane >> 5;
   const float c2 = p.scale * kLog2e;
+  const RowStep q_step = row_step(p, p.q_sh, p.q_ss), l_step = row_step(p, p.l_sh, p.l_ss);
+#pragma unroll 1
   for (int at = (int)blockIdx.x >> 3; at < each && base + at < total; at += (int)gridDim.x >> 3) {
     WeighItem w;
     item_at<kManyKeys>(p, plan, base + at, w);
     const int key0 = w.k0 + wave * 64, rows = w.q.n * p.gq;
+    // rows from the first that sees the item's first key
+    const int first = p.causal ? clamped(w.k0 - w.q.pos, 0, w.q.n) * p.gq / 32 : 0, tiles = (rows + 31) / 32;
+    const __bf16* const q_base = p.q + (int64_t)w.hk * p.gq * p.q_sh + (int64_t)w.q.start * p.q_ss;
+    const float* const l_base = p.lse + (int64_t)w.hk * p.gq * p.l_sh + (int64_t)w.q.start * p.l_ss;
+    Row q_row[LOADS], l_row = row_at(p, first * 32 + l32, p.l_sh, p.l_ss);   // of the next tile to be fetched
+#pragma unroll
+    for (int i = 0; i < LOADS; i++) q_row[i] = row_at(p, first * 32 + (i * 256 + tid) / CPR, p.q_sh, p.q_ss);
+    u32x4 coming[LOADS];
+    float lse_coming;
+    int t_coming;
+    auto fetch = [&]() __attribute__((always_inline)) {   // (in the place of rows behind the last the first is read)
+#pragma unroll
+      for (int i = 0; i < LOADS; i++) {
+        const int64_t off = q_row[i].t < w.q.n ? q_row[i].off : 0;
+        coming[i] = *reinterpret_cast<const u32x4*>(q_base + off + tid % CPR * 8);
+        advance(p, q_row[i], q_step);
+      }
+      t_coming = l_row.t;
+      lse_coming = l_base[l_row.t < w.q.n ? l_row.off : 0];
+      advance(p, l_row, l_step);
+    };
+    auto put = [&](int tile) __attribute__((always_inline)) {
+#pragma unroll
+      for (int i = 0; i < LOADS; i++) {
+        const int r = (i * 256 + tid) / CPR, c = tid % CPR;
+        *reinterpret_cast<u32x4*>(lds + (tile & 1) * M::TILE + r * M::RB + ((c ^ (r % CPR)) << 4)) = coming[i];
+      }
+    };
+    // of the lane's row: what its exponents have taken off (infinity: it adds nothing), and the keys that it sees, from key0 on
+    struct Shown { float ref; int limit; };
+    auto shown = [&]() __attribute__((always_inline)) -> Shown {
+      const bool live = t_coming < w.q.n && fabsf(lse_coming) < INFINITY;
+      return Shown{live ? lse_coming * kLog2e : INFINITY, live ? visible(w.q, t_coming, p.causal) - key0 : 0};
+    };
+    const unsigned operand0 = l32 * M::RB + ((l32 % CPR ^ (F8 ? 2 * hf : hf)) << 4);   // of the lane's chunk 0
+    auto operand = [&](unsigned tile0, int ks) __attribute__((always_inline)) -> bf16x8 {
+      const int c = F8 ? 4 * (ks >> 1) + (ks & 1) : 2 * ks;
+      return *reinterpret_cast<const bf16x8*>(lds + (tile0 ^ (c << 4)));
+    };
+
     bf16x8 kf[2][KS];   // lane (l, hf): K[l][d's of the load order]
 #pragma unroll
     for (int h = 0; h < 2; h++) {
@@ -226,70 +288,78 @@ __global__ void __launch_bounds__(256, 2) weigh_many_kernel(const WeighParams p)
 #pragma unroll
       for (int i = 0; i < 16; i++) acc[h][i] = 0.f;
 
-    // rows from the first that sees the item's first key
-    const int first = p.causal ? clamped(w.k0 - w.q.pos, 0, w.q.n) * p.gq / 32 : 0, tiles = (rows + 31) / 32;
-    u32x4 next[LOADS];
-    float next_ref;
-    int next_limit;
-    auto fetch = [&](int tile) __attribute__((always_inline)) {
-#pragma unroll
-      for (int i = 0; i < LOADS; i++) {
-        const int n = i * 256 + tid, r = n / CPR, c = n % CPR;
-        next[i] = *reinterpret_cast<const u32x4*>(row_of(p, w, min(tile * 32 + r, rows - 1)) + 8 * c);
-      }
-      const int r = tile * 32 + l32;
-      next_ref = row_reference(p, w, r, rows);
-      next_limit = next_ref == INFINITY ? 0 : visible(w.q, divide(p.by_gq, r), p.causal) - key0;
-    };
-    auto put = [&](int half) __attribute__((always_inline)) {
-#pragma unroll
-      for (int i = 0; i < LOADS; i++) {
-        const int n = i * 256 + tid, r = n / CPR, c = n % CPR;
-        *reinterpret_cast<u32x4*>(lds + half * M::TILE + r * M::RB + ((c ^ (r % CPR)) << 4)) = next[i];
-      }
-    };
     __syncthreads();   // the sums of the item before have been read
-    if (first < tiles) {
-      fetch(first);
-      put(first & 1);
+    fetch();
+    put(first);
+    Shown now = shown();
+    fetch();
+    put(first + 1);
+    Shown next = shown();
+    fetch();
+    __syncthreads();
+    f32x16 s[2];   // of the tile whose exponentials are next
+    bf16x8 qf[KS];
+#pragma unroll
+    for (int ks = 0; ks < KS; ks++) qf[ks] = operand(operand0 + (first & 1) * M::TILE, ks);
+#pragma unroll
+    for (int h = 0; h < 2; h++) {
+#pragma unroll
+      for (int i = 0; i < 16; i++) s[h][i] = 0.f;
+#pragma unroll
+      for (int ks = 0; ks < KS; ks++) s[h] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[h][ks], qf[ks], s[h], 0, 0, 0);
     }
-    float ref = next_ref;
-    int limit = next_limit;
-    for (int t = first; t < tiles; t++) {
-      if (t + 1 < tiles) fetch(t + 1);
-      __syncthreads();
-      if (__any(limit > 0)) {
-        bf16x8 qf[KS];
+#pragma unroll
+    for (int ks = 0; ks < KS; ks++) qf[ks] = operand(operand0 + ((first + 1) & 1) * M::TILE, ks);
+    __syncthreads();   // the first two tiles have been read
+    // Exponentials of tile t beside the products of tile t + 1, whose operands are in registers; those of tile t + 2 take their places.
+    auto step = [&](int t, auto masked_c) __attribute__((always_inline)) {
+      constexpr bool MASKED = decltype(masked_c)::value;
+      const unsigned tile0 = operand0 + (t & 1) * M::TILE;
+      float ref = now.ref;
+      asm volatile("" : "+v"(ref));   // (or, as at the sums, the compiler draws what both kinds of steps have in common out of them, and spills registers)
+#pragma unroll
+      for (int h = 0; h < 2; h++) {
+        f32x16 made;
+#pragma unroll
+        for (int i = 0; i < 16; i++) made[i] = 0.f;
+        float x[16];
+        auto take = [&](int i0) __attribute__((always_inline)) {
+#pragma unroll
+          for (int i = i0; i < i0 + EACH; i++) {
+            acc[h][i] += !MASKED || 32 * h + 8 * (i >> 2) + 4 * hf + (i & 3) < now.limit ? x[i] : 0.f;
+            asm volatile("" : "+v"(acc[h][i]));
+          }
+        };
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int ks = 0; ks < KS; ks++) {
-          const int c = F8 ? 4 * (ks >> 1) + 2 * hf + (ks & 1) : 2 * ks + hf;
-          qf[ks] = *reinterpret_cast<const bf16x8*>(lds + (t & 1) * M::TILE + l32 * M::RB + ((c ^ (l32 % CPR)) << 4));
+          made = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[h][ks], qf[ks], made, 0, 0, 0);
+          if (h == 1) qf[ks] = operand(tile0, ks);
+#pragma unroll
+          for (int i = ks * EACH; i < (ks + 1) * EACH; i++) x[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[h][i], c2, -ref));
+          if (ks > 0) take((ks - 1) * EACH);
+          __builtin_amdgcn_sched_barrier(0);
         }
-        const bool masked = __any(limit < 64);
-#pragma unroll
-        for (int h = 0; h < 2; h++) {
-          f32x16 s;
-#pragma unroll
-          for (int i = 0; i < 16; i++) s[i] = 0.f;
-#pragma unroll
-          for (int ks = 0; ks < KS; ks++) s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[h][ks], qf[ks], s, 0, 0, 0);
-          if (masked) {
-#pragma unroll
-            for (int i = 0; i < 16; i++) {
-              const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i], c2, -ref));
-              acc[h][i] += 32 * h + 8 * (i >> 2) + 4 * hf + (i & 3) < limit ? e : 0.f;
-            }
-          } else {
-#pragma unroll
-            for (int i = 0; i < 16; i++) acc[h][i] += __builtin_amdgcn_exp2f(__builtin_fmaf(s[i], c2, -ref));
-          }
-        }
+        take(16 - EACH);
+        s[h] = made;
       }
-      if (t + 1 < tiles) {
-        put((t + 1) & 1);
-        ref = next_ref;
-        limit = next_limit;
-      }
+    };
+    int t = first;
+    auto turn = [&](auto masked_c) __attribute__((always_inline)) {
+      put(t + 2);   // (behind the last tile: rows that add nothing)
+      const Shown after = shown();
+      fetch();
+      __syncthreads();
+      step(t, masked_c);
+      now = next;
+      next = after;
+      t++;
+    };
+    while (t < tiles) {   // (a loop for either kind: where they meet the compiler moves all sums from some registers to others)
+#pragma unroll 1
+      while (t < tiles && !__any(now.limit < 64)) turn(std::false_type{});
+#pragma unroll 1
+      while (t < tiles && __any(now.limit < 64)) turn(std::true_type{});
     }
     __syncthreads();
     float* const sums = reinterpret_cast<float*>(lds) + wave * 64 * 33;
