@@ -293,35 +293,25 @@ __global__ void __launch_bounds__(256, 2) weigh_many_kernel(const WeighParams p)
     put(first);
     Shown now = shown();
     fetch();
-    put(first + 1);
-    Shown next = shown();
-    fetch();
     __syncthreads();
-    f32x16 s[2];   // of the tile whose exponentials are next
-    bf16x8 qf[KS];
+    f32x16 s[2];     // scores of the two blocks of 32 keys: one's exponentials beside the other's products
+    bf16x8 qf[KS];   // operands of the rows whose products come next
 #pragma unroll
     for (int ks = 0; ks < KS; ks++) qf[ks] = operand(operand0 + (first & 1) * M::TILE, ks);
 #pragma unroll
-    for (int h = 0; h < 2; h++) {
+    for (int i = 0; i < 16; i++) s[0][i] = 0.f;
 #pragma unroll
-      for (int i = 0; i < 16; i++) s[h][i] = 0.f;
-#pragma unroll
-      for (int ks = 0; ks < KS; ks++) s[h] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[h][ks], qf[ks], s[h], 0, 0, 0);
-    }
-#pragma unroll
-    for (int ks = 0; ks < KS; ks++) qf[ks] = operand(operand0 + ((first + 1) & 1) * M::TILE, ks);
-    __syncthreads();   // the first two tiles have been read
-    // Exponentials of tile t beside the products of tile t + 1, whose operands are in registers; those of tile t + 2 take their places.
+    for (int ks = 0; ks < KS; ks++) s[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[0][ks], qf[ks], s[0], 0, 0, 0);
+    // Exponentials of tile t: the first block's beside the second's products with the same rows, the second's beside the first's with the next ones, whose operands are fetched in between.
     auto step = [&](int t, auto masked_c) __attribute__((always_inline)) {
       constexpr bool MASKED = decltype(masked_c)::value;
-      const unsigned tile0 = operand0 + (t & 1) * M::TILE;
+      const unsigned tile0 = operand0 + ((t + 1) & 1) * M::TILE;
       float ref = now.ref;
       asm volatile("" : "+v"(ref));   // (or, as at the sums, the compiler draws what both kinds of steps have in common out of them, and spills registers)
 #pragma unroll
       for (int h = 0; h < 2; h++) {
-        f32x16 made;
 #pragma unroll
-        for (int i = 0; i < 16; i++) made[i] = 0.f;
+        for (int i = 0; i < 16; i++) s[1 - h][i] = 0.f;
         float x[16];
         auto take = [&](int i0) __attribute__((always_inline)) {
 #pragma unroll
@@ -333,26 +323,24 @@ __global__ void __launch_bounds__(256, 2) weigh_many_kernel(const WeighParams p)
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int ks = 0; ks < KS; ks++) {
-          made = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[h][ks], qf[ks], made, 0, 0, 0);
-          if (h == 1) qf[ks] = operand(tile0, ks);
+          s[1 - h] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[1 - h][ks], qf[ks], s[1 - h], 0, 0, 0);
+          if (h == 0) qf[ks] = operand(tile0, ks);
 #pragma unroll
           for (int i = ks * EACH; i < (ks + 1) * EACH; i++) x[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[h][i], c2, -ref));
           if (ks > 0) take((ks - 1) * EACH);
           __builtin_amdgcn_sched_barrier(0);
         }
         take(16 - EACH);
-        s[h] = made;
       }
     };
     int t = first;
     auto turn = [&](auto masked_c) __attribute__((always_inline)) {
-      put(t + 2);   // (behind the last tile: rows that add nothing)
-      const Shown after = shown();
+      put(t + 1);   // (behind the last tile: rows that add nothing)
+      const Shown next = shown();
       fetch();
       __syncthreads();
       step(t, masked_c);
       now = next;
-      next = after;
       t++;
     };
     while (t < tiles) {   // (a loop for either kind: where they meet the compiler moves all sums from some registers to others)
