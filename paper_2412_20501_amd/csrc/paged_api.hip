@@ -45,12 +45,12 @@ tr_status take_tree(const tr_tree& tree, int64_t tokens, tr::TreeParams& p, SeqV
   return TR_OK;
 }
 
-size_t workspace_bytes_of(const tr_tensor* q, const tr_tensor* k_pages, int64_t n_seqs, int64_t max_pages) {
+size_t workspace_bytes_of(const tr_tensor* q, const tr_tensor* k_pages, int64_t n_seqs, int64_t max_pages, bool tree) {
   if (!q || !k_pages || q->dtype != TR_BF16 || q->B != 1 || q->S < 0 || q->S > kMaxKeys || q->H < 0 || q->H > INT32_MAX || (q->D != 64 && q->D != 128)) return 0;
   if ((k_pages->dtype != TR_BF16 && k_pages->dtype != TR_F8E4M3) || k_pages->B < 0 || k_pages->H < 1 || q->H % k_pages->H || k_pages->D != q->D || k_pages->S < 16 || k_pages->S % 16) return 0;
   if (n_seqs < 0 || n_seqs > kMaxAttended || max_pages < 0 || max_pages > kMaxKeys / k_pages->S || q->S * q->H >= ((int64_t)1 << 31)) return 0;
   if (q->S == 0 || q->H == 0 || n_seqs == 0) return 0;
-  const tr::PagedLaunch l = tr::paged_launch(q->S, n_seqs, max_pages * k_pages->S, (int)k_pages->H, (int)(q->H / k_pages->H), (int)q->D, k_pages->dtype == TR_F8E4M3);
+  const tr::PagedLaunch l = tr::paged_launch(q->S, n_seqs, max_pages * k_pages->S, (int)k_pages->H, (int)(q->H / k_pages->H), (int)q->D, k_pages->dtype == TR_F8E4M3, tree);
   int64_t floats = 0;
   for (int i = 0; i < l.n; i++) floats += l.part[i].floats((int)q->D);
   return (size_t)floats * 4;
@@ -96,10 +96,10 @@ tr_status attend(const tr_tensor* q_, const tr_tensor* k_pages_, const tr_tensor
   if (q->H == 0 || q->S == 0 || p.seq.n == 0) return TR_OK;
 
   const int gq = (int)(q->H / k_pages->H), D = (int)q->D;
-  const tr::PagedLaunch l = tr::paged_launch(q->S, p.seq.n, (int64_t)p.seq.max_pages * p.seq.page_size, (int)k_pages->H, gq, D, k_scales != nullptr);
+  const tr::PagedLaunch l = tr::paged_launch(q->S, p.seq.n, (int64_t)p.seq.max_pages * p.seq.page_size, (int)k_pages->H, gq, D, k_scales != nullptr, tree != nullptr);
   for (int i = 0; i < l.n; i++)
     if (l.part[i].tiles + l.part[i].share.most() >= ((int64_t)1 << 23) - 8) return fail(TR_ERR_SHAPE, "too many workgroups for one launch");   // (of 512 threads, fewer than 2^32 in all)
-  const size_t need = workspace_bytes_of(q, k_pages, seqs->n_seqs, seqs->max_pages);
+  const size_t need = workspace_bytes_of(q, k_pages, seqs->n_seqs, seqs->max_pages, tree != nullptr);
   if (workspace && need > 0) {
     if ((uintptr_t)workspace % 256) return fail(TR_ERR_WORKSPACE, "workspace must be 256-byte aligned");
     if (workspace_bytes < need) return fail(TR_ERR_WORKSPACE, "workspace too small: %zu < %zu bytes", workspace_bytes, need);
@@ -213,10 +213,10 @@ tr_status tr_cache_read(const tr_tensor* k_pages_, const tr_tensor* v_pages_, co
 }
 
 size_t tr_paged_attn_workspace_bytes(const tr_tensor* q, const tr_tensor* k_pages, int64_t n_seqs, int64_t max_pages) {
-  return workspace_bytes_of(q, k_pages, n_seqs, max_pages);
+  return workspace_bytes_of(q, k_pages, n_seqs, max_pages, false);
 }
 size_t tr_paged_attn_tree_workspace_bytes(const tr_tensor* q, const tr_tensor* k_pages, int64_t n_seqs, int64_t max_pages) {
-  return workspace_bytes_of(q, k_pages, n_seqs, max_pages);
+  return workspace_bytes_of(q, k_pages, n_seqs, max_pages, true);
 }
 
 tr_status tr_paged_attn(const tr_tensor* q, const tr_tensor* k_pages, const tr_tensor* v_pages, const tr_tensor* k_scales, const tr_tensor* v_scales,

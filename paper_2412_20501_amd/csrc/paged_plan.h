@@ -153,15 +153,15 @@ struct PagedLaunch {
 };
 // The launches of a call.  The lengths are not known here, so it goes by the average rows of a sequence and K/V head: up to 32, sequences are taken to be
 // of single tokens and drafts, and workgroups of 16 or 32 rows serve them all; a lone sequence of more is one of many rows; several are a mixture,
-// a launch for either kind.
-inline PagedLaunch paged_launch(int64_t tokens, int64_t n_seqs, int64_t max_keys, int Hkv, int gq, int D, bool f8) {
+// a launch for either kind.  The sequences of a tree's call are taken to be alike: one launch.
+inline PagedLaunch paged_launch(int64_t tokens, int64_t n_seqs, int64_t max_keys, int Hkv, int gq, int D, bool f8, bool tree = false) {
   PagedLaunch l;
   const int64_t rows = tokens * gq;
   constexpr int any = 0x7fffffff;
   const RowClass few16 = {16, 0, any}, few32 = {32, 0, any}, many = {kManyRows, 0, any};
   const int few = gq <= 4 ? 16 : 32;   // rows of few tokens in a mixture: 16 / gq tokens (4 at groups of 4), 32 / gq beyond (4 at 8, 2 at 16, none above 32)
   const RowClass only_few = {few, 0, few}, only_many = {kManyRows, few, any};
-  const bool mixed = rows > 32 * n_seqs && n_seqs > 1;
+  const bool mixed = !tree && rows > 32 * n_seqs && n_seqs > 1;
   l.n = mixed ? 2 : 1;
   l.part[0].rows = mixed ? only_few : rows <= 16 * n_seqs ? few16 : rows <= 32 * n_seqs ? few32 : many;
   l.part[1].rows = only_many;
