@@ -59,9 +59,7 @@ __device__ __forceinline__ int v_tile_off(int row, int c) {   // the same of a V
 }
 
 // true: done; false: the item needs the other way (nothing has been written)
-//
-// SPLIT: up to 128 rows of e4m3 keys.  They leave half of the waves without any, and its tiles are done before the next ones' loads are back: so those waves bring in the tiles of all, RING pairs ahead, two shares each.
-template <int D, bool F8, bool OUT_F32, bool SPLIT, typename P>
+template <int D, bool F8, bool OUT_F32, typename P>
 __device__ __forceinline__ bool tile_rows(const P& p, const Item& w, int slot_row, char* lds) {
   typedef Tile<D> T;
   constexpr int RB = T::RB, BN = T::BN, NS = T::NS, TILE_BYTES = T::TILE_BYTES, KS = D / 16, DB = D / 32, CPR = D / 8, SUB = 32, NSW = BN / SUB;
@@ -90,11 +88,10 @@ __device__ __forceinline__ bool tile_rows(const P& p, const Item& w, int slot_ro
     const int i = divide(p.seq.by_page, uniform(key));
     return Place{(int)min((unsigned)table[i], last_page), key - i * p.seq.page_size};
   };
-  auto last_slot_of = [&](int of, int row) __attribute__((always_inline)) -> int {   // of a row of the last tile in its group
-    const int first = (w.k0 + of * SHARE + last_tile * BN) & ~15, group = min(first, (end - 1) & ~15);
+  auto last_slot = [&](int row) __attribute__((always_inline)) -> int {   // of a row of the last tile in its group
+    const int first = (share0 + last_tile * BN) & ~15, group = min(first, (end - 1) & ~15);
     return min(w.k0 + last_tile * BN + row, end - 1) - group;
   };
-  auto last_slot = [&](int row) __attribute__((always_inline)) -> int { return last_slot_of(wave, row); };
   const unsigned lds_base = (unsigned)(unsigned long)(lds_ptr_t)lds;
   // Byte offsets of the lane's loads from its group of 16 keys.  In the last tile rows behind the end take the last key's place; what that changes is counted
   // anew there, to be held in no register (at D 128 there is none left), like a lane's place in e4m3 tiles: 16 values of a row, whose slot is also its scale's.
@@ -143,11 +140,11 @@ __device__ __forceinline__ bool tile_rows(const P& p, const Item& w, int slot_ro
     r.x = *(global_u32x4)((global_bytes)(uintptr_t)src + (unsigned)(slot * p.slot_b + l % L8 * 16));
     r.scale = ((global_bytes)(uintptr_t)s)[(unsigned)slot];
   };
-  auto put8_of = [&](int of, const Raw& r, int tile, int l, auto is_v_c, bool edge) __attribute__((always_inline)) {
+  auto put8 = [&](const Raw& r, int tile, int l, auto is_v_c, bool edge) __attribute__((always_inline)) {
     constexpr bool V = decltype(is_v_c)::value != 0;
     const u32x4 lo = {f8_pair(r.x[0], false, r.scale), f8_pair(r.x[0], true, r.scale), f8_pair(r.x[1], false, r.scale), f8_pair(r.x[1], true, r.scale)};
     const u32x4 hi = {f8_pair(r.x[2], false, r.scale), f8_pair(r.x[2], true, r.scale), f8_pair(r.x[3], false, r.scale), f8_pair(r.x[3], true, r.scale)};
-    const int row = of * SHARE + l / L8, to = V ? v_tile_off<D>(row, l % L8 * 2) : k_tile_off<D>(row, l % L8 * 2);
+    const int row = wave * SHARE + l / L8, to = V ? v_tile_off<D>(row, l % L8 * 2) : k_tile_off<D>(row, l % L8 * 2);
     *reinterpret_cast<u32x4*>(lds + tile + to) = lo;
     *reinterpret_cast<u32x4*>(lds + tile + (to ^ 16)) = hi;   // the chunk beside it, in either order
     if (V && edge) {
@@ -155,7 +152,6 @@ __device__ __forceinline__ bool tile_rows(const P& p, const Item& w, int slot_ro
       look(hi);
     }
   };
-  auto put8 = [&](const Raw& r, int tile, int l, auto is_v_c, bool edge) __attribute__((always_inline)) { put8_of(wave, r, tile, l, is_v_c, edge); };
   auto send = [&](const char* base, Place at, bool last, const unsigned (&off)[IPW], bool v, int lds_off) __attribute__((always_inline)) {
     const char* const src = uniform_at(base, (int64_t)at.page * p.page_b + (int64_t)at.slot * p.slot_b);
     if (last) {
@@ -403,19 +399,13 @@ __device__ __forceinline__ bool tile_rows(const P& p, const Item& w, int slot_ro
     constexpr unsigned v_imm = kt == 0 ? sp * TILE_BYTES + (NSW - 1) * SUBB : su * TILE_BYTES + (kt - 1) * SUBB;
     constexpr unsigned k_imm = (su + (kt + 2) / NSW) % NS * TILE_BYTES + (kt + 2) % NSW * SUBB;
     const int j = NSW * u + kt;
-    if (INNER || j <= (kt == 0 ? jw_first : jw_in)) {
+    if (INNER ? !is_tree<P> || rows_here : j <= (kt == 0 ? jw_first : jw_in)) {
       if (even) step(j * SUB, IC<0>{}, IC<(int)v_imm>{}, IC<(int)k_imm>{}, sA, sB, pB, pA, inner_c);
       else step(j * SUB, IC<0>{}, IC<(int)v_imm>{}, IC<(int)k_imm>{}, sB, sA, pA, pB, inner_c);
     }
   };
   if (n_tiles > 0) {
-    if constexpr (SPLIT) {   // (what the prologue has in registers; the next pairs are the other waves')
-      const int l = lane_anew();
-      if (3 <= last_tile) put8(k_raw, 3 * TILE_BYTES, l, IC<0>{}, false);
-      if (2 <= last_tile) put8(v_raw, (NS + 2) * TILE_BYTES, l, IC<1>{}, 2 >= edge_tile);
-    } else {
-      pair(3, 2, IC<0>{});
-    }
+    pair(3, 2, IC<0>{});
     if (jw > 0) {
 #pragma unroll
       for (int i = 0; i < 16; i++) sA[i] = 0.f;
@@ -449,7 +439,7 @@ __device__ __forceinline__ bool tile_rows(const P& p, const Item& w, int slot_ro
     asm volatile("" ::: "memory");
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
-    if constexpr (!SPLIT) pair((su + 3) % NS, (su + 2) % NS, inner_c);
+    pair((su + 3) % NS, (su + 2) % NS, inner_c);
     tile_step(u, su_c, IC<0>{}, inner_c);
     tile_step(u, su_c, IC<1>{}, inner_c);
     if constexpr (NSW > 2) {
@@ -459,79 +449,10 @@ __device__ __forceinline__ bool tile_rows(const P& p, const Item& w, int slot_ro
   };
   // Inner tiles: every step runs in this wave without a mask, and what they send lies in front of the last tile.  Waves may disagree about where they
   // end: both bodies hold the same barrier and the same number of loads.
-  const int j_inner = min(min(jw, NSW * n_tiles - 1), kmask_from >= 0 ? kmask_from / SUB : -1) - (NSW - 1);
+  // A tree's few rows may leave waves without any.  Those too send inner tiles as inner ones, or all wait for them: loads that may be left out are waited for at once (16 trees of 100 rows in
+  // 8 bits 78 -> 69 us).
+  const int j_inner = is_tree<P> && !rows_here ? kPosLimit : min(min(jw, NSW * n_tiles - 1), kmask_from >= 0 ? kmask_from / SUB : -1) - (NSW - 1);
   const int u_inner = uniform(min(min(j_inner < 0 ? -1 : j_inner / NSW, last_tile - (F8 ? 6 : 5)), edge_tile - 3));
-  if constexpr (SPLIT) {
-    if (wave >= 4) {
-      // Pair a = u + 3 (K of tile a, V of tile a - 1) goes out behind barrier B_u, as above, and pair a + RING is asked for in its place.
-      constexpr int RING = NS;
-      const int l = lane_anew();
-      Raw rk[RING][2], rv[RING][2];
-      struct Offset { int64_t pages, scales; };   // of a share of a tile
-      struct Found { int page, slot; };           // as the table has it
-      const unsigned char* const ksb = p.k_scales + (int64_t)w.hk * p.scale_sh;
-      const unsigned char* const vsb = p.v_scales + (int64_t)w.hk * p.scale_sh;
-      Offset before[2];                           // of tile b - 1
-      Found now[2], next[2];                      // of tiles b and b + 1: looked up a pair ahead
-      auto look_up = [&](int of, int t) __attribute__((always_inline)) -> Found {
-        const int key = min((w.k0 + of * SHARE + min(t, last_tile) * BN) & ~15, (end - 1) & ~15), i = divide(p.seq.by_page, uniform(key));
-        return Found{table[i], key - i * p.seq.page_size};
-      };
-      auto offset_of = [&](Found f) __attribute__((always_inline)) -> Offset {
-        const int64_t page = min((unsigned)f.page, last_page);
-        return Offset{page * p.page_b + (int64_t)f.slot * p.slot_b, page * p.scale_sp + f.slot};
-      };
-      auto get = [&](int of, const char* pages, const unsigned char* scales, Offset at, bool last, Raw& r) __attribute__((always_inline)) {
-        const int row = of * SHARE + l / L8, slot = last ? last_slot_of(of, row) : row & 15;
-        r.x = *(global_u32x4)((global_bytes)(uintptr_t)(pages + at.pages) + (unsigned)(slot * p.slot_b + l % L8 * 16));
-        r.scale = ((global_bytes)(uintptr_t)(scales + at.scales))[(unsigned)slot];
-      };
-      auto ask = [&](int b, int slot) __attribute__((always_inline)) {   // (behind the last tile that once more, never read: with loads that may be left out all are waited for)
-#pragma unroll
-        for (int i = 0; i < 2; i++) {
-          const int of = wave - 4 + 4 * i;
-          const Offset at = offset_of(now[i]);
-          get(of, kb, ksb, at, b >= last_tile, rk[slot][i]);
-          get(of, vb, vsb, before[i], b - 1 >= last_tile, rv[slot][i]);
-          before[i] = at;
-          now[i] = next[i];
-          next[i] = look_up(of, b + 2);
-        }
-      };
-      if (n_tiles > 0) {
-#pragma unroll
-        for (int i = 0; i < 2; i++) {
-          const int of = wave - 4 + 4 * i;
-          before[i] = offset_of(look_up(of, 3));
-          now[i] = look_up(of, 4);
-          next[i] = look_up(of, 5);
-        }
-#pragma unroll
-        for (int i = 0; i < RING; i++) ask(4 + i, i);
-      }
-      for (int u0 = 1; u0 <= n_tiles; u0 += NS) {
-#pragma unroll
-        for (int i = 0; i < NS; i++) {   // u = u0 + i, u mod NS = (1 + i) mod NS
-          const int u = u0 + i, b = u + 3;
-          if (u > n_tiles) break;
-          __builtin_amdgcn_s_waitcnt(0xC07F);
-          asm volatile("" ::: "memory");
-          __builtin_amdgcn_s_barrier();
-          asm volatile("" ::: "memory");
-#pragma unroll
-          for (int k = 0; k < 2; k++) {
-            const int of = wave - 4 + 4 * k;
-            if (b <= last_tile) put8_of(of, rk[i][k], (i + 4) % NS * TILE_BYTES, l, IC<0>{}, false);
-            if (b - 1 <= last_tile) put8_of(of, rv[i][k], (NS + (i + 3) % NS) * TILE_BYTES, l, IC<1>{}, b - 1 >= edge_tile);
-          }
-          ask(b + RING, i);
-        }
-      }
-      if (__any(bad != 0) && lane == 0) *reinterpret_cast<int*>(lds + T::FLAG) = 1;
-      __syncthreads();   // (with the other waves' below)
-      return *reinterpret_cast<volatile int*>(lds + T::FLAG) == 0;
-    }
-  }
   if (1 <= n_tiles) tile_body(1, IC<1>{}, IC<0>{});
   if (2 <= n_tiles) tile_body(2, IC<2>{}, IC<0>{});
   if (3 <= n_tiles) tile_body(3, IC<3>{}, IC<0>{});
@@ -609,11 +530,7 @@ __global__ void __launch_bounds__(512, 2) paged_many_kernel(const P p) {
   Item w;
   if (!find_item(p, make_plan(p), (int)blockIdx.x, w)) return;
   const int row0 = w.tile * kManyRows, slot_row = w.slot * kManyRows, n = min(kManyRows, w.rows - row0);
-  if constexpr (F8 && is_tree<P>) {
-    if (n <= 128 ? tile_rows<D, F8, OUT_F32, true>(p, w, slot_row, lds) : tile_rows<D, F8, OUT_F32, false>(p, w, slot_row, lds)) return;
-  } else {
-    if (tile_rows<D, F8, OUT_F32, false>(p, w, slot_row, lds)) return;
-  }
+  if (tile_rows<D, F8, OUT_F32>(p, w, slot_row, lds)) return;
 #pragma unroll 1
   for (int r = 0; r < n; r += 16) {
     __syncthreads();
