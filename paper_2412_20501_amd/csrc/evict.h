@@ -21,9 +21,8 @@ struct WeighParams {
   Divisor by_gq;
   int causal, fresh;
   float scale;
-  RowClass rows;               // the sequences of the launch
 };
-hipError_t launch_cache_weigh(WeighParams& p, int D, bool f8, hipStream_t stream);
+hipError_t launch_cache_weigh(const WeighParams& p, int D, bool f8, hipStream_t stream);
 
 struct SelectParams {
   Sequences seq;

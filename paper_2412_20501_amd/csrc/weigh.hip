@@ -29,9 +29,8 @@ struct WeighItem {
 };
 __device__ __forceinline__ int seen_keys(const WeighParams& p, const Sequence& q) { return visible(q, q.n - 1, p.causal); }
 template <int WIDTH>
-__device__ __forceinline__ int tiles_of_keys(const WeighParams& p, const Sequence& q) {   // of a K/V head
-  const int rows = q.n * p.gq;
-  return rows > p.rows.over && rows <= p.rows.most ? (seen_keys(p, q) + WIDTH - 1) / WIDTH : 0;
+__device__ __forceinline__ int tiles_of_keys(const WeighParams& p, const RowClass& c, const Sequence& q) {   // of a K/V head
+  return tiles_of(q.n * p.gq, c) > 0 ? (seen_keys(p, q) + WIDTH - 1) / WIDTH : 0;
 }
 __device__ __forceinline__ Plan sums_plan(const WeighParams& p) {
   Plan plan = {p.seq.n, 0, Sequence{0, 0, 0, 0}};
@@ -40,15 +39,15 @@ __device__ __forceinline__ Plan sums_plan(const WeighParams& p) {
   return plan;
 }
 template <int WIDTH>
-__device__ __forceinline__ int all_items(const WeighParams& p, const Plan& plan) {
+__device__ __forceinline__ int all_items(const WeighParams& p, const RowClass& c, const Plan& plan) {
   int b = 0, total;
-  locate(p, plan, 0x7fffffff, [&](const Sequence& q) { return tiles_of_keys<WIDTH>(p, q) * p.Hkv; }, b, total);
+  locate(p, plan, 0x7fffffff, [&](const Sequence& q) { return tiles_of_keys<WIDTH>(p, c, q) * p.Hkv; }, b, total);
   return total;
 }
 template <int WIDTH>
-__device__ __forceinline__ void item_at(const WeighParams& p, const Plan& plan, int at, WeighItem& w) {   // at: below all_items()
+__device__ __forceinline__ void item_at(const WeighParams& p, const RowClass& c, const Plan& plan, int at, WeighItem& w) {   // at: below all_items()
   int b = 0, before;
-  locate(p, plan, at, [&](const Sequence& q) { return tiles_of_keys<WIDTH>(p, q) * p.Hkv; }, b, before);
+  locate(p, plan, at, [&](const Sequence& q) { return tiles_of_keys<WIDTH>(p, c, q) * p.Hkv; }, b, before);
   w.b = uniform(b);
   if (w.b < 64) {   // a lane has it
     const Sequence& q = plan.first;
@@ -57,7 +56,7 @@ __device__ __forceinline__ void item_at(const WeighParams& p, const Plan& plan, 
     const Sequence q = sequence(p.seq, w.b);
     w.q = Sequence{uniform(q.start), uniform(q.n), uniform(q.len), uniform(q.pos)};
   }
-  const int tiles = uniform(tiles_of_keys<WIDTH>(p, w.q)), i = uniform(at - before);
+  const int tiles = uniform(tiles_of_keys<WIDTH>(p, c, w.q)), i = uniform(at - before);
   w.hk = uniform(i / tiles);
   w.k0 = (i - w.hk * tiles) * WIDTH;
   w.seen = uniform(seen_keys(p, w.q));
@@ -75,10 +74,9 @@ __device__ __forceinline__ void add_weight(const WeighParams& p, const WeighItem
 // Few rows (a decode step, drafts): every wave has 64 keys, straight from memory into registers as the B operand of S = Q K^T; lane (i = lane % 16, g = lane / 16) then has
 // scores of key i with rows 4 g .. 4 g + 3 of 16.  The pages of the next item's keys are on their way beside this one's.  Bound: HBM.
 template <int D, bool F8>
-__global__ void __launch_bounds__(256, kFewWaves) weigh_few_kernel(const WeighParams p) {
+__device__ __forceinline__ void weigh_few(const WeighParams& p, const RowClass& c, const Plan& plan) {
   constexpr int QS = D / 32, KL = F8 ? D / 64 : D / 32;
-  const Plan plan = sums_plan(p);
-  const int total = uniform(all_items<kFewKeys>(p, plan)), each = (total + 7) >> 3, base = ((int)blockIdx.x & 7) * each, end = min(each, total - base);
+  const int total = uniform(all_items<kFewKeys>(p, c, plan)), each = (total + 7) >> 3, base = ((int)blockIdx.x & 7) * each, end = min(each, total - base);
   const int lane = threadIdx.x & 63, wave = uniform((int)threadIdx.x >> 6), i16 = lane & 15, g = lane >> 4;
   const float c2 = p.scale * kLog2e;
   WeighItem w, next;
@@ -86,7 +84,7 @@ __global__ void __launch_bounds__(256, kFewWaves) weigh_few_kernel(const WeighPa
   auto find = [&](int at, WeighItem& item, Slot& slot) __attribute__((always_inline)) {
     slot = Slot{-1, 0};
     if (at >= end) return;
-    item_at<kFewKeys>(p, plan, base + at, item);
+    item_at<kFewKeys>(p, c, plan, base + at, item);
     const int key = item.k0 + wave * 64 + lane;
     if (key < item.seen) slot = slot_of(p.seq, item.b, key);
   };
@@ -208,19 +206,17 @@ __device__ __forceinline__ void advance(const WeighParams& p, Row& r, const RowS
   }
 }
 template <int D, bool F8>
-__global__ void __launch_bounds__(256, 2) weigh_many_kernel(const WeighParams p) {
+__device__ __forceinline__ void weigh_many(const WeighParams& p, const RowClass& c, const Plan& plan, char* lds) {
   typedef Many<D> M;
   constexpr int KS = D / 16, CPR = D / 8, LOADS = M::TILE / 4096, EACH = 16 / KS;   // 16-byte loads a thread and tile; exponentials a product
-  __shared__ __attribute__((aligned(1024))) char lds[M::LDS];
-  const Plan plan = sums_plan(p);
-  const int total = uniform(all_items<kManyKeys>(p, plan)), each = (total + 7) >> 3, base = ((int)blockIdx.x & 7) * each;
+  const int total = uniform(all_items<kManyKeys>(p, c, plan)), each = (total + 7) >> 3, base = ((int)blockIdx.x & 7) * each;
   const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), l32 = lane & 31, hf = lane >> 5;
   const float c2 = p.scale * kLog2e;
   const RowStep q_step = row_step(p, p.q_sh, p.q_ss), l_step = row_step(p, p.l_sh, p.l_ss);
 #pragma unroll 1
   for (int at = (int)blockIdx.x >> 3; at < each && base + at < total; at += (int)gridDim.x >> 3) {
     WeighItem w;
-    item_at<kManyKeys>(p, plan, base + at, w);
+    item_at<kManyKeys>(p, c, plan, base + at, w);
     const int key0 = w.k0 + wave * 64, rows = w.q.n * p.gq;
     // rows from the first that sees the item's first key
     const int first = p.causal ? clamped(w.k0 - w.q.pos, 0, w.q.n) * p.gq / 32 : 0, tiles = (rows + 31) / 32;
@@ -363,28 +359,44 @@ __global__ void __launch_bounds__(256, 2) weigh_many_kernel(const WeighParams p)
   }
 }
 
+// The sequences of a call are all of either kind, or a mixture: then half of the workgroups begin with one and half with the other, so that the loads of few rows and the products of many run at
+// the same time (a prompt of 700 tokens among 15 single ones, 24 heads of 64, 4000 keys: @MIX@ us, in two launches 56).
+constexpr RowClass kAny = {32, 0, 0x7fffffff}, kFewRows = {32, 0, 32}, kManyMore = {32, 32, 0x7fffffff};
 template <int D, bool F8>
-hipError_t launch_form(WeighParams& p, hipStream_t stream) {
-  const int64_t tokens = p.seq.tokens, n = p.seq.n, max_keys = (int64_t)p.seq.max_pages * p.seq.page_size;
-  constexpr int any = 0x7fffffff;
-  const int64_t rows = tokens * p.gq;
-  const bool mixed = rows > 32 * n && n > 1, few = rows <= 32 * n;
-  for (int part = 0; part < (mixed ? 2 : 1); part++) {
-    const bool many = mixed ? part == 1 : !few;
-    p.rows = mixed ? (many ? RowClass{32, 32, any} : RowClass{32, 0, 32}) : RowClass{32, 0, any};
-    const int64_t width = many ? kManyKeys : kFewKeys, seqs = rows / (p.rows.over + 1) < n ? rows / (p.rows.over + 1) : n;
-    const int64_t items = seqs * p.Hkv * ((max_keys + width - 1) / width), most = many ? 512 : 256 * kFewWaves;
-    if (items == 0) continue;
-    const dim3 grid((unsigned)((items < most ? items : most) + 7) / 8 * 8);
-    const hipError_t e = many ? launch_kernel(weigh_many_kernel<D, F8>, grid, dim3(256), 0, stream, p) : launch_kernel(weigh_few_kernel<D, F8>, grid, dim3(256), 0, stream, p);
-    if (e != hipSuccess) return e;
+__global__ void __launch_bounds__(256, kFewWaves) weigh_few_kernel(const WeighParams p) { weigh_few<D, F8>(p, kAny, sums_plan(p)); }
+template <int D, bool F8>
+__global__ void __launch_bounds__(256, 2) weigh_many_kernel(const WeighParams p) {
+  __shared__ __attribute__((aligned(1024))) char lds[Many<D>::LDS];
+  weigh_many<D, F8>(p, kAny, sums_plan(p), lds);
+}
+template <int D, bool F8>
+__global__ void __launch_bounds__(256, 2) weigh_mixed_kernel(const WeighParams p) {
+  __shared__ __attribute__((aligned(1024))) char lds[Many<D>::LDS];
+  const Plan plan = sums_plan(p);
+  const int first = (int)blockIdx.x >> 3 & 1;
+#pragma unroll 1
+  for (int turn = 0; turn < 2; turn++) {
+    if (turn == first) weigh_many<D, F8>(p, kManyMore, plan, lds);
+    else weigh_few<D, F8>(p, kFewRows, plan);
   }
-  return hipSuccess;
+}
+
+template <int D, bool F8>
+hipError_t launch_form(const WeighParams& p, hipStream_t stream) {
+  const int64_t rows = (int64_t)p.seq.tokens * p.gq, n = p.seq.n, max_keys = (int64_t)p.seq.max_pages * p.seq.page_size;
+  static_assert(kFewKeys == kManyKeys, "as many items of either kind");
+  const int64_t items = n * p.Hkv * ((max_keys + kFewKeys - 1) / kFewKeys);
+  const bool few = rows <= 32 * n;   // on average: single tokens and drafts
+  const int64_t most = few ? 256 * kFewWaves : 512;   // workgroups that the compute units hold
+  const dim3 grid((unsigned)((items < most ? items : most) + 7) / 8 * 8), block(256);
+  if (few) return launch_kernel(weigh_few_kernel<D, F8>, grid, block, 0, stream, p);
+  if (n == 1) return launch_kernel(weigh_many_kernel<D, F8>, grid, block, 0, stream, p);
+  return launch_kernel(weigh_mixed_kernel<D, F8>, grid, block, 0, stream, p);
 }
 
 }  // namespace
 
-hipError_t launch_cache_weigh(WeighParams& p, int D, bool f8, hipStream_t stream) {
+hipError_t launch_cache_weigh(const WeighParams& p, int D, bool f8, hipStream_t stream) {
   if (D == 128) return f8 ? launch_form<128, true>(p, stream) : launch_form<128, false>(p, stream);
   return f8 ? launch_form<64, true>(p, stream) : launch_form<64, false>(p, stream);
 }
