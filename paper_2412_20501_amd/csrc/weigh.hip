@@ -19,7 +19,8 @@ typedef float f32x16 __attribute__((ext_vector_type(16)));
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr int kFewWaves = 4;     // a SIMD, of few rows
 constexpr int kFewKeys = 256;    // of an item of few rows: 64 a wave
-constexpr int kManyKeys = 256;   // of many rows
+constexpr int kTogetherBelow = 256;
+constexpr int kManyKeys = 256;   // of many rows: 64 a wave, or, where that leaves compute units without an item, 64 that the waves have together
 
 // Items: (sequence, K/V head, stretch of keys) of the launch's sequences, numbered so that those of a head lie together, and each XCD has a contiguous eighth of all.
 struct WeighItem {
@@ -177,13 +178,13 @@ struct Many {
   static constexpr int SUMS = 4 * 64 * 33 * 4;                 // where the waves add up their lanes' sums
   static constexpr int LDS = 2 * TILE > SUMS ? 2 * TILE : SUMS;
 };
-// Every 32nd row of an item, a (token, query head) pair: where it is, by additions.
+// Every 32nd or 128th row of an item, a (token, query head) pair: where it is, by additions.
 struct RowStep {
   int t, j;
   int64_t off, wrap;
 };
-__device__ __forceinline__ RowStep row_step(const WeighParams& p, int64_t sh, int64_t ss) {
-  const int t = uniform(divide(p.by_gq, 32)), j = 32 - t * p.gq;
+__device__ __forceinline__ RowStep row_step(const WeighParams& p, int rows, int64_t sh, int64_t ss) {
+  const int t = uniform(divide(p.by_gq, rows)), j = rows - t * p.gq;
   return RowStep{t, j, j * sh + t * ss, ss - p.gq * sh};
 }
 struct Row {
@@ -205,32 +206,38 @@ __device__ __forceinline__ void advance(const WeighParams& p, Row& r, const RowS
     r.off += by.wrap;
   }
 }
-template <int D, bool F8>
-__device__ __forceinline__ void weigh_many(const WeighParams& p, const RowClass& c, const Plan& plan, char* lds) {
+template <int D, bool F8, bool TOGETHER>   // TOGETHER: the waves of a workgroup have the same 64 keys, and every fourth tile of rows, which they read for themselves
+__device__ __forceinline__ void weigh_rows(const WeighParams& p, const RowClass& c, const Plan& plan, char* lds) {
   typedef Many<D> M;
   constexpr int KS = D / 16, CPR = D / 8, LOADS = M::TILE / 4096, EACH = 16 / KS;   // 16-byte loads a thread and tile; exponentials a product
-  const int total = uniform(all_items<kManyKeys>(p, c, plan)), each = (total + 7) >> 3, base = ((int)blockIdx.x & 7) * each;
+  constexpr int WIDTH = TOGETHER ? 64 : kManyKeys, STEP = TOGETHER ? 4 : 1;         // keys of an item; from a wave's tile to its next one
+  const int total = uniform(all_items<WIDTH>(p, c, plan)), each = (total + 7) >> 3, base = ((int)blockIdx.x & 7) * each;
   const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), l32 = lane & 31, hf = lane >> 5;
   const float c2 = p.scale * kLog2e;
-  const RowStep q_step = row_step(p, p.q_sh, p.q_ss), l_step = row_step(p, p.l_sh, p.l_ss);
+  const RowStep q_step = row_step(p, 32 * STEP, p.q_sh, p.q_ss), l_step = row_step(p, 32 * STEP, p.l_sh, p.l_ss);
 #pragma unroll 1
   for (int at = (int)blockIdx.x >> 3; at < each && base + at < total; at += (int)gridDim.x >> 3) {
     WeighItem w;
-    item_at<kManyKeys>(p, c, plan, base + at, w);
-    const int key0 = w.k0 + wave * 64, rows = w.q.n * p.gq;
+    item_at<WIDTH>(p, c, plan, base + at, w);
+    const int key0 = TOGETHER ? w.k0 : w.k0 + wave * 64, rows = w.q.n * p.gq;
     // rows from the first that sees the item's first key
-    const int first = p.causal ? clamped(w.k0 - w.q.pos, 0, w.q.n) * p.gq / 32 : 0, tiles = (rows + 31) / 32;
+    const int first = (p.causal ? clamped(w.k0 - w.q.pos, 0, w.q.n) * p.gq / 32 : 0) + (TOGETHER ? wave : 0), tiles = (rows + 31) / 32;
     const __bf16* const q_base = p.q + (int64_t)w.hk * p.gq * p.q_sh + (int64_t)w.q.start * p.q_ss;
     const float* const l_base = p.lse + (int64_t)w.hk * p.gq * p.l_sh + (int64_t)w.q.start * p.l_ss;
-    Row q_row[LOADS], l_row = row_at(p, first * 32 + l32, p.l_sh, p.l_ss);   // of the next tile to be fetched
+    Row q_row[TOGETHER ? 1 : LOADS], l_row = row_at(p, first * 32 + l32, p.l_sh, p.l_ss);   // of the next tile to be fetched
 #pragma unroll
-    for (int i = 0; i < LOADS; i++) q_row[i] = row_at(p, first * 32 + (i * 256 + tid) / CPR, p.q_sh, p.q_ss);
+    for (int i = 0; i < (TOGETHER ? 1 : LOADS); i++) q_row[i] = row_at(p, first * 32 + (TOGETHER ? l32 : (i * 256 + tid) / CPR), p.q_sh, p.q_ss);
     u32x4 coming[LOADS];
+    const __bf16* lane_row = q_base;   // together: the lane's row of the next tile
     float lse_coming;
     int t_coming;
     auto fetch = [&]() __attribute__((always_inline)) {   // (in the place of rows behind the last the first is read)
+      if constexpr (TOGETHER) {
+        lane_row = q_base + (q_row[0].t < w.q.n ? q_row[0].off : 0) + (F8 ? 16 : 8) * hf;
+        advance(p, q_row[0], q_step);
+      }
 #pragma unroll
-      for (int i = 0; i < LOADS; i++) {
+      for (int i = 0; i < LOADS && !TOGETHER; i++) {
         const int64_t off = q_row[i].t < w.q.n ? q_row[i].off : 0;
         coming[i] = *reinterpret_cast<const u32x4*>(q_base + off + tid % CPR * 8);
         advance(p, q_row[i], q_step);
@@ -255,6 +262,7 @@ __device__ __forceinline__ void weigh_many(const WeighParams& p, const RowClass&
     const unsigned operand0 = l32 * M::RB + ((l32 % CPR ^ (F8 ? 2 * hf : hf)) << 4);   // of the lane's chunk 0
     auto operand = [&](unsigned tile0, int ks) __attribute__((always_inline)) -> bf16x8 {
       const int c = F8 ? 4 * (ks >> 1) + (ks & 1) : 2 * ks;
+      if constexpr (TOGETHER) return *reinterpret_cast<const bf16x8*>(lane_row + 8 * c);
       return *reinterpret_cast<const bf16x8*>(lds + (tile0 ^ (c << 4)));
     };
 
@@ -286,10 +294,12 @@ __device__ __forceinline__ void weigh_many(const WeighParams& p, const RowClass&
 
     __syncthreads();   // the sums of the item before have been read
     fetch();
-    put(first);
+    if constexpr (!TOGETHER) put(first);
     Shown now = shown();
-    fetch();
-    __syncthreads();
+    if constexpr (!TOGETHER) {
+      fetch();
+      __syncthreads();
+    }
     f32x16 s[2];     // scores of the two blocks of 32 keys: one's exponentials beside the other's products
     bf16x8 qf[KS];   // operands of the rows whose products come next
 #pragma unroll
@@ -331,13 +341,20 @@ __device__ __forceinline__ void weigh_many(const WeighParams& p, const RowClass&
     };
     int t = first;
     auto turn = [&](auto masked_c) __attribute__((always_inline)) {
-      put(t + 1);   // (behind the last tile: rows that add nothing)
-      const Shown next = shown();
-      fetch();
-      __syncthreads();
-      step(t, masked_c);
-      now = next;
-      t++;
+      // (behind the last tile: rows that add nothing)
+      if constexpr (TOGETHER) {
+        fetch();
+        step(t, masked_c);
+        now = shown();
+      } else {
+        put(t + 1);
+        const Shown next = shown();
+        fetch();
+        __syncthreads();
+        step(t, masked_c);
+        now = next;
+      }
+      t += STEP;
     };
     while (t < tiles) {   // (a loop for either kind: where they meet the compiler moves all sums from some registers to others)
 #pragma unroll 1
@@ -355,8 +372,21 @@ __device__ __forceinline__ void weigh_many(const WeighParams& p, const RowClass&
     float sum = 0.f;
 #pragma unroll
     for (int i = 0; i < 32; i++) sum += sums[lane * 33 + i];
-    add_weight(p, w, key0 + lane, sum);
+    if constexpr (TOGETHER) {
+      __syncthreads();
+      float* const of_waves = reinterpret_cast<float*>(lds);
+      of_waves[tid] = sum;
+      __syncthreads();
+      if (wave == 0) add_weight(p, w, key0 + lane, (of_waves[lane] + of_waves[64 + lane]) + (of_waves[128 + lane] + of_waves[192 + lane]));
+    } else {
+      add_weight(p, w, key0 + lane, sum);
+    }
   }
+}
+template <int D, bool F8>
+__device__ __forceinline__ void weigh_many(const WeighParams& p, const RowClass& c, const Plan& plan, char* lds) {
+  if (uniform(all_items<kManyKeys>(p, c, plan)) < kTogetherBelow) weigh_rows<D, F8, true>(p, c, plan, lds);
+  else weigh_rows<D, F8, false>(p, c, plan, lds);
 }
 
 // The sequences of a call are all of either kind, or a mixture: then half of the workgroups begin with one and half with the other, so that the loads of few rows and the products of many run at
@@ -376,7 +406,7 @@ __global__ void __launch_bounds__(256, 2) weigh_mixed_kernel(const WeighParams p
   const int first = (int)blockIdx.x >> 3 & 1;
 #pragma unroll 1
   for (int turn = 0; turn < 2; turn++) {
-    if (turn == first) weigh_many<D, F8>(p, kManyMore, plan, lds);
+    if (turn == first) weigh_rows<D, F8, false>(p, kManyMore, plan, lds);
     else weigh_few<D, F8>(p, kFewRows, plan);
   }
 }
@@ -384,13 +414,12 @@ __global__ void __launch_bounds__(256, 2) weigh_mixed_kernel(const WeighParams p
 template <int D, bool F8>
 hipError_t launch_form(const WeighParams& p, hipStream_t stream) {
   const int64_t rows = (int64_t)p.seq.tokens * p.gq, n = p.seq.n, max_keys = (int64_t)p.seq.max_pages * p.seq.page_size;
-  static_assert(kFewKeys == kManyKeys, "as many items of either kind");
-  const int64_t items = n * p.Hkv * ((max_keys + kFewKeys - 1) / kFewKeys);
   const bool few = rows <= 32 * n;   // on average: single tokens and drafts
+  const int64_t width = few ? kFewKeys : 64, items = n * p.Hkv * ((max_keys + width - 1) / width);
   const int64_t most = few ? 256 * kFewWaves : 512;   // workgroups that the compute units hold
   const dim3 grid((unsigned)((items < most ? items : most) + 7) / 8 * 8), block(256);
   if (few) return launch_kernel(weigh_few_kernel<D, F8>, grid, block, 0, stream, p);
-  if (n == 1) return launch_kernel(weigh_many_kernel<D, F8>, grid, block, 0, stream, p);
+  if (n < 8) return launch_kernel(weigh_many_kernel<D, F8>, grid, block, 0, stream, p);
   return launch_kernel(weigh_mixed_kernel<D, F8>, grid, block, 0, stream, p);
 }
 

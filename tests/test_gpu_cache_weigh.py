@@ -68,6 +68,18 @@ def test_lengths(lib, shape, D, f8):
 
 
 @pytest.mark.parametrize("f8", [False, True])
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("gq", [1, 5, 8])
+@pytest.mark.parametrize("mixed", [False, True])
+def test_many_items(lib, mixed, gq, D, f8):
+    """More stretches of keys than compute units, of sequences with many rows alone and among single tokens."""
+    kv = [600 + 17 * (i % 13) for i in range(40)]
+    q = [70 + i % 5 if not mixed or i % 3 == 0 else i % 2 for i in range(40)]
+    c = Cache(kv, q, 4 if not mixed else 8, D, 32, f8, "token" if gq == 5 else "head", seed=gq)
+    _run(lib, c, c.Hkv * gq)
+
+
+@pytest.mark.parametrize("f8", [False, True])
 @pytest.mark.parametrize("causal", [False, True])
 @pytest.mark.parametrize("fresh", [False, True])
 @pytest.mark.parametrize("n", [2, 77])
