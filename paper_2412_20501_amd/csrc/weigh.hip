@@ -19,7 +19,7 @@ typedef float f32x16 __attribute__((ext_vector_type(16)));
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr int kFewWaves = 4;     // a SIMD, of few rows
 constexpr int kFewKeys = 256;    // of an item of few rows: 64 a wave
-constexpr int kTogetherBelow = 256;
+constexpr int kTogetherBelow = 192;
 constexpr int kManyKeys = 256;   // of many rows: 64 a wave, or, where that leaves compute units without an item, 64 that the waves have together
 
 // Items: (sequence, K/V head, stretch of keys) of the launch's sequences, numbered so that those of a head lie together, and each XCD has a contiguous eighth of all.
