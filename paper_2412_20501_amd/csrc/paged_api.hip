@@ -2,6 +2,8 @@
 #include <math.h>
 #include <string.h>
 
+#include <type_traits>
+
 #include "paged_checks.h"
 
 using tr::check_apart;
@@ -56,8 +58,9 @@ size_t workspace_bytes_of(const tr_tensor* q, const tr_tensor* k_pages, int64_t 
   return (size_t)floats * 4;
 }
 
-// tr_paged_attn, and with a tree tr_paged_attn_tree.
-tr_status attend(const tr_tensor* q_, const tr_tensor* k_pages_, const tr_tensor* v_pages_, const tr_tensor* k_scales_,
+// tr_paged_attn (P = PagedParams, tree = null) and tr_paged_attn_tree (TreeParams).
+template <typename P>
+__attribute__((always_inline)) inline tr_status attend(const tr_tensor* q_, const tr_tensor* k_pages_, const tr_tensor* v_pages_, const tr_tensor* k_scales_,
                  const tr_tensor* v_scales_, const tr_sequences* seqs, const tr_tree* tree, int causal, float scale, const tr_tensor* out_,
                  const tr_tensor* lse_, void* workspace, size_t workspace_bytes, void* hip_stream) {
   tr::clear_error();
@@ -81,12 +84,13 @@ tr_status attend(const tr_tensor* q_, const tr_tensor* k_pages_, const tr_tensor
   if (q->H % k_pages->H) return fail(TR_ERR_SHAPE, "query heads %lld not a multiple of K/V heads %lld", (long long)q->H, (long long)k_pages->H);
   if (!(scale > 0.f) || !isfinite(scale)) return fail(TR_ERR_UNSUPPORTED, "scale must be finite and > 0");
   if (q->S * q->H >= ((int64_t)1 << 31)) return fail(TR_ERR_SHAPE, "too many rows for one call (S * Hq must stay below 2^31)");
-  tr::TreeParams p;
+  P p;
   memset(&p, 0, sizeof(p));
   SeqViews views;
   if ((st = take_sequences(seqs, k_pages, q->S, p.seq, views)) != TR_OK) return st;
   if (seqs->n_seqs > kMaxAttended) return fail(TR_ERR_SHAPE, "%lld sequences, one call attends for 2^16 at most", (long long)seqs->n_seqs);
-  if (tree) {
+  constexpr bool TREE = std::is_same<P, tr::TreeParams>::value;
+  if constexpr (TREE) {
     if ((st = take_tree(*tree, q->S, p, views)) != TR_OK) return st;
   }
   const tr_tensor* const written[] = {out, lse};
@@ -96,10 +100,10 @@ tr_status attend(const tr_tensor* q_, const tr_tensor* k_pages_, const tr_tensor
   if (q->H == 0 || q->S == 0 || p.seq.n == 0) return TR_OK;
 
   const int gq = (int)(q->H / k_pages->H), D = (int)q->D;
-  const tr::PagedLaunch l = tr::paged_launch(q->S, p.seq.n, (int64_t)p.seq.max_pages * p.seq.page_size, (int)k_pages->H, gq, D, k_scales != nullptr, tree != nullptr);
+  const tr::PagedLaunch l = tr::paged_launch(q->S, p.seq.n, (int64_t)p.seq.max_pages * p.seq.page_size, (int)k_pages->H, gq, D, k_scales != nullptr, TREE);
   for (int i = 0; i < l.n; i++)
     if (l.part[i].tiles + l.part[i].share.most() >= ((int64_t)1 << 23) - 8) return fail(TR_ERR_SHAPE, "too many workgroups for one launch");   // (of 512 threads, fewer than 2^32 in all)
-  const size_t need = workspace_bytes_of(q, k_pages, seqs->n_seqs, seqs->max_pages, tree != nullptr);
+  const size_t need = workspace_bytes_of(q, k_pages, seqs->n_seqs, seqs->max_pages, TREE);
   if (workspace && need > 0) {
     if ((uintptr_t)workspace % 256) return fail(TR_ERR_WORKSPACE, "workspace must be 256-byte aligned");
     if (workspace_bytes < need) return fail(TR_ERR_WORKSPACE, "workspace too small: %zu < %zu bytes", workspace_bytes, need);
@@ -127,9 +131,7 @@ tr_status attend(const tr_tensor* q_, const tr_tensor* k_pages_, const tr_tensor
   p.by_gq = tr::make_divisor((unsigned)gq);
   p.causal = causal != 0; p.out_f32 = out->dtype == TR_F32;
   p.scale = scale;
-  float* const scratch = need > 0 ? (float*)workspace : nullptr;
-  const hipError_t e = tree ? tr::launch_paged_attn(p, l, D, k_scales != nullptr, scratch, (hipStream_t)hip_stream)
-                            : tr::launch_paged_attn(static_cast<tr::PagedParams&>(p), l, D, k_scales != nullptr, scratch, (hipStream_t)hip_stream);
+  const hipError_t e = tr::launch_paged_attn(p, l, D, k_scales != nullptr, need > 0 ? (float*)workspace : nullptr, (hipStream_t)hip_stream);
   if (e != hipSuccess) return fail(TR_ERR_HIP, "paged attention launch failed: %s", hipGetErrorString(e));
   return TR_OK;
 }
@@ -222,7 +224,7 @@ size_t tr_paged_attn_tree_workspace_bytes(const tr_tensor* q, const tr_tensor* k
 tr_status tr_paged_attn(const tr_tensor* q, const tr_tensor* k_pages, const tr_tensor* v_pages, const tr_tensor* k_scales, const tr_tensor* v_scales,
                         const tr_sequences* seqs, int causal, float scale, const tr_tensor* out, const tr_tensor* lse, void* workspace,
                         size_t workspace_bytes, void* hip_stream) {
-  return attend(q, k_pages, v_pages, k_scales, v_scales, seqs, nullptr, causal, scale, out, lse, workspace, workspace_bytes, hip_stream);
+  return attend<tr::PagedParams>(q, k_pages, v_pages, k_scales, v_scales, seqs, nullptr, causal, scale, out, lse, workspace, workspace_bytes, hip_stream);
 }
 
 tr_status tr_paged_attn_tree(const tr_tensor* q, const tr_tensor* k_pages, const tr_tensor* v_pages, const tr_tensor* k_scales, const tr_tensor* v_scales,
@@ -232,7 +234,7 @@ tr_status tr_paged_attn_tree(const tr_tensor* q, const tr_tensor* k_pages, const
     tr::clear_error();
     return fail(TR_ERR_NULL, "the tree is NULL");
   }
-  return attend(q, k_pages, v_pages, k_scales, v_scales, seqs, tree, 1, scale, out, lse, workspace, workspace_bytes, hip_stream);
+  return attend<tr::TreeParams>(q, k_pages, v_pages, k_scales, v_scales, seqs, tree, 1, scale, out, lse, workspace, workspace_bytes, hip_stream);
 }
 
 }  // extern "C"

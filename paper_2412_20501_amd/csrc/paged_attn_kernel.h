@@ -501,27 +501,42 @@ __global__ void __launch_bounds__(256) paged_fold_kernel(const P p) {
   const Plan plan = make_plan(p);
   const int part = plan.part, size = p.rows.tile, pieces = max(1, size / ROWS);
   auto cut_tiles = [&](const Sequence& q) { return parts_of(q.len, part) > 1 ? tiles_of(q.n * p.gq, p.rows) * p.Hkv : 0; };
-  auto head_pieces = [&](const Sequence& q) {   // with a row, of a K/V head of a sequence that is cut
+  auto live_pieces = [&](const Sequence& q) {   // of a K/V head of a sequence, those with a row
     const int rows = q.n * p.gq, tiles = tiles_of(rows, p.rows);
     return tiles > 0 ? (tiles - 1) * pieces + (rows - (tiles - 1) * size + ROWS - 1) / ROWS : 0;
   };
   for (int at = (int)blockIdx.x;; at += (int)gridDim.x) {
   int b, before;
-  if (!locate(p, plan, at, [&](const Sequence& q) { return parts_of(q.len, part) > 1 ? head_pieces(q) * p.Hkv : 0; }, b, before)) return;
+  // (a tree's last tile is mostly its only one: 16 of 100 rows, 8 heads, 17.8 -> 13.5 us)
+  if constexpr (is_tree<P>) {
+    if (!locate(p, plan, at, [&](const Sequence& q) { return parts_of(q.len, part) > 1 ? live_pieces(q) * p.Hkv : 0; }, b, before)) return;
+  } else {
+    if (!locate(p, plan, at / pieces, cut_tiles, b, before)) return;
+  }
   Item w;
   w.q = uniform_sequence(p, uniform(b));
   w.rows = uniform(w.q.n * p.gq);
   const int base = sum_before(p, plan, uniform(b), [&](const Sequence& q) { return cut_tiles(q) * parts_of(q.len, part); });
-  const int parts = uniform(parts_of(w.q.len, part)), tiles = uniform(tiles_of(w.rows, p.rows)), of_head = uniform(head_pieces(w.q)), from_first = uniform(at - before);
-  w.hk = uniform(from_first / of_head);
-  const int of_this = from_first - w.hk * of_head, tile = uniform(min(of_this / pieces, tiles - 1)), i = w.hk * tiles + tile;
-  const int row0 = tile * size, rows = min(size, w.rows - row0);
+  const int parts = uniform(parts_of(w.q.len, part)), tiles = uniform(tiles_of(w.rows, p.rows));
+  int i, piece;   // tile of the sequence, piece of the tile
+  if constexpr (is_tree<P>) {
+    const int each = uniform(live_pieces(w.q)), n = uniform(at - before);
+    w.hk = uniform(n / each);
+    const int tile = uniform(min((n - w.hk * each) / pieces, tiles - 1));
+    piece = n - w.hk * each - tile * pieces;
+    i = w.hk * tiles + tile;
+  } else {
+    i = uniform(at / pieces - before);
+    w.hk = uniform(i / tiles);
+    piece = at % pieces;
+  }
+  const int row0 = (i - w.hk * tiles) * size, rows = min(size, w.rows - row0);
   const int n_live = uniform(parts_of(last_limit(p, w.q, row0 + rows - 1), part));
   if (n_live == 1) continue;   // one part: written already
   if (base < 0 || base + (i + 1) * parts > p.slots) continue;   // (only where sequences overlap)
   w.n_parts = 1;   // what follows is stored for good
   const int c = (int)threadIdx.x % LANES;
-  const int r = (of_this - tile * pieces) * ROWS + (int)threadIdx.x / LANES;
+  const int r = piece * ROWS + (int)threadIdx.x / LANES;
   if (r < rows) {
     const int64_t slot_row = ((int64_t)base + (int64_t)i * parts) * size + r;
     const float* const ls = p.part_lse + slot_row;
