@@ -381,7 +381,8 @@ size_t tr_paged_attn_tree_workspace_bytes(const tr_tensor* q, const tr_tensor* k
  * fresh != 0: the keys of the new tokens themselves (c = q_pos[b] + i, those that tr_cache_write has just written) start from 0 instead of what their slots hold.
  * A token whose lse is not finite (it saw nothing, or a NaN) adds nothing; what its row of q or a masked key holds reaches no weight.  Keys that no token sees keep their weight, slots
  * that hold no key of a sequence with new tokens are not touched.  Scores and sums are in fp32.  A page that several sequences of the call share gets the sum of
- * one of them (or a mixture): weigh such sequences in calls of their own.  The result is bitwise reproducible.  At most 2^16 sequences.  Nothing is allocated; may be captured.
+ * one of them (or a mixture): weigh such sequences in calls of their own.  The result is otherwise bitwise reproducible.  At most 2^16 sequences, found in time that grows with their square, as
+ * in tr_paged_attn; S * Hq below 2^30.  Nothing is allocated; may be captured.
  */
 tr_status tr_cache_weigh(const tr_tensor* q, const tr_tensor* lse, const tr_tensor* k_pages, const tr_tensor* k_scales, const tr_sequences* seqs,
                          int causal, float scale, int fresh, const tr_tensor* weights, void* hip_stream);
@@ -409,8 +410,8 @@ tr_status tr_cache_select(const tr_tensor* weights, const tr_sequences* seqs, in
  * Moves kept keys together: key kept->keys[b][h][i] of sequence b becomes key start[b] + i, for i < count[b] (taken as 0 .. max_keys), with K, V, their scales and, if given, their
  * weights, in place.  start: [n_seqs] int32 or NULL for zeros.  An eviction moves what tr_cache_select chose; an accepted path of a tree is moved behind the
  * text with start = number of the first drafted token's key and one list for all heads.  The sequence then has start[b] + count[b] keys: kv_len is the caller's to change.
- *   A list must rise, and no key may move up: keys[b][h][i] >= start[b] + i.  An entry that moves up, a key or a place that is not 0 <= .. < kv_len[b], or that is on no
- *   page, is skipped: its place is left as it was.  Of a list that does not rise, places hold what any of the entries in question had, nothing else is touched.
+ *   A list must rise, and no key may get a larger number: keys[b][h][i] >= start[b] + i.  An entry that would, a key or a place that is not 0 <= .. < kv_len[b], or that is on no
+ *   page, is skipped: its place is left as it was.  Of a list that does not rise, the places of its entries may hold any of the sequence's rows; nothing else is touched.
  *   No page may belong to two sequences of the call that move keys.
  * weights as in tr_cache_weigh, or NULL.  q_start and q_pos are not used.  Nothing is allocated; may be captured.
  */
@@ -423,7 +424,7 @@ tr_status tr_cache_keep(const tr_tensor* k_pages, const tr_tensor* v_pages, cons
  * from this thread carries them in its dispatch: start_event then holds the time the kernel
  * began executing and stop_event the time it finished, so hipEventElapsedTime(start, stop)
  * is the kernel's own duration without queueing gaps.  Only that one launch is timed
- * (tr_ring_attn, tr_paged_attn: its first kernel; a block step whose keys are cut: its attention, not the fold); the events stay owned by the caller.  Always TR_OK.
+ * (tr_ring_attn, tr_paged_attn, tr_paged_attn_tree: its first kernel; a block step whose keys are cut: its attention, not the fold); the events stay owned by the caller.  Always TR_OK.
  */
 tr_status tr_time_next_kernel(void* start_event, void* stop_event);
 

@@ -19,7 +19,7 @@ typedef float f32x16 __attribute__((ext_vector_type(16)));
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr int kFewWaves = 4;     // a SIMD, of few rows
 constexpr int kFewKeys = 256;    // of an item of few rows: 64 a wave
-constexpr int kTogetherBelow = 192;
+constexpr int kTogetherBelow = 192;   // items of many rows
 constexpr int kManyKeys = 256;   // of many rows: 64 a wave, or, where that leaves compute units without an item, 64 that the waves have together
 
 // Items: (sequence, K/V head, stretch of keys) of the launch's sequences, numbered so that those of a head lie together, and each XCD has a contiguous eighth of all.
@@ -73,7 +73,9 @@ __device__ __forceinline__ void add_weight(const WeighParams& p, const WeighItem
 }
 
 // Few rows (a decode step, drafts): every wave has 64 keys, straight from memory into registers as the B operand of S = Q K^T; lane (i = lane % 16, g = lane / 16) then has
-// scores of key i with rows 4 g .. 4 g + 3 of 16.  The pages of the next item's keys are on their way beside this one's.  Bound: HBM.
+// scores of key i with rows 4 g .. 4 g + 3 of 16, so that a key's sum is four additions and two exchanges between lanes.  More rows than 16 are gone through with the keys held.  The pages of the next item's
+// keys are on their way beside this one's keys (found one after the other, table, then keys: 173 us for the 139 below).  Bound: HBM: a token of 64 sequences of 0.8K to 16K keys on 8 heads of 128 in 8 bits
+// 135 us, 4.5 TB/s of K and weights; of 16 of 8K in bf16 44.5 us, 6.2 TB/s.
 template <int D, bool F8>
 __device__ __forceinline__ void weigh_few(const WeighParams& p, const RowClass& c, const Plan& plan) {
   constexpr int QS = D / 32, KL = F8 ? D / 64 : D / 32;
@@ -170,8 +172,14 @@ __device__ __forceinline__ void weigh_few(const WeighParams& p, const RowClass& 
   }
 }
 
-// Many rows (a prompt's chunk): every wave has 64 keys in registers, as the A operand of S^T = K Q^T, and goes through the rows 32 at a time, which the workgroup brings into LDS.  The
-// products of a tile of rows run beside the exponentials of the one in front, and the operands of the one behind are fetched in the places of those that have been used.
+// Many rows (a prompt's chunk): every wave has 64 keys in registers, as the A operand of S^T = K Q^T with 32x32x16 products, and goes through the rows 32 at a time, which the workgroup brings into
+// LDS.  A lane then has one row's scores with 32 of the keys, so one reference a tile, and sums of its own for each key, which are added up over the lanes once at the end.  The keys' two blocks of 32 take
+// turns: one's exponentials run beside the other's products.
+// Bound: the vector unit: a score is 2 D flops on the matrix cores, 4 cycles of 64 scores at D 128, and an exponential of 16, a fused multiply-add and an addition of 4 each in quarters of them: 24 cycles for
+// 16 of products, with about a quarter more for rows and masks.  2048 tokens of 32 heads of 128 on 32K keys 547 us, 0.98 PFLOP/s (exponentials behind all products of a tile 655; four waves of 32 keys
+// a SIMD, which overlap by themselves, 631).
+// Where few keys meet many rows (a prompt's first chunk) 256 keys a workgroup leave compute units without any: the waves then have the same 64 keys and every fourth tile of rows, whose operands they
+// read from memory themselves (2048 tokens on themselves 171 -> 67 us, 500 50 -> 21; but 2048 on 8192 keys, an item for every unit, 189 -> 264).
 template <int D>
 struct Many {
   static constexpr int RB = 2 * D, TILE = 32 * RB;             // bytes of a row, of a tile of rows
@@ -390,7 +398,7 @@ __device__ __forceinline__ void weigh_many(const WeighParams& p, const RowClass&
 }
 
 // The sequences of a call are all of either kind, or a mixture: then half of the workgroups begin with one and half with the other, so that the loads of few rows and the products of many run at
-// the same time (a prompt of 700 tokens among 15 single ones, 24 heads of 64, 4000 keys: @MIX@ us, in two launches 56).
+// the same time (a prompt of 700 tokens among 15 single ones, 24 heads of 64, 4000 keys: 51 us, in two launches 56).  Fewer than 8 sequences are not worth it: all are taken for ones of many rows.
 constexpr RowClass kAny = {32, 0, 0x7fffffff}, kFewRows = {32, 0, 32}, kManyMore = {32, 32, 0x7fffffff};
 template <int D, bool F8>
 __global__ void __launch_bounds__(256, kFewWaves) weigh_few_kernel(const WeighParams p) { weigh_few<D, F8>(p, kAny, sums_plan(p)); }
