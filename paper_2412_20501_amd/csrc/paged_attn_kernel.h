@@ -495,19 +495,23 @@ __global__ void __launch_bounds__(256, paged_few_waves(D, F8, RT)) paged_few_ker
 // ---- Row tiles whose keys were cut (6 us for 32 tiles of 16 rows in 16 parts, 13 for 64 of 256 rows in four, 34 MB): out = sum of exp(lse_i - lse) out_i over their live parts, in their order.
 // A workgroup has pieces of 1024 / D rows of a tile, D / 4 lanes a row.  What bounds it is latency: the lanes of a row
 // fetch the lse of one part each, and pieces of eight parts are on their way at a time.
+// Of trees, whose tiles may have few rows, pieces that have none are not counted, and a workgroup has two turns: 16 trees of 100 rows on 8 heads 17.8 -> about 11 us.
+template <typename P>
+constexpr int fold_turns = is_tree<P> ? 2 : 1;
 template <int D, bool OUT_F32, typename P>
 __global__ void __launch_bounds__(256) paged_fold_kernel(const P p) {
   constexpr int LANES = D / 4, ROWS = 256 / LANES, AHEAD = 8;
+  constexpr int TURNS = fold_turns<P>, PIECE = ROWS * TURNS;   // rows of a piece
   const Plan plan = make_plan(p);
-  const int part = plan.part, size = p.rows.tile, pieces = max(1, size / ROWS);
+  const int part = plan.part, size = p.rows.tile, pieces = max(1, size / PIECE);
   auto cut_tiles = [&](const Sequence& q) { return parts_of(q.len, part) > 1 ? tiles_of(q.n * p.gq, p.rows) * p.Hkv : 0; };
   auto live_pieces = [&](const Sequence& q) {   // of a K/V head of a sequence, those with a row
     const int rows = q.n * p.gq, tiles = tiles_of(rows, p.rows);
-    return tiles > 0 ? (tiles - 1) * pieces + (rows - (tiles - 1) * size + ROWS - 1) / ROWS : 0;
+    return tiles > 0 ? (tiles - 1) * pieces + (rows - (tiles - 1) * size + PIECE - 1) / PIECE : 0;
   };
   for (int at = (int)blockIdx.x;; at += (int)gridDim.x) {
   int b, before;
-  // (a tree's last tile is mostly its only one: 16 of 100 rows, 8 heads, 17.8 -> 13.5 us)
+  // (a tree's last tile is mostly its only one)
   if constexpr (is_tree<P>) {
     if (!locate(p, plan, at, [&](const Sequence& q) { return parts_of(q.len, part) > 1 ? live_pieces(q) * p.Hkv : 0; }, b, before)) return;
   } else {
@@ -536,8 +540,9 @@ __global__ void __launch_bounds__(256) paged_fold_kernel(const P p) {
   if (base < 0 || base + (i + 1) * parts > p.slots) continue;   // (only where sequences overlap)
   w.n_parts = 1;   // what follows is stored for good
   const int c = (int)threadIdx.x % LANES;
-  const int r = piece * ROWS + (int)threadIdx.x / LANES;
-  if (r < rows) {
+  for (int turn = 0; turn < TURNS; turn++) {
+    const int r = piece * PIECE + turn * ROWS + (int)threadIdx.x / LANES;
+    if (r >= rows) break;
     const int64_t slot_row = ((int64_t)base + (int64_t)i * parts) * size + r;
     const float* const ls = p.part_lse + slot_row;
     const float* const out = p.part_out + slot_row * D + 4 * c;

@@ -28,7 +28,7 @@ hipError_t launch_out(P& p, const PagedLaunch& l, float* workspace, hipStream_t 
     if (e != hipSuccess) return e;
     if (p.share.most() == 0) continue;
     const unsigned cut = (unsigned)std::min<int64_t>(c.tiles, p.share.most());   // tiles that are cut, at most
-    e = launch_kernel(paged_fold_kernel<D, OUT_F32, P>, dim3(std::min(cut * (unsigned)std::max(1, c.rows.tile * D / 1024), is_tree<P> ? 2048u : 1024u)), dim3(256), 0, stream, p);
+    e = launch_kernel(paged_fold_kernel<D, OUT_F32, P>, dim3(std::min(cut * (unsigned)std::max(1, c.rows.tile * D / 1024 / fold_turns<P>), 1024u)), dim3(256), 0, stream, p);
     if (e != hipSuccess) return e;
   }
   return hipSuccess;
