@@ -220,7 +220,7 @@ __global__ void __launch_bounds__(THREADS, 8) select_kernel(const SelectParams p
 //
 // In place: a place may be the source of an entry in front of it, so that rows are read before any is written there.  A list rises and moves nothing up, so a workgroup that goes through a list in its order, reading
 // some rows, waiting for all its reads, and writing them, never writes what it has yet to read.  Workgroups share out sequences, heads, K and V, and, where those are few, pieces of the rows.  Bound: HBM: 64
-// sequences of 4.6K keys on 8 heads of 128 in 8 bits back to 4096 247 us, 4.5 TB/s (with keys and pages looked up in front of each load 338).
+// sequences of 4.6K keys on 8 heads of 128 in 8 bits back to 4096 238 us, 4.65 TB/s (with keys and pages looked up in front of each load 338); one long list: the instructions that find its entries.
 constexpr int kKeepThreads = 512, kKeepAhead = 8;   // entries of a thread of those that move scales and weights, at a time
 
 struct KeepList {
@@ -248,36 +248,58 @@ __device__ __forceinline__ int64_t from_other(int64_t x, int lane) {
   return (int64_t)(((uint64_t)(unsigned)__shfl((int)(x >> 32), lane) << 32) | (unsigned)__shfl((int)x, lane));
 }
 
-// Every wave has 64 entries at a time: lane i finds the places of the i-th, and a row's piece is 16 bytes of LANES lanes.  While rows are on their way, so are the pages of
+// Every wave has SETS times 64 entries at a time: lane i finds the places of the i-th of each, and a row's piece is 16 bytes of LANES lanes.  While rows are on their way, so are the pages of
 // the next entries and the keys of those behind them.
-template <int LANES>
+template <int LANES, int SETS>
 __device__ __forceinline__ void move_rows(const KeepParams& p, const KeepList& l, int b, char* pages, int64_t at_head) {
-  constexpr int ROWS = 64 / LANES;   // at once
-  const int lane = threadIdx.x & 63, wave = uniform((int)threadIdx.x >> 6), c = lane % LANES;
+  constexpr int ROWS = 64 / LANES, ALL = SETS * kKeepThreads;   // rows at once; entries of the workgroup
+  const int lane = threadIdx.x & 63, first = uniform((int)threadIdx.x >> 6) * 64 * SETS, c = lane % LANES;
   char* const base = pages + at_head + c * 16;
-  int key = key_of(l, wave * 64 + lane), key_next = key_of(l, kKeepThreads + wave * 64 + lane);
-  Slot s = {0, 0}, d = {0, 0};
-  bool moves = entry(p, l, b, wave * 64 + lane, key, s, d);
-#pragma unroll 1
-  for (int i0 = wave * 64; i0 < l.n + wave * 64; i0 += kKeepThreads) {   // (as often in every wave)
-    const int64_t from = moves ? (int64_t)s.page * p.page_b + (int64_t)s.slot * p.slot_b : -1, to = moves ? (int64_t)d.page * p.page_b + (int64_t)d.slot * p.slot_b : -1;
-    key = key_next;
-    key_next = key_of(l, i0 + 2 * kKeepThreads + lane);
-    moves = entry(p, l, b, i0 + kKeepThreads + lane, key, s, d);
-    u32x4 x[LANES];
-#pragma unroll
-    for (int j = 0; j < LANES; j++) {
-      const int64_t at = from_other(from, j * ROWS + lane / LANES);
-      if (at >= 0) x[j] = *reinterpret_cast<const u32x4*>(base + at);
+  int key_next[SETS];
+  int64_t from[SETS], to[SETS];   // of the next entries, -1: none
+  auto find = [&](int k, int i, int key) __attribute__((always_inline)) {
+    Slot s, d;
+    from[k] = to[k] = -1;
+    if (entry(p, l, b, i, key, s, d)) {
+      from[k] = (int64_t)s.page * p.page_b + (int64_t)s.slot * p.slot_b;
+      to[k] = (int64_t)d.page * p.page_b + (int64_t)d.slot * p.slot_b;
     }
+  };
+#pragma unroll
+  for (int k = 0; k < SETS; k++) {
+    const int i = first + k * 64 + lane;
+    key_next[k] = key_of(l, i + ALL);
+    find(k, i, key_of(l, i));
+  }
+#pragma unroll 1
+  for (int i0 = 0; i0 < l.n; i0 += ALL) {
+    int64_t src[SETS], dst[SETS];
+#pragma unroll
+    for (int k = 0; k < SETS; k++) {
+      const int i = i0 + ALL + first + k * 64 + lane, key = key_next[k];
+      src[k] = from[k];
+      dst[k] = to[k];
+      key_next[k] = key_of(l, i + ALL);
+      find(k, i, key);
+    }
+    u32x4 x[SETS][LANES];
+#pragma unroll
+    for (int k = 0; k < SETS; k++)
+#pragma unroll
+      for (int j = 0; j < LANES; j++) {
+        const int64_t at = from_other(src[k], j * ROWS + lane / LANES);
+        if (at >= 0) x[k][j] = *reinterpret_cast<const u32x4*>(base + at);
+      }
     __builtin_amdgcn_s_waitcnt(0);   // the rows are here, not only asked for
     asm volatile("" ::: "memory");
     __syncthreads();
 #pragma unroll
-    for (int j = 0; j < LANES; j++) {
-      const int64_t at = from_other(to, j * ROWS + lane / LANES);
-      if (at >= 0) *reinterpret_cast<u32x4*>(base + at) = x[j];
-    }
+    for (int k = 0; k < SETS; k++)
+#pragma unroll
+      for (int j = 0; j < LANES; j++) {
+        const int64_t at = from_other(dst[k], j * ROWS + lane / LANES);
+        if (at >= 0) *reinterpret_cast<u32x4*>(base + at) = x[k][j];
+      }
   }
 }
 __device__ __forceinline__ void move_scales(const KeepParams& p, const KeepList& l, int b, int h) {   // and weights
@@ -315,13 +337,13 @@ __device__ __forceinline__ void move_scales(const KeepParams& p, const KeepList&
 }
 
 // blockIdx.x: piece of the rows of K, of V, and behind them scales and weights; y: sequence and head.
-template <int LANES>
+template <int LANES, int SETS>
 __global__ void __launch_bounds__(kKeepThreads) keep_kernel(const KeepParams p, const int pieces) {
   for (int64_t y = blockIdx.y; y < (int64_t)p.seq.n * p.heads; y += gridDim.y) {
     const int b = (int)(y / p.heads), h = (int)(y - (int64_t)b * p.heads), x = (int)blockIdx.x;
     const KeepList l = list_of(p, b, h);
     if (x >= 2 * pieces) move_scales(p, l, b, h);
-    else move_rows<LANES>(p, l, b, x >= pieces ? p.v_pages : p.k_pages, (int64_t)h * p.head_b + (x >= pieces ? x - pieces : x) * (LANES * 16));
+    else move_rows<LANES, SETS>(p, l, b, x >= pieces ? p.v_pages : p.k_pages, (int64_t)h * p.head_b + (x >= pieces ? x - pieces : x) * (LANES * 16));
   }
 }
 
@@ -345,14 +367,23 @@ hipError_t launch_cache_select(const SelectParams& p, hipStream_t stream) {
   return rows >= 256 ? launch_select<512>(p, room, grid, stream) : launch_select<1024>(p, room, grid, stream);
 }
 
-hipError_t launch_cache_keep(const KeepParams& p, hipStream_t stream) {
+namespace {
+template <int LANES, int SETS>
+hipError_t launch_keep(const KeepParams& p, int pieces, hipStream_t stream) {
   const int64_t lists = (int64_t)p.seq.n * p.heads;
-  const unsigned y = (unsigned)(lists < 65535 ? lists : 65535), side = p.k_scales || p.weights ? 1 : 0;
-  const int pieces = lists * 2 >= 256 || p.row_bytes < 128 ? 1 : p.row_bytes / 64, lanes = p.row_bytes / pieces / 16;
-  const dim3 grid(2 * pieces + side, y), block(kKeepThreads);
-  if (lanes == 16) return launch_kernel(keep_kernel<16>, grid, block, 0, stream, p, pieces);
-  if (lanes == 8) return launch_kernel(keep_kernel<8>, grid, block, 0, stream, p, pieces);
-  return launch_kernel(keep_kernel<4>, grid, block, 0, stream, p, pieces);
+  const dim3 grid(2 * pieces + (p.k_scales || p.weights ? 1 : 0), (unsigned)(lists < 65535 ? lists : 65535));
+  return launch_kernel(keep_kernel<LANES, SETS>, grid, dim3(kKeepThreads), 0, stream, p, pieces);
+}
+}  // namespace
+
+hipError_t launch_cache_keep(const KeepParams& p, hipStream_t stream) {
+  const int pieces = (int64_t)p.seq.n * p.heads * 2 >= 256 || p.row_bytes < 128 ? 1 : p.row_bytes / 64, lanes = p.row_bytes / pieces / 16;
+  // Long lists: more entries between two barriers, if fewer workgroups share a compute unit (64 lists of up to 4608 keys on 8 heads of 128 bytes 247 -> 238 us, of 256 bytes 467 -> 456, one of 32768 53 -> 46; but
+  // of 600 keys 23 -> 42).
+  const bool many = p.most > 2048;
+  if (lanes == 16) return many ? launch_keep<16, 2>(p, pieces, stream) : launch_keep<16, 1>(p, pieces, stream);
+  if (lanes == 8) return many ? launch_keep<8, 4>(p, pieces, stream) : launch_keep<8, 1>(p, pieces, stream);
+  return many ? launch_keep<4, 4>(p, pieces, stream) : launch_keep<4, 1>(p, pieces, stream);
 }
 
 }  // namespace tr

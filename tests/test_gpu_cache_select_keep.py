@@ -119,6 +119,28 @@ def test_keep_paths(lib, f8):
     _keep(lib, c, [[[s + j for j in p]] for s, p in zip(start, paths)], [len(p) for p in paths], start)
 
 
+@pytest.mark.parametrize("f8", [False, True])
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("seqs", [1, 64])
+def test_keep_long_lists(lib, seqs, D, f8):
+    """Lists that take several turns of a workgroup, whole rows and pieces of them."""
+    kv, n, H = 3100 + 16 * (seqs == 1) * 400, 2900, 2
+    c = Cache([kv] * seqs, [0] * seqs, H, D, 16, f8, "token" if D == 64 else "head", seed=10, poison=False)
+    g = torch.Generator().manual_seed(seqs)
+    keys = torch.rand(seqs, H, kv, generator=g).topk(n).indices.sort(-1).values
+    w = torch.rand(c.n_pages, H, 16, generator=g).cuda()
+    head = torch.arange(H)[None, :, None]
+    place = lambda i: (c.table.cpu().long()[torch.arange(seqs)[:, None, None], i // 16], head, i % 16)   # noqa: E731
+    ref = {}
+    for k, t in _tensors(c, w).items():
+        t = t.cpu()
+        ref[k] = t.clone()
+        ref[k][place(torch.arange(n).expand(seqs, H, n))] = t[place(keys)]
+    lib.tr_cache_keep(c.pages["k"], c.pages["v"], c.table, c.kv_len, keys.to(torch.int32).cuda(), torch.full((seqs,), n, dtype=torch.int32, device="cuda"), None, *c.scale_args(), w)
+    for k, t in _tensors(c, w).items():
+        assert torch.equal(t.cpu(), ref[k]), k
+
+
 def test_keep_skips_what_it_cannot_do(lib):
     """Entries beyond the keys, negative, that would move up, or that come from or go to no page; counts out of range."""
     c = Cache([100, 100, 100, 100], [0] * 4, 2, 64, 16, True, "head", seed=7)
