@@ -180,10 +180,11 @@ def test_tensors_that_are_not_on_the_gpu(tr):
         tr.tr_paged_attn_tree_workspace_bytes(torch.zeros(1, 8, 3, 128, dtype=torch.bfloat16), torch.zeros(4, 2, 16, 128, dtype=torch.bfloat16), i(4))
 
 
-def test_bits_of_a_tree(tmp_path):
-    exe = str(tmp_path / "tree_bits_check")
+@pytest.mark.parametrize("name,ok", [("tree_bits_check", "tree bits ok"), ("tree_launch_check", "tree launches ok")])
+def test_host_checks(tmp_path, name, ok):
+    exe = str(tmp_path / name)
     subprocess.run(["g++", "-O1", "-std=c++17", "-Wall", "-Wextra", "-Werror", "-fsanitize=address,undefined", "-I",
-                    os.path.join(ROOT, "paper_2412_20501_amd", "csrc"), os.path.join(ROOT, "tests", "c_abi", "tree_bits_check.cpp"), "-o", exe],
+                    os.path.join(ROOT, "paper_2412_20501_amd", "csrc"), os.path.join(ROOT, "tests", "c_abi", name + ".cpp"), "-o", exe],
                    check=True, capture_output=True, text=True)
     res = subprocess.run([exe], capture_output=True, text=True, timeout=120)
-    assert res.returncode == 0 and "tree bits ok" in res.stdout, res.stdout + res.stderr
+    assert res.returncode == 0 and ok in res.stdout, res.stdout + res.stderr

@@ -289,6 +289,53 @@ def test_pages_past_32_bits(lib):
         assert torch.equal(dense(x)[:, :300], want[x])
 
 
+@pytest.mark.parametrize("gq", [17, 33, 40, 100])
+@pytest.mark.parametrize("rows", ["few", "many", "long"])
+def test_wide_groups(lib, gq, rows):
+    """More query heads a K/V head than a tile of rows has rows, or a number that divides none."""
+    kv, q = {"few": ([70, 300], [1, 0]), "many": ([70, 300, 1000], [3, 9, 2]), "long": ([400] * 110, [2] * 110)}[rows]
+    c = Cache(kv, q, 1, 64, 16, rows == "many", "head", seed=gq)
+    x = _tokens(c.tokens, gq, 64, 1)
+    lse = lse_of(c, x, 0.125, lambda b: causal_mask(c, b))
+    w = torch.rand(c.n_pages, 1, 16, generator=torch.Generator().manual_seed(1)).cuda()
+    ref, err = weigh(c, x, lse, 0.125, w, True, lambda b: causal_mask(c, b))
+    lib.tr_cache_weigh(x, lse, c.pages["k"], c.table, c.kv_len, c.q_start, True, 0.125, w, True, c.scales["k"])
+    _near(w, ref, err)
+    if rows != "long":
+        sees = [tree_of([-1] * n) for n in q]
+        out, l = torch.zeros_like(x), torch.zeros(1, gq, c.tokens, device="cuda")
+        lib.tr_paged_attn_tree(x, *c.args(), c.q_start, torch.cat([packed(s, 1) for s in sees if len(s)]).cuda(), 0.125, out, l, *c.scale_args())
+        check(attention_on(c, x, 0.125, lambda b: seen_in_tree(c, b, sees[b])), out, l)
+
+
+def test_more_lists_than_a_grid_has_rows(lib):
+    """70000 sequences of one page each: chosen from and moved."""
+    n, D = 70000, 64
+    g = torch.Generator().manual_seed(2)
+    table = torch.randperm(n, generator=g).to(torch.int32).cuda().unsqueeze(1)
+    kv_len = torch.randint(0, 17, (n,), generator=g).to(torch.int32).cuda()
+    w = torch.rand(n, 1, 16, generator=g).cuda()
+    k = torch.randint(-9, 9, (n, 1, 16, D), generator=g).bfloat16().cuda()
+    v = k + 1
+    keys, count = torch.full((n, 1, 5), -1, dtype=torch.int32, device="cuda"), torch.zeros(n, dtype=torch.int32, device="cuda")
+    lib.tr_cache_select(w, table, kv_len, 1, 1, keys, count)
+    slots = torch.arange(16, device="cuda")
+    at = table[:, 0].long()
+    rank = w[at, 0].double()
+    rank = torch.where((slots < 1) | (slots == kv_len[:, None] - 1), 2.0, rank)
+    rank = torch.where(slots < kv_len[:, None], rank, -1.0)
+    best = rank.sort(dim=-1, descending=True, stable=True).indices[:, :5]
+    there = torch.arange(5, device="cuda") < kv_len.clamp(max=5)[:, None]
+    best = torch.where(there, best, 99).sort(-1).values
+    assert torch.equal(count, kv_len.clamp(max=5)) and torch.equal(keys[:, 0].long(), torch.where(there, best, -1))
+    want_k, want_w = k.clone(), w.clone()
+    seq, i = there.nonzero(as_tuple=True)
+    want_k[at[seq], 0, i] = k[at[seq], 0, best[seq, i]]
+    want_w[at[seq], 0, i] = w[at[seq], 0, best[seq, i]]
+    lib.tr_cache_keep(k, v, table, kv_len, keys, count, weights=w)
+    assert torch.equal(k, want_k) and torch.equal(v, want_k + 1) and torch.equal(w, want_w)
+
+
 def test_refusals_in_python(lib):
     c = Cache([100], [2], 2, 64, 16, False, "head", seed=90)
     q, lse = _tokens(2, 8, 64, 91), torch.zeros(1, 8, 2, device="cuda")
