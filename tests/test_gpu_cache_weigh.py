@@ -134,6 +134,27 @@ def test_masked_keys_may_hold_anything(lib, n):
     assert torch.equal(w0, w1)
 
 
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("n", [2, 40, 500])
+def test_masked_keys_may_hold_anything_in_8_bits(lib, n, D):
+    """A NaN among the values, and a scale that is none, of the two last keys: they reach the weights of those keys alone."""
+    c = Cache([633], [n], 2, D, 16, True, "head", seed=9)
+    q = torch.randn(1, 8, n, D, generator=torch.Generator().manual_seed(1)).bfloat16().cuda()
+    lse = lse_of(c, q, 0.1, lambda b: causal_mask(c, b))
+    w0 = torch.zeros(c.n_pages, 2, 16, device="cuda")
+    w1 = w0.clone()
+    args = (c.table, c.kv_len, c.q_start, True, 0.1)
+    lib.tr_cache_weigh(q, lse, c.pages["k"], *args, w0, True, c.scales["k"])
+    at = [(int(c.table[0, key // 16]), key % 16) for key in (631, 632)]
+    c.pages["k"].view(torch.uint8)[at[0][0], :, at[0][1], 3] = 0x7f
+    c.scales["k"].view(torch.uint8)[at[1][0], :, at[1][1]] = 255
+    lib.tr_cache_weigh(q, lse, c.pages["k"], *args, w1, True, c.scales["k"])
+    for page, slot in at:
+        assert w1[page, :, slot].isnan().all()
+        w1[page, :, slot] = w0[page, :, slot]
+    assert torch.equal(w0, w1)
+
+
 def test_steps_add_up_to_what_a_chunk_adds(lib):
     """A prompt token by token, and at once: each key's weights over the causal softmax, whose sum over the keys is one a row."""
     n, Hq = 150, 8

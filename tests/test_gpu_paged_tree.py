@@ -165,6 +165,21 @@ def test_masked_keys_may_hold_anything(lib, n):
         check([(slice(0, n - 1), ref_o[:, :, :-1], ref_l[:, :, :-1], d_o[:, :, :-1], d_l[:, :, :-1])], out, lse)
 
 
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("n", [4, 40, 70])
+def test_masked_keys_may_hold_anything_in_8_bits(lib, n, D):
+    """The same of 8-bit drafts whose scales are none."""
+    c = Cache([333], [n], 2, D, 16, True, "head", seed=9)
+    page, slot = int(c.table[0, 332 // 16]), 332 % 16
+    for name in "kv":
+        c.scales[name].view(torch.uint8)[page, :, slot] = 255
+    _, out, lse, _ = _run(lib, c, 8)
+    assert out[:, :, n - 1].isnan().all()
+    _, _, _, found = _run(lib, Cache([333], [n], 2, D, 16, True, "head", seed=9), 8)
+    for (rows, ref_o, ref_l, d_o, d_l) in found:
+        check([(slice(0, n - 1), ref_o[:, :, :-1], ref_l[:, :, :-1], d_o[:, :, :-1], d_l[:, :, :-1])], out, lse)
+
+
 @pytest.mark.parametrize("n", [3, 70])
 def test_entries_that_are_no_pages(lib, n):
     c = Cache([500, 3000], [n, n], 2, 128, 16, False, "token", seed=7)
