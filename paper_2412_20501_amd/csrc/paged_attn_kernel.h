@@ -497,12 +497,13 @@ __global__ void __launch_bounds__(256, paged_few_waves(D, F8, RT)) paged_few_ker
 // A workgroup has pieces of 1024 / D rows of a tile, D / 4 lanes a row.  What bounds it is latency: the lanes of a row
 // fetch the lse of one part each, and pieces of eight parts are on their way at a time.
 // Of trees, whose tiles may have few rows, pieces that have none are not counted, and a workgroup has two turns: 16 trees of 100 rows on 8 heads 17.8 -> about 11 us.
+// SHARED, for few tiles in many parts: pieces of a wave's rows, of whose parts each wave has a quarter, added up in the waves' order (100 rows of two heads of 64 in 94 parts 24 -> 8.5 us, 32 of eight of 128 in 32 parts 11 -> 5.8).
 template <typename P>
 constexpr int fold_turns = is_tree<P> ? 2 : 1;
-template <int D, bool OUT_F32, typename P>
+template <int D, bool OUT_F32, bool SHARED, typename P>
 __global__ void __launch_bounds__(256) paged_fold_kernel(const P p) {
   constexpr int LANES = D / 4, ROWS = 256 / LANES, AHEAD = 8;
-  constexpr int TURNS = fold_turns<P>, PIECE = ROWS * TURNS;   // rows of a piece
+  constexpr int TURNS = SHARED ? 1 : fold_turns<P>, PIECE = SHARED ? 64 / LANES : ROWS * TURNS;   // rows of a piece
   const Plan plan = make_plan(p);
   const int part = plan.part, size = p.rows.tile, pieces = max(1, size / PIECE);
   auto cut_tiles = [&](const Sequence& q) { return parts_of(q.len, part) > 1 ? tiles_of(q.n * p.gq, p.rows) * p.Hkv : 0; };
@@ -542,8 +543,15 @@ __global__ void __launch_bounds__(256) paged_fold_kernel(const P p) {
   w.n_parts = 1;   // what follows is stored for good
   const int c = (int)threadIdx.x % LANES;
   for (int turn = 0; turn < TURNS; turn++) {
-    const int r = piece * PIECE + turn * ROWS + (int)threadIdx.x / LANES;
-    if (r >= rows) break;
+    int r = piece * PIECE + turn * ROWS + (int)threadIdx.x / LANES, first = 0, end = n_live;   // parts of the wave
+    if (!SHARED && r >= rows) break;
+    const int wave = uniform((int)threadIdx.x >> 6), row = r - wave * PIECE;
+    if constexpr (SHARED) {
+      const int each = (n_live + 3) / 4;
+      first = min(wave * each, n_live);
+      end = min(first + each, n_live);
+      r = min(row, rows - 1);
+    }
     const int64_t slot_row = ((int64_t)base + (int64_t)i * parts) * size + r;
     const float* const ls = p.part_lse + slot_row;
     const float* const out = p.part_out + slot_row * D + 4 * c;
@@ -561,21 +569,39 @@ __global__ void __launch_bounds__(256) paged_fold_kernel(const P p) {
     }
     f32x4 o = {0.f, 0.f, 0.f, 0.f};
     float total = 0.f;
-    for (int k0 = 0; k0 < n_live; k0 += LANES) {
+    for (int k0 = first; k0 < end; k0 += LANES) {
       float mine = -INFINITY;   // weight of part k0 + c; -inf, in its place, of a part without a visible key, whose result says nothing
-      if (k0 + c < n_live) mine = ls[(int64_t)(k0 + c) * size];
+      if (k0 + c < end) mine = ls[(int64_t)(k0 + c) * size];
       mine = mine == -INFINITY ? 0.f : expf(mine - top);
-      for (int k1 = k0; k1 < min(k0 + LANES, n_live); k1 += AHEAD) {
+      for (int k1 = k0; k1 < min(k0 + LANES, end); k1 += AHEAD) {
         f32x4 y[AHEAD];
 #pragma unroll
-        for (int j = 0; j < AHEAD; j++) y[j] = *reinterpret_cast<const f32x4*>(out + (int64_t)min(k1 + j, n_live - 1) * size * D);
+        for (int j = 0; j < AHEAD; j++) y[j] = *reinterpret_cast<const f32x4*>(out + (int64_t)min(k1 + j, end - 1) * size * D);
 #pragma unroll
         for (int j = 0; j < AHEAD; j++) {
-          const float a = k1 + j < n_live ? __shfl(mine, k1 - k0 + j, LANES) : 0.f;
+          const float a = k1 + j < end ? __shfl(mine, k1 - k0 + j, LANES) : 0.f;
           total += a;
 #pragma unroll
           for (int e = 0; e < 4; e++) o[e] += a == 0.f ? 0.f : a * y[j][e];
         }
+      }
+    }
+    if constexpr (SHARED) {
+      __shared__ float of_waves[3][5][64];   // results and totals of the lanes of waves 1 to 3
+      const int lane = (int)threadIdx.x & 63;
+      __syncthreads();   // (those of the piece before have been read)
+      if (wave > 0) {
+#pragma unroll
+        for (int e = 0; e < 4; e++) of_waves[wave - 1][e][lane] = o[e];
+        of_waves[wave - 1][4][lane] = total;
+      }
+      __syncthreads();
+      if (wave > 0 || row >= rows) continue;
+#pragma unroll
+      for (int x = 0; x < 3; x++) {
+#pragma unroll
+        for (int e = 0; e < 4; e++) o[e] += of_waves[x][e][lane];
+        total += of_waves[x][4][lane];
       }
     }
     const float inv = total == 0.f ? 0.f : 1.f / total;

@@ -28,7 +28,11 @@ hipError_t launch_out(P& p, const PagedLaunch& l, float* workspace, hipStream_t 
     if (e != hipSuccess) return e;
     if (p.share.most() == 0) continue;
     const unsigned cut = (unsigned)std::min<int64_t>(c.tiles, p.share.most());   // tiles that are cut, at most
-    e = launch_kernel(paged_fold_kernel<D, OUT_F32, P>, dim3(std::min(cut * (unsigned)std::max(1, c.rows.tile * D / 1024 / fold_turns<P>), 1024u)), dim3(256), 0, stream, p);
+    // Few tiles in more than eight parts each: shared (a tree of 100 rows on 2 heads of 64 and 24K keys, in 94 parts, 38 -> 22 us; but four of 256 rows on 8 heads and 8K keys, in eight, 56 -> 59).
+    if (is_tree<P> && std::min<int64_t>(p.share.most() / cut, c.parts) > 8)
+      e = launch_kernel(paged_fold_kernel<D, OUT_F32, is_tree<P>, P>, dim3(std::min(cut * (unsigned)(c.rows.tile * D / 256), 1024u)), dim3(256), 0, stream, p);
+    else
+      e = launch_kernel(paged_fold_kernel<D, OUT_F32, false, P>, dim3(std::min(cut * (unsigned)std::max(1, c.rows.tile * D / 1024 / fold_turns<P>), 1024u)), dim3(256), 0, stream, p);
     if (e != hipSuccess) return e;
   }
   return hipSuccess;

@@ -1,4 +1,5 @@
 """tr_paged_attn_tree against a 64-bit implementation, within bounds that follow from its roundings (paged_util)."""
+import math
 import random
 
 import pytest
@@ -80,6 +81,33 @@ def test_any_bits(lib, n, f8):
     _, out, lse, found = _run(lib, c, 8, kind="any", out_dtype=torch.float32)
     check(found, out, lse)
     assert (out[:, :, 0] == 0).all() and torch.isneginf(lse[:, :, 0]).all()
+
+
+@pytest.mark.parametrize("f8", [False, True])
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("kv,q,Hkv,gq", [
+    ([9000], [25], 2, 4),                    # 100 rows, 36 parts
+    ([9000, 40, 3000, 130], [5, 3, 20, 4], 1, 4),
+    ([5000, 4999], [1, 2], 1, 1),            # a row or two
+    ([6000, 700], [77, 131], 1, 5),          # two and three tiles, the last ones of few rows
+    ([20000], [300], 1, 1),
+])
+def test_few_tiles_in_many_parts(lib, kv, q, Hkv, gq, D, f8):
+    """Trees behind long texts, whose parts the waves of the fold share; also with parts that some rows, or all, see nothing of, and with an infinity in V."""
+    c = Cache(kv, q, Hkv, D, 32, f8, "head", seed=len(kv) + D)
+    _, out, lse, found = _run(lib, c, Hkv * gq, behind=2)
+    check(found, out, lse)
+    pos = [n // 3 if i % 2 == 0 else -2 for i, n in enumerate(kv)]
+    _, out, lse, found = _run(lib, c, Hkv * gq, pos=pos, kind="any", out_dtype=torch.float32)
+    check(found, out, lse)
+    key = kv[0] - q[0]                       # the first draft
+    page, slot = int(c.table[0, key // 32]), key % 32
+    if f8:
+        c.pages["v"].view(torch.uint8)[page, 0, slot, 7] = 127
+    else:
+        c.pages["v"][page, 0, slot, 7] = math.inf
+    _, out, lse, found = _run(lib, c, Hkv * gq, kind="any")
+    check(found, out, lse)
 
 
 def test_words_that_are_too_few_and_too_many(lib):
