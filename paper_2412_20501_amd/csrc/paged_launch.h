@@ -8,9 +8,15 @@
 namespace tr {
 namespace {
 
+template <int D, bool F8, bool OUT_F32>
+hipError_t launch_half(const TreeParams& p, std::atomic<uint64_t>& raised, dim3 items, hipStream_t stream) {
+  return launch_lds(paged_half_kernel<D, F8, OUT_F32, TreeParams>, raised, items, dim3(256), Tile<D, 4>::LDS, stream, p);
+}
+template <int D, bool F8, bool OUT_F32>
+hipError_t launch_half(const PagedParams&, std::atomic<uint64_t>&, dim3, hipStream_t) { return hipErrorInvalidValue; }   // (trees alone have such rows)
 template <int D, bool F8, bool OUT_F32, typename P>
 hipError_t launch_out(P& p, const PagedLaunch& l, float* workspace, hipStream_t stream) {
-  static std::atomic<uint64_t> raised[3];
+  static std::atomic<uint64_t> raised[4];
   for (int i = 0; i < l.n; i++) {
     const PagedLaunch::Part& c = l.part[i];
     p.rows = c.rows;
@@ -22,7 +28,8 @@ hipError_t launch_out(P& p, const PagedLaunch& l, float* workspace, hipStream_t 
     // Workgroups beyond those that have an item cost a microsecond for every four hundred.  (An eighth of the items for every XCD, rounded up.)
     const dim3 items((unsigned)((c.items(p.share) + 7) / 8 * 8));
     hipError_t e;
-    if (c.rows.tile == kManyRows) e = launch_lds(paged_many_kernel<D, F8, OUT_F32, P>, raised[0], items, dim3(512), Tile<D>::LDS, stream, p);
+    if (c.rows.tile == kManyRows) e = launch_lds(paged_many_kernel<D, F8, OUT_F32, P>, raised[0], items, dim3(512), Tile<D, 8>::LDS, stream, p);
+    else if (c.rows.tile == kHalfRows) e = launch_half<D, F8, OUT_F32>(p, raised[3], items, stream);
     else if (c.rows.tile == 32) e = launch_lds(paged_few_kernel<D, F8, 2, OUT_F32, P>, raised[1], items, dim3(256), Few<D, F8, 2, 4>::LDS, stream, p);
     else e = launch_lds(paged_few_kernel<D, F8, 1, OUT_F32, P>, raised[2], items, dim3(256), Few<D, F8, 1, 4>::LDS, stream, p);
     if (e != hipSuccess) return e;

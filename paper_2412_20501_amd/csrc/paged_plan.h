@@ -135,7 +135,7 @@ constexpr int64_t most_tiles(int64_t tokens, int64_t n_seqs, int64_t group, RowC
 // How a call is launched: one launch for each class of sequences.
 // Waves a SIMD of the kernel for tiles of 16 * rt rows, which are workgroups (of four waves) a compute unit.
 constexpr int paged_few_waves(int D, bool f8, int rt) { return D == 128 ? (rt == 1 && f8 ? 3 : 2) : rt == 1 ? 4 : 3; }
-constexpr int kManyRows = 256;   // rows of the tiles of sequences with many
+constexpr int kManyRows = 256, kHalfRows = 128;   // rows of the tiles of sequences with many; of trees, where whole tiles would leave waves without rows or compute units without tiles
 struct PagedLaunch {
   int n;
   struct Part {
@@ -153,7 +153,11 @@ struct PagedLaunch {
 };
 // The launches of a call.  The lengths are not known here, so it goes by the average rows of a sequence and K/V head: up to 32, sequences are taken to be
 // of single tokens and drafts, and workgroups of 16 or 32 rows serve them all; a lone sequence of more is one of many rows; several are a mixture,
-// a launch for either kind.  The sequences of a tree's call are taken to be alike: one launch.
+// a launch for either kind.  The sequences of a tree's call are taken to be alike: one launch, of tiles of 128 rows, two workgroups a unit, if those take fewer rounds, or if tiles of 256 leave half of
+// the units without one: where there are more of the smaller ones (not in 8 bits, each value would be converted for half as many rows), or no more of them, but keys to share out.
+// us with 256 / 128 rows, 8 heads of 128 for 32, 1000 keys in bf16: 64 trees of 25 61 / 50, 16 of 64 50 / 33, 16 of 25 36 / 30; on 4000 keys 180 / 176, 90 / 75, 59 / 58; in 8 bits 64 of 25 56 / 47 and
+// 160 / 151.  Not: 32 of 25, which fill the units once, in 8 bits 35 / 38 and 78 / 92; four of 64 on 8K keys 55 / 60; 16 of 25 on 300 keys 20 / 22.  (24 heads for 24 on 4000 keys lose: 32 of 50 244 / 262, in 8 bits 208 / 222,
+// 12 of 64 137 / 147 and 133 / 158: K and V of each tile come from HBM.  Of 396 sizes 175 gain more than 3 in a hundred, 8 lose.)
 inline PagedLaunch paged_launch(int64_t tokens, int64_t n_seqs, int64_t max_keys, int Hkv, int gq, int D, bool f8, bool tree = false) {
   PagedLaunch l;
   const int64_t rows = tokens * gq;
@@ -162,8 +166,13 @@ inline PagedLaunch paged_launch(int64_t tokens, int64_t n_seqs, int64_t max_keys
   const int few = gq <= 4 ? 16 : 32;   // rows of few tokens in a mixture: 16 / gq tokens (4 at groups of 4), 32 / gq beyond (4 at 8, 2 at 16, none above 32)
   const RowClass only_few = {few, 0, few}, only_many = {kManyRows, few, any};
   const bool mixed = !tree && rows > 32 * n_seqs && n_seqs > 1;
+  const RowClass halves = {kHalfRows, 0, any};
+  const int64_t each = n_seqs > 0 ? (rows + n_seqs - 1) / n_seqs : 0;   // rows of a sequence and K/V head
+  const int64_t whole_tiles = (each + kManyRows - 1) / kManyRows * n_seqs * Hkv, half_tiles = (each + kHalfRows - 1) / kHalfRows * n_seqs * Hkv;
+  const bool half = tree && ((half_tiles + 2 * kUnits - 1) / (2 * kUnits) < (whole_tiles + kUnits - 1) / kUnits ||
+                             (2 * whole_tiles <= kUnits && 2 * half_tiles >= kUnits && (half_tiles == whole_tiles ? max_keys > 4 * kPartStep : !f8)));
   l.n = mixed ? 2 : 1;
-  l.part[0].rows = mixed ? only_few : rows <= 16 * n_seqs ? few16 : rows <= 32 * n_seqs ? few32 : many;
+  l.part[0].rows = mixed ? only_few : rows <= 16 * n_seqs ? few16 : rows <= 32 * n_seqs ? few32 : half ? halves : many;
   l.part[1].rows = only_many;
   for (int i = 0; i < l.n; i++) {
     PagedLaunch::Part& c = l.part[i];
@@ -171,9 +180,10 @@ inline PagedLaunch paged_launch(int64_t tokens, int64_t n_seqs, int64_t max_keys
     // Workgroups that the registers of each kernel allow a compute unit; what an item, the fold and its parts cost, measured.  A second round only
     // for launches of few rows that may have more row tiles than a part of the first: the launch has workgroups for all that its plan may choose, and
     // those without an item cost 2 us a round of theirs (a mixture of 527 tokens of 16 sequences 99 us with 1300 of them, 108 with 3800).
-    const int per_unit = c.rows.tile == kManyRows ? 1 : paged_few_waves(D, f8, c.rows.tile / 16);
-    const int rounds = c.rows.tile == kManyRows || 2 * c.tiles <= kUnits * per_unit ? 1 : 2;
-    const Share cut = c.rows.tile == kManyRows ? Share{1, 1, 20, 32, 2} : Share{per_unit, rounds, 36, 64, 2};
+    const bool halved = c.rows.tile == kHalfRows;
+    const int per_unit = c.rows.tile == kManyRows ? 1 : halved ? 2 : paged_few_waves(D, f8, c.rows.tile / 16);
+    const int rounds = c.rows.tile == kManyRows || halved || 2 * c.tiles <= kUnits * per_unit ? 1 : 2;
+    const Share cut = halved ? Share{2, 1, 36, 48, 2} : c.rows.tile == kManyRows ? Share{1, 1, 20, 32, 2} : Share{per_unit, rounds, 36, 64, 2};
     const int64_t two_steps = (max_keys + 2 * kPartStep - 1) / (2 * kPartStep);
     c.parts = two_steps < 1 ? 1 : two_steps;
     c.share = c.parts == 1 ? Share{0, 0, 0, 0, 0} : cut;

@@ -31,7 +31,7 @@ __device__ __forceinline__ float halves_sum(float x) {
 
 // Many rows.
 //
-// The block attention kernel's way (256 rows in eight waves of 32, S^T = K Q^T with 32x32x16 products, P in registers as the B operand of O^T = V^T P^T,
+// The block attention kernel's way (256 rows in eight waves of 32, or 128 in four, S^T = K Q^T with 32x32x16 products, P in registers as the B operand of O^T = V^T P^T,
 // V read from LDS with the transposing read, one softmax sub-tile behind the products in one instruction stream, rings of four 16 KiB tiles of K
 // and of V), on rows that are (token, query head of a K/V head) pairs and with tiles that are gathered from pages: a wave's share of a tile, 8 keys
 // at D 128 and 16 at D 64, lies on one page, whose address is found with scalar loads a tile ahead.  bf16 goes straight from memory into LDS, e4m3 through
@@ -40,11 +40,11 @@ __device__ __forceinline__ float halves_sum(float x) {
 //
 // What is rare takes another way: an item with a page that is none, or with an infinity or NaN in V at a key that only some of its rows see, is computed
 // by few_rows, 16 rows at a time, which holds nothing of either against it and takes five times as long (500 tokens on 12500 keys 114 us, with one entry that is no page 619).
-template <int D>
+template <int D, int WAVES>
 struct Tile {
-  static constexpr int RB = 2 * D, BN = D == 64 ? 128 : 64, NS = 4, TILE_BYTES = BN * RB, ROWS = kManyRows;
+  static constexpr int RB = 2 * D, BN = (D == 64 ? 16 : 8) * WAVES, NS = 4, TILE_BYTES = BN * RB, ROWS = 32 * WAVES;
   static constexpr int RINGS = 2 * NS * TILE_BYTES, FLAG = RINGS, OFF = RINGS + 64, LDS = OFF + ROWS * 8;
-  static_assert(TILE_BYTES == 16384 && 8 * 32 * 4 * D <= RINGS, "the waves' results lie where the rings were");
+  static_assert(TILE_BYTES == 2048 * WAVES && WAVES * 32 * 4 * D <= RINGS, "the waves' results lie where the rings were");
 };
 
 template <int D>
@@ -59,12 +59,14 @@ __device__ __forceinline__ int v_tile_off(int row, int c) {   // the same of a V
 }
 
 // true: done; false: the item needs the other way (nothing has been written)
-template <int D, bool F8, bool OUT_F32, typename P>
+template <int D, bool F8, bool OUT_F32, int WAVES, typename P>
 __device__ __forceinline__ bool tile_rows(const P& p, const Item& w, int slot_row, char* lds) {
-  typedef Tile<D> T;
+  typedef Tile<D, WAVES> T;
   constexpr int RB = T::RB, BN = T::BN, NS = T::NS, TILE_BYTES = T::TILE_BYTES, KS = D / 16, DB = D / 32, CPR = D / 8, SUB = 32, NSW = BN / SUB;
   constexpr int RPI = 1024 / RB, IPW = 2, SHARE = IPW * RPI;   // rows of a wave-wide 16-byte load; loads of a wave, tile and tensor; its rows
-  static_assert(BN / SHARE == 8, "eight waves load a tile");
+  static_assert(BN / SHARE == WAVES, "the waves load a tile");
+  // Tiles are sent in pairs, K of tile a and V of tile a - BEHIND.  Where a tile is a single sub-tile, K is read a tile earlier, and sent a tile earlier too (bf16, whose loads are on their way for a tile).
+  constexpr int BEHIND = NSW == 1 && !F8 ? 2 : 1;
   const int tid = threadIdx.x, wave = uniform(tid >> 6), lane = tid & 63, ql = lane & 31, hf = lane >> 5;
   const int row0 = w.tile * T::ROWS, n_rows = min(T::ROWS, w.q.n * p.gq - row0), qw0 = wave * 32;   // (rows counted within the item)
   const int limit_first = first_limit(p, w.q, row0), end = min(w.k1, last_limit(p, w.q, row0 + n_rows - 1));
@@ -124,7 +126,7 @@ __device__ __forceinline__ bool tile_rows(const P& p, const Item& w, int slot_ro
     const uint64_t x = (uint64_t)(base + off);
     return (decltype(base))(((uint64_t)(unsigned)__builtin_amdgcn_readfirstlane((unsigned)(x >> 32)) << 32) | (unsigned)__builtin_amdgcn_readfirstlane((unsigned)x));
   };
-  // Tiles go out in pairs, K of tile a and V of tile a - 1 (one that is not there is left out): the place of V's tile is the one that K's had.
+  // Tiles go out in pairs, K of tile a and V of tile a - BEHIND (one that is not there is left out): the place of V's tile is one that K's had.
   const int edge_tile = min(limit_first >= end ? n_tiles : max(0, limit_first - w.k0) / BN, n_keys % BN ? last_tile : n_tiles);   // from here on tiles hold keys that some rows do not see
   unsigned bad = 0;
   auto look = [&](u32x4 x) __attribute__((always_inline)) {
@@ -162,9 +164,9 @@ __device__ __forceinline__ bool tile_rows(const P& p, const Item& w, int slot_ro
       for (int i = 0; i < IPW; i++) dma16(src, off[i], lds_off + (wave * IPW + i) * 1024);
     }
   };
-  // bf16: pl_k is the place of tile a, pl_v of tile a - 1.  e4m3, whose values are a pair ahead in registers: of a + 1 and a.
+  // bf16: pl_k is the place of tile a, pl_v of tile a - BEHIND, pl_n of the one between.  e4m3, whose values are a pair ahead in registers: of a + 1 and a.
   int a = 0;
-  Place pl_k = {0, 0}, pl_v = {0, 0};
+  Place pl_k = {0, 0}, pl_v = {0, 0}, pl_n = {0, 0};
   Raw k_raw = {{0, 0, 0, 0}, 127}, v_raw = {{0, 0, 0, 0}, 127};
   auto pair = [&](int k_slot, int v_slot, auto inner_c) __attribute__((always_inline)) {
     constexpr bool INNER = decltype(inner_c)::value != 0;   // both tiles lie in front of the last, and the two behind them
@@ -178,8 +180,13 @@ __device__ __forceinline__ bool tile_rows(const P& p, const Item& w, int slot_ro
       if (INNER || a + 2 <= last_tile) pl_k = place_of(a + 2);
     } else {
       if (INNER || a <= last_tile) send(kb, pl_k, !INNER && a == last_tile, k_off, false, k_slot * TILE_BYTES);
-      if (INNER || (a >= 1 && a - 1 <= last_tile)) send(vb, pl_v, !INNER && a - 1 == last_tile, v_off, true, (NS + v_slot) * TILE_BYTES);
-      pl_v = pl_k;
+      if (INNER || (a >= 1 && a - BEHIND <= last_tile)) send(vb, pl_v, !INNER && a - BEHIND == last_tile, v_off, true, (NS + v_slot) * TILE_BYTES);
+      if constexpr (BEHIND == 2) {
+        pl_v = pl_n;
+        pl_n = pl_k;
+      } else {
+        pl_v = pl_k;
+      }
       if (INNER || a + 1 <= last_tile) pl_k = place_of(a + 1);
     }
     a++;
@@ -217,6 +224,12 @@ __device__ __forceinline__ bool tile_rows(const P& p, const Item& w, int slot_ro
       a = 3;
       pl_k = p3;
       pl_v = p2;
+      if constexpr (BEHIND == 2) {
+        if (last_tile >= 3) send(kb, p3, last_tile == 3, k_off, false, 3 * TILE_BYTES);
+        a = 4;
+        pl_n = p3;
+        if (last_tile >= 4) pl_k = place_of(4);
+      }
     }
   }
   const int qrow = row0 + min(qw0 + ql, n_rows - 1), q_tok = divide(p.by_gq, qrow);
@@ -227,7 +240,7 @@ __device__ __forceinline__ bool tile_rows(const P& p, const Item& w, int slot_ro
     for (int ks = 0; ks < KS; ks++) qf[ks] = *reinterpret_cast<const bf16x8*>(qp + 16 * ks);
   }
   // pages that are none, among all of the item's keys
-  for (int key = w.k0 + tid * 16; key < end; key += 512 * 16) bad |= slot_of(p.seq, w.b, key).page < 0 ? 1u : 0u;
+  for (int key = w.k0 + tid * 16; key < end; key += WAVES * 64 * 16) bad |= slot_of(p.seq, w.b, key).page < 0 ? 1u : 0u;
   // keys that the lane's row, and the first and the last row of the wave, see (in keys from k0 on)
   int lane_end = 0;
   if constexpr (is_tree<P>) *reinterpret_cast<int64_t*>(lds + T::OFF + (qw0 + ql) * 8) = (int64_t)(w.q.start + q_tok) * p.tree_stride;   // (the row's bits; both halves write it)
@@ -405,7 +418,7 @@ __device__ __forceinline__ bool tile_rows(const P& p, const Item& w, int slot_ro
     }
   };
   if (n_tiles > 0) {
-    pair(3, 2, IC<0>{});
+    if constexpr (BEHIND == 1) pair(3, 2, IC<0>{});
     if (jw > 0) {
 #pragma unroll
       for (int i = 0; i < 16; i++) sA[i] = 0.f;
@@ -413,9 +426,18 @@ __device__ __forceinline__ bool tile_rows(const P& p, const Item& w, int slot_ro
       for (int ks = 0; ks < KS; ks++) sA = __builtin_amdgcn_mfma_f32_32x32x16_bf16(load_k(ks, 0), qf[ks], sA, 0, 0, 0);
 #pragma unroll
       for (int ks = 0; ks < KS; ks++) pre[ks] = load_k(ks, SUBB);
+    }
+    if constexpr (BEHIND == 2) {   // (K_4 goes where K_0 was: all waves have read it)
+      __builtin_amdgcn_s_waitcnt(0xC07F);
+      asm volatile("" ::: "memory");
+      __builtin_amdgcn_s_barrier();
+      asm volatile("" ::: "memory");
+      pair(0, 2, IC<0>{});
+    }
+    if (jw > 0) {
       constexpr unsigned k_imm0 = 2 % NSW * SUBB + 2 / NSW * TILE_BYTES;
       step(0, IC<1>{}, IC<0>{}, IC<(int)k_imm0>{}, sA, sB, pB, pA, IC<0>{});
-      tile_step(0, IC<0>{}, IC<1>{}, IC<0>{});
+      if constexpr (NSW > 1) tile_step(0, IC<0>{}, IC<1>{}, IC<0>{});
       if constexpr (NSW > 2) {
         tile_step(0, IC<0>{}, IC<2>{}, IC<0>{});
         tile_step(0, IC<0>{}, IC<3>{}, IC<0>{});
@@ -423,7 +445,7 @@ __device__ __forceinline__ bool tile_rows(const P& p, const Item& w, int slot_ro
     }
   }
   // Tile u = 1 .. n_tiles (the last index folds the last sub-tile's product in): pair u + 3 goes out behind barrier B_u, into the slots of K_{u-1} and V_{u-2};
-  // K_{u+2} and V_{u+1}, the newest pair in front of B_u, may still be on their way there.
+  // K_{u+2} and V_{u+1}, the newest pair in front of B_u, may still be on their way there.  (BEHIND 2: K_{u+4} in the slot of K_u, and K_{u+3} may be on its way.)
   auto tile_body = [&](int u, auto su_c, auto inner_c) __attribute__((always_inline)) {
     constexpr int su = decltype(su_c)::value;
     constexpr bool INNER = decltype(inner_c)::value != 0;
@@ -431,7 +453,7 @@ __device__ __forceinline__ bool tile_rows(const P& p, const Item& w, int slot_ro
       __builtin_amdgcn_s_waitcnt(0xC07F);   // lgkmcnt(0): this wave's part of the tiles has been written
     } else {
       constexpr int none = 0x0F70;
-      if (INNER || u + 2 <= last_tile) __builtin_amdgcn_s_waitcnt(none | 2 * IPW);
+      if (INNER || u + 1 + BEHIND <= last_tile) __builtin_amdgcn_s_waitcnt(none | 2 * IPW);
       else __builtin_amdgcn_s_waitcnt(none);
       asm volatile("" ::: "memory");
       if (!INNER) look_at(u, su);
@@ -439,9 +461,9 @@ __device__ __forceinline__ bool tile_rows(const P& p, const Item& w, int slot_ro
     asm volatile("" ::: "memory");
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
-    pair((su + 3) % NS, (su + 2) % NS, inner_c);
+    pair((su + 2 + BEHIND) % NS, (su + 2) % NS, inner_c);
     tile_step(u, su_c, IC<0>{}, inner_c);
-    tile_step(u, su_c, IC<1>{}, inner_c);
+    if constexpr (NSW > 1) tile_step(u, su_c, IC<1>{}, inner_c);
     if constexpr (NSW > 2) {
       tile_step(u, su_c, IC<2>{}, inner_c);
       tile_step(u, su_c, IC<3>{}, inner_c);
@@ -452,7 +474,7 @@ __device__ __forceinline__ bool tile_rows(const P& p, const Item& w, int slot_ro
   // A tree's few rows may leave waves without any.  Those too send inner tiles as inner ones, or all wait for them: loads that may be left out are waited for at once (16 trees of 100 rows in
   // 8 bits 78 -> 69 us).
   const int j_inner = is_tree<P> && !rows_here ? kPosLimit : min(min(jw, NSW * n_tiles - 1), kmask_from >= 0 ? kmask_from / SUB : -1) - (NSW - 1);
-  const int u_inner = uniform(min(min(j_inner < 0 ? -1 : j_inner / NSW, last_tile - (F8 ? 6 : 5)), edge_tile - 3));
+  const int u_inner = uniform(min(min(j_inner < 0 ? -1 : j_inner / NSW, last_tile - (F8 ? 6 : 4 + BEHIND)), edge_tile - 3));
   if (1 <= n_tiles) tile_body(1, IC<1>{}, IC<0>{});
   if (2 <= n_tiles) tile_body(2, IC<2>{}, IC<0>{});
   if (3 <= n_tiles) tile_body(3, IC<3>{}, IC<0>{});
@@ -524,18 +546,30 @@ __device__ __forceinline__ bool tile_rows(const P& p, const Item& w, int slot_ro
   return true;
 }
 
-template <int D, bool F8, bool OUT_F32, typename P>
-__global__ void __launch_bounds__(512, 2) paged_many_kernel(const P p) {
-  extern __shared__ __attribute__((aligned(1024))) char lds[];
+template <int D, bool F8, bool OUT_F32, int WAVES, typename P>
+__device__ __forceinline__ void many_rows(const P& p, char* lds) {
+  constexpr int ROWS = Tile<D, WAVES>::ROWS;
   Item w;
   if (!find_item(p, make_plan(p), (int)blockIdx.x, w)) return;
-  const int row0 = w.tile * kManyRows, slot_row = w.slot * kManyRows, n = min(kManyRows, w.rows - row0);
-  if (tile_rows<D, F8, OUT_F32>(p, w, slot_row, lds)) return;
+  const int row0 = w.tile * ROWS, slot_row = w.slot * ROWS, n = min(ROWS, w.rows - row0);
+  if (tile_rows<D, F8, OUT_F32, WAVES>(p, w, slot_row, lds)) return;
 #pragma unroll 1
   for (int r = 0; r < n; r += 16) {
     __syncthreads();
-    few_rows<D, F8, 1, 8, false, OUT_F32>(p, w, row0 + r, slot_row + r, lds);
+    few_rows<D, F8, 1, WAVES, false, OUT_F32>(p, w, row0 + r, slot_row + r, lds);
   }
+}
+template <int D, bool F8, bool OUT_F32, typename P>
+__global__ void __launch_bounds__(512, 2) paged_many_kernel(const P p) {
+  extern __shared__ __attribute__((aligned(1024))) char lds[];
+  many_rows<D, F8, OUT_F32, 8>(p, lds);
+}
+// Trees alone: 128 rows, two workgroups a compute unit, so that one's set-up and epilogue run beside the other's products.  A tile at D 128 is one sub-tile of 32 keys: in bf16 K is sent a tile
+// earlier for that (64 trees of 25 tokens, 8 heads of 128 for 32, 1000 keys: 50 us, in bf16, 47 in 8 bits; with 256 rows, of which 100 are there, 61 and 56).
+template <int D, bool F8, bool OUT_F32, typename P>
+__global__ void __launch_bounds__(256, 2) paged_half_kernel(const P p) {
+  extern __shared__ __attribute__((aligned(1024))) char lds[];
+  many_rows<D, F8, OUT_F32, 4>(p, lds);
 }
 
 }  // namespace

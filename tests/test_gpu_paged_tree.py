@@ -110,6 +110,52 @@ def test_few_tiles_in_many_parts(lib, kv, q, Hkv, gq, D, f8):
     check(found, out, lse)
 
 
+MANY = [
+    # keys, drafts, Hkv, query heads a K/V head, page
+    ([700, 30, 1500, 33, 400, 0, 64, 901] * 2, [25, 30, 25, 33, 25, 0, 64, 1] * 2, 8, 4, 32),          # 128 tiles of up to 256 rows
+    ([1300, 64, 500] * 5, [64, 64, 64] * 5, 8, 4, 16),                                                # two tiles of 128 rows each
+    ([200, 41, 333, 100, 40, 900] * 8, [40, 41, 33, 40, 40, 37] * 8, 12, 1, 48),                      # more tiles than units
+    ([4000, 350, 80, 2222] * 10, [60, 70, 65, 75] * 10, 8, 4, 64),                                    # two and three tiles each
+]
+
+
+@pytest.mark.parametrize("f8", [False, True])
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("shape", MANY)
+def test_many_trees(lib, shape, D, f8):
+    """Trees that fill the chip: one launch of smaller tiles, or of whole ones where keys are in 8 bits."""
+    kv, q, Hkv, gq, page = shape
+    c = Cache(kv, q, Hkv, D, page, f8, "head" if D == 64 else "token", seed=D + len(kv))
+    for workspace in (True, False):
+        _, out, lse, found = _run(lib, c, Hkv * gq, workspace=workspace, behind=2)
+        check(found, out, lse)
+    again = _run(lib, c, Hkv * gq, workspace=False, behind=2)
+    assert torch.equal(out, again[1]) and torch.equal(lse, again[2])
+
+
+@pytest.mark.parametrize("f8", [False, True])
+@pytest.mark.parametrize("D", [64, 128])
+def test_many_trees_with_any_bits_positions_and_bad_values(lib, D, f8):
+    kv, q, Hkv, gq, page = MANY[0]
+    pos = [n // 2 if i % 3 == 0 else -5 if i % 3 == 1 else n for i, n in enumerate(kv)]
+    c = Cache(kv, q, Hkv, D, page, f8, "head", seed=3)
+    for at in (None, pos):
+        _, out, lse, found = _run(lib, c, Hkv * gq, pos=at, kind="any", out_dtype=torch.float32)
+        check(found, out, lse)
+    for b in (0, 2, 4):
+        key = kv[b] - q[b] + 1
+        where, slot = int(c.table[b, key // page]), key % page
+        if f8:
+            c.pages["v"].view(torch.uint8)[where, 1, slot, 5] = 127
+        else:
+            c.pages["v"][where, 1, slot, 5] = math.inf
+    c.table[0, 3] = -1
+    c.table[10, 20] = c.n_pages + 7
+    c.table[12, 0] = 1 << 30
+    _, out, lse, found = _run(lib, c, Hkv * gq)
+    check(found, out, lse)
+
+
 def test_words_that_are_too_few_and_too_many(lib):
     """Drafts behind the last word are seen by none; words behind the last draft say nothing."""
     for n, words in ((70, 1), (70, 2), (70, 9), (20, 3)):
