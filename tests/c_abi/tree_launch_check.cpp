@@ -12,7 +12,7 @@
 int main() {
   std::mt19937_64 rng(17);
   auto any = [&](int64_t lo, int64_t hi) { return lo + (int64_t)(rng() % (uint64_t)(hi - lo + 1)); };
-  int cut_calls = 0, tiles_met[3] = {};
+  int cut_calls = 0, cut_of_128 = 0, tiles_met[4] = {};
   for (int round = 0; round < 30000; round++) {
     const int n = (int)any(1, round % 3 ? 12 : 300), gq = (int)any(1, round % 7 ? 9 : 80), Hkv = (int)any(1, 24), max_pages = (int)any(1, (int64_t)1 << any(0, 13)), drafts = (int)any(0, 1 << any(0, 8));
     std::vector<int> start(n + 1), len(n), table(1);
@@ -28,7 +28,7 @@ int main() {
     const tr::PagedLaunch l = tr::paged_launch(tokens, n, (int64_t)max_pages * 16, Hkv, gq, D, round % 5 == 0, true);
     EXPECT(l.n == 1);
     const tr::PagedLaunch::Part& c = l.part[0];
-    tiles_met[c.rows.tile == 16 ? 0 : c.rows.tile == 32 ? 1 : 2]++;
+    tiles_met[c.rows.tile == 16 ? 0 : c.rows.tile == 32 ? 1 : c.rows.tile == 128 ? 2 : 3]++;
     for (bool shared : {true, false}) {
       const tr::Share share = shared ? c.share : tr::Share{0, 0, 0, 0, 0};
       int64_t work = 0, tiles = 0, items = 0, slots = 0, cut = 0;
@@ -55,9 +55,10 @@ int main() {
       EXPECT(items <= c.items(share) && slots <= share.slots(c.tiles) && slots * c.rows.tile * (D + 1) <= c.floats(D));
       EXPECT(shared || cut == 0);
       cut_calls += cut > 0;
+      cut_of_128 += cut > 0 && c.rows.tile == 128;
     }
   }
-  if (cut_calls < 1000 || !tiles_met[0] || !tiles_met[1] || !tiles_met[2]) { printf("FAILED: %d cut\n", cut_calls); return 1; }
+  if (cut_calls < 1000 || cut_of_128 < 100 || !tiles_met[0] || !tiles_met[1] || !tiles_met[2] || !tiles_met[3]) { printf("FAILED: %d cut, %d\n", cut_calls, cut_of_128); return 1; }
   printf("tree launches ok\n");
   return 0;
 }
