@@ -77,7 +77,7 @@ __device__ __forceinline__ void add_weight(const WeighParams& p, const WeighItem
 // keys are on their way beside this one's keys (found one after the other, table, then keys: 173 us for the 139 below).  Bound: HBM: a token of 64 sequences of 0.8K to 16K keys on 8 heads of 128 in 8 bits
 // 135 us, 4.5 TB/s of K and weights; of 16 of 8K in bf16 44.5 us, 6.2 TB/s.
 template <int D, bool F8>
-__device__ __forceinline__ void weigh_few(const WeighParams& p, const RowClass& c, const Plan& plan) {
+__device__ __forceinline__ void weigh_few(const WeighParams& p, const RowClass& c, const Plan& plan, int turn) {   // turn: of the XCD's workgroups, the items' order
   constexpr int QS = D / 32, KL = F8 ? D / 64 : D / 32;
   const int total = uniform(all_items<kFewKeys>(p, c, plan)), each = (total + 7) >> 3, base = ((int)blockIdx.x & 7) * each, end = min(each, total - base);
   const int lane = threadIdx.x & 63, wave = uniform((int)threadIdx.x >> 6), i16 = lane & 15, g = lane >> 4;
@@ -91,8 +91,8 @@ __device__ __forceinline__ void weigh_few(const WeighParams& p, const RowClass& 
     const int key = item.k0 + wave * 64 + lane;
     if (key < item.seen) slot = slot_of(p.seq, item.b, key);
   };
-  find((int)blockIdx.x >> 3, next, mine);
-  for (int at = (int)blockIdx.x >> 3; at < end; at += (int)gridDim.x >> 3) {
+  find(turn, next, mine);
+  for (int at = turn; at < end; at += (int)gridDim.x >> 3) {
     w = next;
     const Slot slot_now = mine;
     const int key0 = w.k0 + wave * 64, rows = w.q.n * p.gq;
@@ -401,7 +401,7 @@ __device__ __forceinline__ void weigh_many(const WeighParams& p, const RowClass&
 // the same time (a prompt of 700 tokens among 15 single ones, 24 heads of 64, 4000 keys: 51 us, in two launches 56).  Fewer than 8 sequences are not worth it: all are taken for ones of many rows.
 constexpr RowClass kAny = {32, 0, 0x7fffffff}, kFewRows = {32, 0, 32}, kManyMore = {32, 32, 0x7fffffff};
 template <int D, bool F8>
-__global__ void __launch_bounds__(256, kFewWaves) weigh_few_kernel(const WeighParams p) { weigh_few<D, F8>(p, kAny, sums_plan(p)); }
+__global__ void __launch_bounds__(256, kFewWaves) weigh_few_kernel(const WeighParams p) { weigh_few<D, F8>(p, kAny, sums_plan(p), (int)blockIdx.x >> 3); }
 template <int D, bool F8>
 __global__ void __launch_bounds__(256, 2) weigh_many_kernel(const WeighParams p) {
   __shared__ __attribute__((aligned(1024))) char lds[Many<D>::LDS];
@@ -415,7 +415,7 @@ __global__ void __launch_bounds__(256, 2) weigh_mixed_kernel(const WeighParams p
 #pragma unroll 1
   for (int turn = 0; turn < 2; turn++) {
     if (turn == first) weigh_rows<D, F8, false>(p, kManyMore, plan, lds);
-    else weigh_few<D, F8>(p, kFewRows, plan);
+    else weigh_few<D, F8>(p, kFewRows, plan, ((int)gridDim.x - 1 - (int)blockIdx.x) >> 3);   // (from the last workgroup on: where there are few items, none has one of either kind)
   }
 }
 
@@ -425,7 +425,8 @@ hipError_t launch_form(const WeighParams& p, hipStream_t stream) {
   const bool few = rows <= 32 * n;   // on average: single tokens and drafts
   const int64_t width = few ? kFewKeys : 64, items = n * p.Hkv * ((max_keys + width - 1) / width);
   const int64_t most = few ? 256 * kFewWaves : 512;   // workgroups that the compute units hold
-  const dim3 grid((unsigned)((items < most ? items : most) + 7) / 8 * 8), block(256);
+  const int64_t wanted = items + (few || n < 8 ? 0 : 8);   // (a mixture's two kinds are rounded up apart)
+  const dim3 grid((unsigned)((wanted < most ? wanted : most) + 7) / 8 * 8), block(256);
   if (few) return launch_kernel(weigh_few_kernel<D, F8>, grid, block, 0, stream, p);
   if (n < 8) return launch_kernel(weigh_many_kernel<D, F8>, grid, block, 0, stream, p);
   return launch_kernel(weigh_mixed_kernel<D, F8>, grid, block, 0, stream, p);
