@@ -19,7 +19,7 @@ typedef float f32x16 __attribute__((ext_vector_type(16)));
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr int kFewWaves = 4;     // a SIMD, of few rows
 constexpr int kFewKeys = 256;    // of an item of few rows: 64 a wave
-constexpr int kTogetherBelow = 192;   // items of many rows
+constexpr int kTogetherBelow = 192, kTogetherInMixture = 128;   // items of many rows
 constexpr int kManyKeys = 256;   // of many rows: 64 a wave, or, where that leaves compute units without an item, 64 that the waves have together
 
 // Items: (sequence, K/V head, stretch of keys) of the launch's sequences, numbered so that those of a head lie together, and each XCD has a contiguous eighth of all.
@@ -220,7 +220,9 @@ __device__ __forceinline__ void weigh_rows(const WeighParams& p, const RowClass&
   constexpr int KS = D / 16, CPR = D / 8, LOADS = M::TILE / 4096, EACH = 16 / KS;   // 16-byte loads a thread and tile; exponentials a product
   constexpr int WIDTH = TOGETHER ? 64 : kManyKeys, STEP = TOGETHER ? 4 : 1;         // keys of an item; from a wave's tile to its next one
   const int total = uniform(all_items<WIDTH>(p, c, plan)), each = (total + 7) >> 3, base = ((int)blockIdx.x & 7) * each;
-  const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), l32 = lane & 31, hf = lane >> 5;
+  int tid = threadIdx.x;
+  asm volatile("" : "+v"(tid));   // (or what follows from it is held, in a mixture, over the few rows' turn)
+  const int lane = tid & 63, wave = uniform(tid >> 6), l32 = lane & 31, hf = lane >> 5;
   const float c2 = p.scale * kLog2e;
   const RowStep q_step = row_step(p, 32 * STEP, p.q_sh, p.q_ss), l_step = row_step(p, 32 * STEP, p.l_sh, p.l_ss);
 #pragma unroll 1
@@ -392,20 +394,21 @@ __device__ __forceinline__ void weigh_rows(const WeighParams& p, const RowClass&
   }
 }
 template <int D, bool F8>
-__device__ __forceinline__ void weigh_many(const WeighParams& p, const RowClass& c, const Plan& plan, char* lds) {
-  if (uniform(all_items<kManyKeys>(p, c, plan)) < kTogetherBelow) weigh_rows<D, F8, true>(p, c, plan, lds);
+__device__ __forceinline__ void weigh_many(const WeighParams& p, const RowClass& c, const Plan& plan, int together_below, char* lds) {
+  if (uniform(all_items<kManyKeys>(p, c, plan)) < together_below) weigh_rows<D, F8, true>(p, c, plan, lds);
   else weigh_rows<D, F8, false>(p, c, plan, lds);
 }
 
 // The sequences of a call are all of either kind, or a mixture: then half of the workgroups begin with one and half with the other, so that the loads of few rows and the products of many run at
 // the same time (a prompt of 700 tokens among 15 single ones, 24 heads of 64, 4000 keys: 51 us, in two launches 56).  Fewer than 8 sequences are not worth it: all are taken for ones of many rows.
+// Few keys meet many rows sooner here (8 heads of 128 for 32: a prompt of 512 on 2000 keys among 15 54 -> 32 us with 64 keys a workgroup, of 256 on 3900 45 -> 42, but on 5000 44 -> 51).
 constexpr RowClass kAny = {32, 0, 0x7fffffff}, kFewRows = {32, 0, 32}, kManyMore = {32, 32, 0x7fffffff};
 template <int D, bool F8>
 __global__ void __launch_bounds__(256, kFewWaves) weigh_few_kernel(const WeighParams p) { weigh_few<D, F8>(p, kAny, sums_plan(p), (int)blockIdx.x >> 3); }
 template <int D, bool F8>
 __global__ void __launch_bounds__(256, 2) weigh_many_kernel(const WeighParams p) {
   __shared__ __attribute__((aligned(1024))) char lds[Many<D>::LDS];
-  weigh_many<D, F8>(p, kAny, sums_plan(p), lds);
+  weigh_many<D, F8>(p, kAny, sums_plan(p), kTogetherBelow, lds);
 }
 template <int D, bool F8>
 __global__ void __launch_bounds__(256, 2) weigh_mixed_kernel(const WeighParams p) {
@@ -414,7 +417,7 @@ __global__ void __launch_bounds__(256, 2) weigh_mixed_kernel(const WeighParams p
   const int first = (int)blockIdx.x >> 3 & 1;
 #pragma unroll 1
   for (int turn = 0; turn < 2; turn++) {
-    if (turn == first) weigh_rows<D, F8, false>(p, kManyMore, plan, lds);
+    if (turn == first) weigh_many<D, F8>(p, kManyMore, plan, kTogetherInMixture, lds);
     else weigh_few<D, F8>(p, kFewRows, plan, ((int)gridDim.x - 1 - (int)blockIdx.x) >> 3);   // (from the last workgroup on: where there are few items, none has one of either kind)
   }
 }
@@ -422,7 +425,10 @@ __global__ void __launch_bounds__(256, 2) weigh_mixed_kernel(const WeighParams p
 template <int D, bool F8>
 hipError_t launch_form(const WeighParams& p, hipStream_t stream) {
   const int64_t rows = (int64_t)p.seq.tokens * p.gq, n = p.seq.n, max_keys = (int64_t)p.seq.max_pages * p.seq.page_size;
-  const bool few = rows <= 32 * n;   // on average: single tokens and drafts
+  // On average few: single tokens and drafts; but where a sequence may have many (not all the same number of tokens), and short keys leave the compute units room, a mixture (16 sequences of 300 keys
+  // with a prompt of 100 29.1 -> 10.7 us, 9 of 27 with one of 23 13.9 -> 7.7; drafts of different numbers lose: 16 of 5 on 400 keys 6.8 -> 7.2).
+  const bool short_keys = n * p.Hkv * ((max_keys + kFewKeys - 1) / kFewKeys) <= 512;
+  const bool few = rows <= 32 * n && !(n >= 8 && short_keys && p.seq.tokens % n != 0 && (p.seq.tokens - n + 1) * (int64_t)p.gq > 32);
   const int64_t width = few ? kFewKeys : 64, items = n * p.Hkv * ((max_keys + width - 1) / width);
   const int64_t most = few ? 256 * kFewWaves : 512;   // workgroups that the compute units hold
   const int64_t wanted = items + (few || n < 8 ? 0 : 8);   // (a mixture's two kinds are rounded up apart)

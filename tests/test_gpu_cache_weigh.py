@@ -80,6 +80,26 @@ def test_many_items(lib, mixed, gq, D, f8):
 
 
 @pytest.mark.parametrize("f8", [False, True])
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("kv,q,Hkv,gq", [
+    ([300, 75, 1, 90, 0, 64, 65, 257, 30], [100, 1, 1, 3, 0, 1, 2, 1, 1], 2, 4),      # short keys: a mixture for few rows on average
+    ([27] * 8 + [26], [1] * 8 + [23], 4, 7),
+    ([900, 40, 800, 1000, 700, 650, 300, 5, 33], [500, 1, 1, 130, 1, 1, 9, 1, 17], 3, 5),   # 64 keys a workgroup for many rows
+    ([3000] + [100] * 11, [200] + [1] * 11, 12, 1),                                   # 256
+    ([6, 5, 4, 3, 2, 1, 1, 300], [6, 5, 4, 3, 2, 1, 1, 300], 1, 1),                   # nothing but new tokens
+])
+def test_a_prompt_among_few(lib, kv, q, Hkv, gq, causal, D, f8):
+    c = Cache(kv, q, Hkv, D, 16, f8, "token" if gq == 4 else "head", seed=11)
+    w = _run(lib, c, Hkv * gq, causal, causal, behind=3)
+    assert torch.equal(w, _run(lib, c, Hkv * gq, causal, causal, behind=3))
+    if causal and gq > 1:
+        c.table[0, 1] = -1
+        pos = [n // 2 if i % 2 else n + 3 for i, n in enumerate(kv)]
+        _run(lib, c, Hkv * gq, True, True, pos, layout="apart")
+
+
+@pytest.mark.parametrize("f8", [False, True])
 @pytest.mark.parametrize("causal", [False, True])
 @pytest.mark.parametrize("fresh", [False, True])
 @pytest.mark.parametrize("n", [2, 77])
