@@ -71,12 +71,12 @@ __device__ __forceinline__ void write_four(int* out, const Border& border, int k
   }
 }
 
-// A wave has a stretch of the row's keys, 256 at a time.  Ranks are held in LDS where they fit (`room` of them), and are read from memory again where they do not; those that
-// share the first digit with the border, mostly a few hundredths of them, are held once more as a list, unless it is too long.  Bound: the instructions of one compute unit, and its barriers (512 rows of 4608 keys: 10 us of a workgroup's time, 3 of them for the weights
-// to come; 8 of 32768: 21).
+// A wave has a stretch of the row's keys, 256 at a time.  Ranks are held in LDS, as many as fit (`room`), and those behind them in registers (EXTRA); what is left is read from memory again where it is
+// needed.  Those that share the first digit with the border, mostly a few hundredths of them, are held once more as a list, unless it is too long.  Bound: the instructions of one compute unit, and its barriers
+// (512 rows of 4608 keys: 10 us of a workgroup's time, 3 of them for the weights to come; 8 of 32768: 21; 8 of 65536 30, with all ranks read again where LDS does not hold them 55).
 constexpr int kRoom = 32768, kList = 2048;   // ranks that LDS has room for; entries of the list
-template <int THREADS>
-__global__ void __launch_bounds__(THREADS, 8) select_kernel(const SelectParams p, const int room) {
+template <int THREADS, int EXTRA>   // EXTRA: pieces of four ranks behind those that a thread holds in registers
+__global__ void __launch_bounds__(THREADS, EXTRA > 0 ? 4 : 8) select_kernel(const SelectParams p, const int room) {
   extern __shared__ __attribute__((aligned(16))) char lds[];
   __shared__ __attribute__((aligned(16))) int counts[2 * kDigits + kDigits / 2];   // of the three passes
   __shared__ unsigned list[kList];
@@ -109,9 +109,20 @@ __global__ void __launch_bounds__(THREADS, 8) select_kernel(const SelectParams p
       }
       return u;
     };
-    const bool held = len <= room;
     const int steps = (len + 4 * THREADS - 1) / (4 * THREADS), piece0 = wave * steps * 64 + lane;   // of a wave; pieces of four keys are piece0 + 64 i
-    auto four = [&](int i) __attribute__((always_inline)) -> u32x4 { return held ? ranks[piece0 + 64 * i] : fetch(4 * (piece0 + 64 * i)); };
+    const int in_lds = min(steps, room / (4 * THREADS)), behind = in_lds + EXTRA;                   // pieces in LDS; those from `behind` on are held nowhere
+    u32x4* const mine = ranks + wave * in_lds * 64 + lane;   // (each thread reads what it wrote)
+    u32x4 kept[EXTRA > 0 ? EXTRA : 1];
+    auto over = [&](auto body) __attribute__((always_inline)) {   // all pieces: body(i, ranks)
+      for (int i = 0; i < in_lds; i++) body(i, mine[64 * i]);
+      if constexpr (EXTRA > 0) {
+#pragma unroll
+        for (int j = 0; j < EXTRA; j++)
+          if (in_lds + j < steps) body(in_lds + j, kept[j]);
+      }
+#pragma unroll 1
+      for (int i = behind; i < steps; i++) body(i, fetch(4 * (piece0 + 64 * i)));
+    };
     Border border = {0, p.most};   // (at least one of the keys goes: len > most)
     auto find = [&](int pass, int shift) __attribute__((always_inline)) -> bool {
       __syncthreads();
@@ -135,16 +146,29 @@ __global__ void __launch_bounds__(THREADS, 8) select_kernel(const SelectParams p
     for (int i = tid; i < (2 * kDigits + kDigits / 2) / 4; i += THREADS) reinterpret_cast<u32x4*>(counts)[i] = u32x4{0, 0, 0, 0};
     __syncthreads();
     int zeros = 0;   // (most weights may be 0: they are counted apart, 64 additions to one place are 64 turns)
-#pragma unroll 4
-    for (int i = 0; i < steps; i++) {
-      const u32x4 x = fetch(4 * (piece0 + 64 * i));
-      if (held) ranks[piece0 + 64 * i] = x;   // (each thread reads what it wrote)
+    auto count = [&](const u32x4 x) __attribute__((always_inline)) {
 #pragma unroll
       for (int k = 0; k < 4; k++) {
         zeros += x[k] == kZero ? 1 : 0;
         if ((x[k] & ~kZero) != 0) atomicAdd(&counts[x[k] >> 21], 1);
       }
+    };
+#pragma unroll 4
+    for (int i = 0; i < in_lds; i++) {
+      const u32x4 x = fetch(4 * (piece0 + 64 * i));
+      mine[64 * i] = x;
+      count(x);
     }
+    if constexpr (EXTRA > 0) {
+#pragma unroll
+      for (int j = 0; j < EXTRA; j++)
+        if (in_lds + j < steps) kept[j] = fetch(4 * (piece0 + 64 * (in_lds + j)));
+#pragma unroll
+      for (int j = 0; j < EXTRA; j++)
+        if (in_lds + j < steps) count(kept[j]);
+    }
+#pragma unroll 4
+    for (int i = behind; i < steps; i++) count(fetch(4 * (piece0 + 64 * i)));
     zeros = __builtin_amdgcn_readlane(wave_scan(zeros), 63);
     if (lane == 0 && zeros > 0) {
       atomicAdd(&counts[kZero >> 21], zeros);
@@ -152,16 +176,15 @@ __global__ void __launch_bounds__(THREADS, 8) select_kernel(const SelectParams p
     }
     if (find(0, 21)) {
       const unsigned digit = border.rank >> 21;
-      for (int i = 0; i < steps; i++) {
-        const u32x4 x = four(i);
-        int mine = 0;
+      over([&](int, const u32x4 x) __attribute__((always_inline)) {
+        int have = 0;
 #pragma unroll
-        for (int k = 0; k < 4; k++) mine += x[k] >> 21 == digit && x[k] != kZero ? 1 : 0;
-        if (!__any(mine != 0)) continue;
-        const int upto = wave_scan(mine);
+        for (int k = 0; k < 4; k++) have += x[k] >> 21 == digit && x[k] != kZero ? 1 : 0;
+        if (!__any(have != 0)) return;
+        const int upto = wave_scan(have);
         int at = 0;
         if (lane == 63) at = atomicAdd(&n_list, upto);
-        at = __builtin_amdgcn_readlane(at, 63) + upto - mine;
+        at = __builtin_amdgcn_readlane(at, 63) + upto - have;
 #pragma unroll
         for (int k = 0; k < 4; k++)
           if (x[k] >> 21 == digit && x[k] != kZero) {
@@ -169,7 +192,7 @@ __global__ void __launch_bounds__(THREADS, 8) select_kernel(const SelectParams p
             if (at < kList) list[at] = x[k];
             at++;
           }
-      }
+      });
       if (tid == 0 && digit == kZero >> 21) atomicAdd(&counts[kDigits + (kZero >> 10 & 2047)], n_zeros);
       find(1, 10);
       const unsigned high = border.rank >> 10;
@@ -177,23 +200,22 @@ __global__ void __launch_bounds__(THREADS, 8) select_kernel(const SelectParams p
         for (int i = tid; i < n_list; i += THREADS)
           if (list[i] >> 10 == high) atomicAdd(&counts[2 * kDigits + (list[i] & 1023)], 1);
       } else {
-        for (int i = 0; i < steps; i++) {
-          const u32x4 x = four(i);
+        over([&](int, const u32x4 x) __attribute__((always_inline)) {
 #pragma unroll
           for (int k = 0; k < 4; k++)
             if (x[k] >> 10 == high && x[k] != kZero) atomicAdd(&counts[2 * kDigits + (x[k] & 1023)], 1);
-        }
+        });
       }
       if (tid == 0 && high == kZero >> 10) atomicAdd(&counts[2 * kDigits], n_zeros);
       find(2, 0);
     }
     // what the waves in front have: keys above the border, and those equal to it
     int above = 0, same = 0;
-    for (int i = 0; i < steps; i++) {
-      const int sum = sum_four(border, four(i));
+    over([&](int, const u32x4 x) __attribute__((always_inline)) {
+      const int sum = sum_four(border, x);
       above += sum & 0xffff;
       same += sum >> 16;
-    }
+    });
     above = wave_scan(above);
     same = wave_scan(same);
     if (lane == 63) {
@@ -205,13 +227,12 @@ __global__ void __launch_bounds__(THREADS, 8) select_kernel(const SelectParams p
     same = lane < wave ? sums[1][lane] : 0;
     above = __builtin_amdgcn_readlane(wave_scan(above), 63);
     same = __builtin_amdgcn_readlane(wave_scan(same), 63);
-    for (int i = 0; i < steps; i++) {
-      const u32x4 x = four(i);
-      const int mine = sum_four(border, x), upto = wave_scan(mine), before = upto - mine, all = __builtin_amdgcn_readlane(upto, 63);
+    over([&](int i, const u32x4 x) __attribute__((always_inline)) {
+      const int sum = sum_four(border, x), upto = wave_scan(sum), before = upto - sum, all = __builtin_amdgcn_readlane(upto, 63);
       write_four(out, border, 4 * (piece0 + 64 * i), x, above + (before & 0xffff), same + (before >> 16));
       above += all & 0xffff;
       same += all >> 16;
-    }
+    });
     __syncthreads();
   }
 }
@@ -350,11 +371,11 @@ __global__ void __launch_bounds__(kKeepThreads) keep_kernel(const KeepParams p, 
 }  // namespace
 
 namespace {
-template <int THREADS>
+template <int THREADS, int EXTRA>
 hipError_t launch_select(const SelectParams& p, int room, dim3 grid, hipStream_t stream) {
   static std::atomic<uint64_t> raised;
-  const hipError_t e = raise_lds(select_kernel<THREADS>, raised, kRoom * 4);
-  return e != hipSuccess ? e : launch_kernel(select_kernel<THREADS>, grid, dim3(THREADS), room * 4, stream, p, room);
+  const hipError_t e = raise_lds(select_kernel<THREADS, EXTRA>, raised, kRoom * 4);
+  return e != hipSuccess ? e : launch_kernel(select_kernel<THREADS, EXTRA>, grid, dim3(THREADS), room * 4, stream, p, room);
 }
 }  // namespace
 
@@ -363,8 +384,11 @@ hipError_t launch_cache_select(const SelectParams& p, hipStream_t stream) {
   const dim3 grid((unsigned)(rows < 65536 ? rows : 65536));
   const int64_t max_keys = (int64_t)p.seq.max_pages * p.seq.page_size;
   const int room = (int)(max_keys < kRoom ? (max_keys + 4095) / 4096 * 4096 : kRoom);   // LDS for what the table has room for
-  // With a row for every compute unit, smaller workgroups, two a unit, are less work: 512 rows of 4608 keys 13.2 us, with 1024 threads 14.2, with 256 14.7; 8 rows of 32768 keys 29.6, 22.3 and 50.7.
-  return rows >= 256 ? launch_select<512>(p, room, grid, stream) : launch_select<1024>(p, room, grid, stream);
+  // With a row for every compute unit, smaller workgroups, two a unit, are less work, as long as LDS holds the ranks of two: 512 rows of 4608 keys 12.7 us, with 1024 threads about 1 more, with 256 1.5; 8 rows of
+  // 32768 keys 21.7, with 512 threads 7 more, with 256 28; 512 rows of 14500 33.3 with 512 threads, 28.2 with 1024.  Registers for another 32768 ranks, where the table has room for so many: 8 rows of 65536 keys 42.7 -> 30.3, 256 of 40000 42.3 -> 30.
+  constexpr int kTwoRows = 12288;
+  if (max_keys > kRoom) return launch_select<1024, 8>(p, room, grid, stream);
+  return rows >= 256 && max_keys <= kTwoRows ? launch_select<512, 0>(p, room, grid, stream) : launch_select<1024, 0>(p, room, grid, stream);
 }
 
 namespace {

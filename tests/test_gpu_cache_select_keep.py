@@ -75,6 +75,37 @@ def test_select_long(lib):
     assert torch.equal(keys[0, 0].long(), ref) and count.tolist() == [20000]
 
 
+@pytest.mark.parametrize("zeros", [0.0, 0.6])
+@pytest.mark.parametrize("kv,most,table", [
+    ([32768], 5000, 0), ([32769], 32768, 0), ([32800, 36864, 36865, 17], 20000, 0), ([65536, 65535, 0, 40000], 33000, 0), ([65537, 98304], 3, 0),
+    ([5000, 32768, 30001], 2222, 40000),               # a table with room for more
+    ([12289, 300, 12288] * 44, 6000, 0),               # more rows than compute units
+])
+def test_select_where_ranks_are_held(lib, kv, most, table, zeros):
+    """Rows that LDS holds, that take registers too, and that are held nowhere from some key on; equal weights, and pages that are none."""
+    c = Cache(kv, [0] * len(kv), 2, 64, 16, False, seed=6)
+    g = torch.Generator().manual_seed(len(kv))
+    w = torch.rand(c.n_pages, 2, 16, generator=g)
+    w[torch.rand(w.shape, generator=g) < zeros] = 0
+    w = (w * 500).round().div(500).cuda() if len(kv) % 2 else w.cuda()
+    if table:
+        c.table = torch.cat([c.table, torch.zeros(len(kv), table // 16 - c.table.shape[1], dtype=torch.int32, device="cuda")], 1)
+    c.table[0, 2] = -1
+    keys, count = torch.full((len(kv), 2, most), -7, dtype=torch.int32, device="cuda"), torch.zeros(len(kv), dtype=torch.int32, device="cuda")
+    first, last = min(4, most // 2), min(100, most // 2)
+    lib.tr_cache_select(w, c.table, c.kv_len, first, last, keys, count)
+    assert count.tolist() == [min(n, most) for n in kv]
+    for b, n in enumerate(kv):
+        page = c.table[b].long().repeat_interleave(16)[:n]
+        for h in range(2):
+            x = torch.where(page >= 0, w[page.clamp(min=0), h, torch.arange(n, device="cuda") % 16], -1.0)
+            x[:first] = math.inf
+            x[n - min(last, n):] = math.inf
+            m = min(n, most)
+            ref = x.sort(descending=True, stable=True).indices[:m].sort().values
+            assert torch.equal(keys[b, h, :m].long(), ref) and (keys[b, h, m:] == -7).all()
+
+
 def _tensors(c, weights):
     t = {}
     for name in "kv":
