@@ -382,7 +382,7 @@ size_t tr_paged_attn_tree_workspace_bytes(const tr_tensor* q, const tr_tensor* k
  * A token whose lse is not finite (it saw nothing, or a NaN) adds nothing; what its row of q or a masked key holds reaches no weight.  Keys that no token sees keep their weight, slots
  * that hold no key of a sequence with new tokens are not touched.  Scores and sums are in fp32.  A page that several sequences of the call share gets the sum of
  * one of them (or a mixture): weigh such sequences in calls of their own.  The result is otherwise bitwise reproducible.  At most 2^16 sequences, found in time that grows with their square, as
- * in tr_paged_attn; S * Hq below 2^30.  Nothing is allocated; may be captured.
+ * in tr_paged_attn; S * Hq below 2^30, n_seqs * Hkv * (max_pages * page_size / 64, rounded up) below 2^31 - 8.  Nothing is allocated; may be captured.
  */
 tr_status tr_cache_weigh(const tr_tensor* q, const tr_tensor* lse, const tr_tensor* k_pages, const tr_tensor* k_scales, const tr_sequences* seqs,
                          int causal, float scale, int fresh, const tr_tensor* weights, void* hip_stream);

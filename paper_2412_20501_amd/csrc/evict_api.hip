@@ -85,7 +85,8 @@ tr_status tr_cache_weigh(const tr_tensor* q_, const tr_tensor* lse_, const tr_te
   SeqViews views;
   if ((st = take_sequences(seqs, k_pages, q->S, p.seq, views)) != TR_OK) return st;
   if (seqs->n_seqs > tr::kMaxAttended) return fail(TR_ERR_SHAPE, "%lld sequences, one call weighs for 2^16 at most", (long long)seqs->n_seqs);
-  if ((double)seqs->n_seqs * (double)k_pages->H * (double)((seqs->max_pages * k_pages->S + 63) / 64) >= 0x1p31) return fail(TR_ERR_SHAPE, "too many keys for one call (sequences * Hkv * keys / 64 must stay below 2^31)");
+  // (the kernels round the number of stretches of keys up to a multiple of 8)
+  if ((double)seqs->n_seqs * (double)k_pages->H * (double)((seqs->max_pages * k_pages->S + 63) / 64) >= 0x1p31 - 8) return fail(TR_ERR_SHAPE, "too many keys for one call (sequences * Hkv * keys / 64 must stay below 2^31 - 8)");
   const tr_tensor* const written[] = {weights};
   const tr_tensor* const read[] = {q, lse, k_pages, k_scales};
   if ((st = check_apart(written, 1, read, 4, views)) != TR_OK) return st;
