@@ -424,7 +424,7 @@ tr_status tr_cache_keep(const tr_tensor* k_pages, const tr_tensor* v_pages, cons
  * from this thread carries them in its dispatch: start_event then holds the time the kernel
  * began executing and stop_event the time it finished, so hipEventElapsedTime(start, stop)
  * is the kernel's own duration without queueing gaps.  Only that one launch is timed
- * (tr_ring_attn, tr_paged_attn, tr_paged_attn_tree: its first kernel; a block step whose keys are cut: its attention, not the fold); the events stay owned by the caller.  Always TR_OK.
+ * (tr_ring_attn, tr_paged_attn, tr_paged_attn_tree, tr_cache_weigh: its first kernel; a block step whose keys are cut: its attention, not the fold); the events stay owned by the caller.  Always TR_OK.
  */
 tr_status tr_time_next_kernel(void* start_event, void* stop_event);
 

@@ -7,6 +7,7 @@
 
 #include "evict.h"
 #include "paged_sums.h"
+#include "weigh_plan.h"
 
 namespace tr {
 namespace {
@@ -18,7 +19,6 @@ typedef float f32x16 __attribute__((ext_vector_type(16)));
 
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr int kFewWaves = 4;     // a SIMD, of few rows
-constexpr int kFewKeys = 256;    // of an item of few rows: 64 a wave
 constexpr int kTogetherBelow = 192, kTogetherInMixture = 128;   // items of many rows
 constexpr int kManyKeys = 256;   // of many rows: 64 a wave, or, where that leaves compute units without an item, 64 that the waves have together
 
@@ -399,16 +399,18 @@ __device__ __forceinline__ void weigh_many(const WeighParams& p, const RowClass&
   else weigh_rows<D, F8, false>(p, c, plan, lds);
 }
 
-// The sequences of a call are all of either kind, or a mixture: then half of the workgroups begin with one and half with the other, so that the loads of few rows and the products of many run at
-// the same time (a prompt of 700 tokens among 15 single ones, 24 heads of 64, 4000 keys: 51 us, in two launches 56).  Fewer than 8 sequences are not worth it: all are taken for ones of many rows.
+// In a mixture half of the workgroups begin with one kind of sequences and half with the other, so that the loads of few rows and the products of many run at
+// the same time (a prompt of 700 tokens among 15 single ones, 24 heads of 64, 4000 keys: 51 us, in two launches 56).
 // Few keys meet many rows sooner here (8 heads of 128 for 32: a prompt of 512 on 2000 keys among 15 54 -> 32 us with 64 keys a workgroup, of 256 on 3900 45 -> 42, but on 5000 44 -> 51).
 constexpr RowClass kAny = {32, 0, 0x7fffffff}, kFewRows = {32, 0, 32}, kManyMore = {32, 32, 0x7fffffff};
-template <int D, bool F8>
-__global__ void __launch_bounds__(256, kFewWaves) weigh_few_kernel(const WeighParams p) { weigh_few<D, F8>(p, kAny, sums_plan(p), (int)blockIdx.x >> 3); }
-template <int D, bool F8>
+template <int D, bool F8, bool APART>   // APART: the other launch has the other sequences
+__global__ void __launch_bounds__(256, kFewWaves) weigh_few_kernel(const WeighParams p) {
+  weigh_few<D, F8>(p, APART ? RowClass{32, 0, kApartRows} : kAny, sums_plan(p), (int)blockIdx.x >> 3);
+}
+template <int D, bool F8, bool APART>
 __global__ void __launch_bounds__(256, 2) weigh_many_kernel(const WeighParams p) {
   __shared__ __attribute__((aligned(1024))) char lds[Many<D>::LDS];
-  weigh_many<D, F8>(p, kAny, sums_plan(p), kTogetherBelow, lds);
+  weigh_many<D, F8>(p, APART ? RowClass{32, kApartRows, 0x7fffffff} : kAny, sums_plan(p), kTogetherBelow, lds);
 }
 template <int D, bool F8>
 __global__ void __launch_bounds__(256, 2) weigh_mixed_kernel(const WeighParams p) {
@@ -424,18 +426,16 @@ __global__ void __launch_bounds__(256, 2) weigh_mixed_kernel(const WeighParams p
 
 template <int D, bool F8>
 hipError_t launch_form(const WeighParams& p, hipStream_t stream) {
-  const int64_t rows = (int64_t)p.seq.tokens * p.gq, n = p.seq.n, max_keys = (int64_t)p.seq.max_pages * p.seq.page_size;
-  // On average few: single tokens and drafts; but where a sequence may have many (not all the same number of tokens), and short keys leave the compute units room, a mixture (16 sequences of 300 keys
-  // with a prompt of 100 29.1 -> 10.7 us, 9 of 27 with one of 23 13.9 -> 7.7; drafts of different numbers lose: 16 of 5 on 400 keys 6.8 -> 7.2).
-  const bool short_keys = n * p.Hkv * ((max_keys + kFewKeys - 1) / kFewKeys) <= 512;
-  const bool few = rows <= 32 * n && !(n >= 8 && short_keys && p.seq.tokens % n != 0 && (p.seq.tokens - n + 1) * (int64_t)p.gq > 32);
-  const int64_t width = few ? kFewKeys : 64, items = n * p.Hkv * ((max_keys + width - 1) / width);
-  const int64_t most = few ? 256 * kFewWaves : 512;   // workgroups that the compute units hold
-  const int64_t wanted = items + (few || n < 8 ? 0 : 8);   // (a mixture's two kinds are rounded up apart)
-  const dim3 grid((unsigned)((wanted < most ? wanted : most) + 7) / 8 * 8), block(256);
-  if (few) return launch_kernel(weigh_few_kernel<D, F8>, grid, block, 0, stream, p);
-  if (n < 8) return launch_kernel(weigh_many_kernel<D, F8>, grid, block, 0, stream, p);
-  return launch_kernel(weigh_mixed_kernel<D, F8>, grid, block, 0, stream, p);
+  const int64_t max_keys = (int64_t)p.seq.max_pages * p.seq.page_size;
+  const WeighForm form = weigh_form(p.seq.tokens, p.seq.n, p.gq, p.Hkv, max_keys);
+  auto items = [&](int64_t width) { return (int64_t)p.seq.n * p.Hkv * ((max_keys + width - 1) / width); };
+  auto grid = [](int64_t wanted, int64_t most) { return dim3((unsigned)((wanted < most ? wanted : most) + 7) / 8 * 8); };   // most: workgroups that the compute units hold
+  const dim3 block(256), few = grid(items(kFewKeys), 256 * kFewWaves), many = grid(items(64), 512), both = grid(items(64) + 8, 512);   // (a mixture's two kinds are rounded up apart)
+  if (form == kWeighFew) return launch_kernel(weigh_few_kernel<D, F8, false>, few, block, 0, stream, p);
+  if (form == kWeighMany) return launch_kernel(weigh_many_kernel<D, F8, false>, many, block, 0, stream, p);
+  if (form == kWeighMixed) return launch_kernel(weigh_mixed_kernel<D, F8>, both, block, 0, stream, p);
+  const hipError_t e = launch_kernel(weigh_few_kernel<D, F8, true>, few, block, 0, stream, p);
+  return e != hipSuccess ? e : launch_kernel(weigh_many_kernel<D, F8, true>, many, block, 0, stream, p);
 }
 
 }  // namespace
