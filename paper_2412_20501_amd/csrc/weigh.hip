@@ -19,7 +19,7 @@ typedef float f32x16 __attribute__((ext_vector_type(16)));
 
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr int kFewWaves = 4;     // a SIMD, of few rows
-constexpr int kTogetherBelow = 192, kTogetherInMixture = 128;   // items of many rows
+constexpr int kTogetherBelow = 192, kTogetherInMixture = 128, kSmallMixture = 8;   // items of many rows; sequences
 constexpr int kManyKeys = 256;   // of many rows: 64 a wave, or, where that leaves compute units without an item, 64 that the waves have together
 
 // Items: (sequence, K/V head, stretch of keys) of the launch's sequences, numbered so that those of a head lie together, and each XCD has a contiguous eighth of all.
@@ -401,7 +401,8 @@ __device__ __forceinline__ void weigh_many(const WeighParams& p, const RowClass&
 
 // In a mixture half of the workgroups begin with one kind of sequences and half with the other, so that the loads of few rows and the products of many run at
 // the same time (a prompt of 700 tokens among 15 single ones, 24 heads of 64, 4000 keys: 51 us, in two launches 56).
-// Few keys meet many rows sooner here (8 heads of 128 for 32: a prompt of 512 on 2000 keys among 15 54 -> 32 us with 64 keys a workgroup, of 256 on 3900 45 -> 42, but on 5000 44 -> 51).
+// Few keys meet many rows sooner here (8 heads of 128 for 32: a prompt of 512 on 2000 keys among 15 54 -> 32 us with 64 keys a workgroup, of 256 on 3900 45 -> 42, but on 5000 44 -> 51), unless the
+// sequences are a handful, which may all have many (2 of 100 tokens on 4000 keys 13 us, with the other limit 20, 4 of 128 on 1000 17.6 and 19.9; mixtures lose by that: 7 with a prompt of 256 on 4500 42 and 36).
 constexpr RowClass kAny = {32, 0, 0x7fffffff}, kFewRows = {32, 0, 32}, kManyMore = {32, 32, 0x7fffffff};
 template <int D, bool F8, bool APART>   // APART: the other launch has the other sequences
 __global__ void __launch_bounds__(256, kFewWaves) weigh_few_kernel(const WeighParams p) {
@@ -419,7 +420,7 @@ __global__ void __launch_bounds__(256, 2) weigh_mixed_kernel(const WeighParams p
   const int first = (int)blockIdx.x >> 3 & 1;
 #pragma unroll 1
   for (int turn = 0; turn < 2; turn++) {
-    if (turn == first) weigh_many<D, F8>(p, kManyMore, plan, kTogetherInMixture, lds);
+    if (turn == first) weigh_many<D, F8>(p, kManyMore, plan, p.seq.n < kSmallMixture ? kTogetherBelow : kTogetherInMixture, lds);
     else weigh_few<D, F8>(p, kFewRows, plan, ((int)gridDim.x - 1 - (int)blockIdx.x) >> 3);   // (from the last workgroup on: where there are few items, none has one of either kind)
   }
 }

@@ -26,6 +26,7 @@ int main() {
       EXPECT(rows > 32 || form == tr::kWeighFew);
       EXPECT(form != tr::kWeighApart || rows > tr::kApartRows);
       EXPECT(n > 1 || form == (rows <= 32 ? tr::kWeighFew : tr::kWeighMany));
+      EXPECT(n == 1 || form != tr::kWeighMany);   // (others beside it may have single tokens)
       EXPECT(!left || form != tr::kWeighFew);   // a token more never goes back
       left |= form != tr::kWeighFew;
     }
