@@ -386,6 +386,7 @@ hipError_t launch_cache_select(const SelectParams& p, hipStream_t stream) {
   const int room = (int)(max_keys < kRoom ? (max_keys + 4095) / 4096 * 4096 : kRoom);   // LDS for what the table has room for
   // With a row for every compute unit, smaller workgroups, two a unit, are less work, as long as LDS holds the ranks of two: 512 rows of 4608 keys 12.7 us, with 1024 threads about 1 more, with 256 1.5; 8 rows of
   // 32768 keys 21.7, with 512 threads 7 more, with 256 28; 512 rows of 14500 33.3 with 512 threads, 28.2 with 1024.  Registers for another 32768 ranks, where the table has room for so many: 8 rows of 65536 keys 42.7 -> 30.3, 256 of 40000 42.3 -> 30.
+  // What the rows need lies on the device, so a table with room for more costs short rows: with room for 16K (64K) keys 512 rows of 4608 take 18.7 us (19.4) for 12.6, of 1000 keys 13.6 (14.8) for 7.8, 8 of 4608 9.1 (9.7) for 9.1.
   constexpr int kTwoRows = 12288;
   if (max_keys > kRoom) return launch_select<1024, 8>(p, room, grid, stream);
   return rows >= 256 && max_keys <= kTwoRows ? launch_select<512, 0>(p, room, grid, stream) : launch_select<1024, 0>(p, room, grid, stream);
@@ -402,8 +403,8 @@ hipError_t launch_keep(const KeepParams& p, int pieces, hipStream_t stream) {
 
 hipError_t launch_cache_keep(const KeepParams& p, hipStream_t stream) {
   const int pieces = (int64_t)p.seq.n * p.heads * 2 >= 256 || p.row_bytes < 128 ? 1 : p.row_bytes / 64, lanes = p.row_bytes / pieces / 16;
-  // Long lists: more entries between two barriers, if fewer workgroups share a compute unit (64 lists of up to 4608 keys on 8 heads of 128 bytes 247 -> 238 us, of 256 bytes 467 -> 456, one of 32768 53 -> 46; but
-  // of 600 keys 23 -> 42).
+  // Long lists: more entries between two barriers, if fewer workgroups share a compute unit (64 lists of up to 4608 keys on 8 heads of 128 bytes 247 -> 238 us, of 256 bytes 467 -> 456, one of 32768 53 -> 46).
+  // Their length lies on the device, so lists with room for more than they hold lose: 64 of 600 keys in 8 bits 28 -> 44, of 2000 96 -> 109, 8 of 600 9.3 -> 13.5.
   const bool many = p.most > 2048;
   if (lanes == 16) return many ? launch_keep<16, 2>(p, pieces, stream) : launch_keep<16, 1>(p, pieces, stream);
   if (lanes == 8) return many ? launch_keep<8, 4>(p, pieces, stream) : launch_keep<8, 1>(p, pieces, stream);

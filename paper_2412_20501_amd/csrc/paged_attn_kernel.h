@@ -60,7 +60,7 @@ struct Item {
 // Rows of a tile see keys 0 .. limit(row) - 1; row r of a sequence and K/V head is query head r mod gq of token r / gq.
 __device__ __forceinline__ int row_limit(const PagedParams& p, const Sequence& q, int r) { return visible(q, divide(p.by_gq, r), p.causal); }
 // What all rows of a tile see whose first row is r, and what some row of one sees whose last row is r.  In a tree all rows see the keys in front of the drafts; behind them a row's bits take the place of its limit, read where a
-// stretch of keys reaches there (tree_bits), which costs a load of one or two words a row and 32 keys: 512 tokens in 8 branches behind 30K keys 245 us, 1.03 PFLOP/s, 16 trees of 25 tokens on 2K to 4K keys in 8 bits 61 us.
+// stretch of keys reaches there (tree_bits), which costs a load of one or two words a row and 32 keys: 512 tokens in 8 branches behind 30K keys 245 us, 1.03 PFLOP/s, 16 trees of 25 tokens on 2K to 4K keys in 8 bits 60 us.
 __device__ __forceinline__ int first_limit(const PagedParams& p, const Sequence& q, int r) { return row_limit(p, q, r); }
 __device__ __forceinline__ int first_limit(const TreeParams& p, const Sequence& q, int r) { return visible_to_all(q); }
 __device__ __forceinline__ int last_limit(const PagedParams& p, const Sequence& q, int r) { return row_limit(p, q, r); }

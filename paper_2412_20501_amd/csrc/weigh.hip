@@ -175,8 +175,8 @@ __device__ __forceinline__ void weigh_few(const WeighParams& p, const RowClass& 
 // Many rows (a prompt's chunk): every wave has 64 keys in registers, as the A operand of S^T = K Q^T with 32x32x16 products, and goes through the rows 32 at a time, which the workgroup brings into
 // LDS.  A lane then has one row's scores with 32 of the keys, so one reference a tile, and sums of its own for each key, which are added up over the lanes once at the end.  The keys' two blocks of 32 take
 // turns: one's exponentials run beside the other's products.
-// Bound: the vector unit: a score is 2 D flops on the matrix cores, 4 cycles of 64 scores at D 128, and an exponential of 16, a fused multiply-add and an addition of 4 each in quarters of them: 24 cycles for
-// 16 of products, with about a quarter more for rows and masks.  2048 tokens of 32 heads of 128 on 32K keys 547 us, 0.98 PFLOP/s (exponentials behind all products of a tile 655; four waves of 32 keys
+// Bound: the vector unit: 64 scores at D 128 take the matrix core of a SIMD 16 cycles and its vector unit 24, an exponential of 16 and a fused multiply-add and an addition of 4 each, with about a quarter more
+// for rows and masks.  2048 tokens of 32 heads of 128 on 32K keys 547 us, 0.98 PFLOP/s (exponentials behind all products of a tile 655; four waves of 32 keys
 // a SIMD, which overlap by themselves, 631).
 // Where few keys meet many rows (a prompt's first chunk) 256 keys a workgroup leave compute units without any: the waves then have the same 64 keys and every fourth tile of rows, whose operands they
 // read from memory themselves (2048 tokens on themselves 171 -> 67 us, 500 50 -> 21; but 2048 on 8192 keys, an item for every unit, 189 -> 264).
